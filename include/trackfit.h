@@ -389,6 +389,100 @@ int64_t trackfit_debug_alloc(int64_t fail_nth, int64_t* attempted);
 int trackfit_forward_noalloc(const trackfit_config_t* cfg, const float* weights, const float* hits,
                              const int32_t* n_hits, int64_t n_tracks, float* out_params, void* stream);
 
+/* ---- Operators on packed sequences -------------------------------------------------
+ * The steps between the projections of an encoder layer other than this library's own
+ * layers, on the packed layout of trackfit_forward_packed: the rows of all sequences
+ * back to back, offsets [n_seq + 1] int64 (sequence b = rows offsets[b] ..
+ * offsets[b + 1] - 1; non-decreasing, within the rows; empty sequences are allowed).
+ * The paper's encoder comparison (App. A.3, Tab. A.1) has such encoders beside the
+ * minGRU; none of these operators is tied to a model.
+ *   dtype    type of the row arrays: TRACKFIT_FP32, TRACKFIT_BF16_PROJ (bf16) or
+ *            TRACKFIT_FP16_PROJ (fp16).  Sums, softmax statistics, norms and states
+ *            are fp32 whatever the type.
+ *   strides  elements from a row to the next; heads stand side by side within a row,
+ *            so q, k and v may be column blocks of one projection.
+ * Row arrays are device memory, 16-byte aligned, rows too (stride x element size a
+ * multiple of 16); state arrays fp32, contiguous, 16-byte aligned; fp32 and int32
+ * vectors 4-byte, int64 ones 8-byte aligned.  Widths of heads are multiples of 8 up to
+ * 128, heads at most 256.  Outputs may not overlap inputs unless a function says so;
+ * rows that belong to no sequence are neither read nor written.  Offsets that break the
+ * rule leave the outputs undefined, but no access leaves the arrays.
+ * Asynchronous on `stream`, whose device is the current one and holds the arrays; no
+ * allocation, no host synchronisation; capturable.  Calls that may run at the same time
+ * need workspaces of their own (as two graphs that are replayed side by side do).
+ * n_rows = 0, n_q_rows = 0 and n_seq = 0 are valid.  Errors: INVALID_ARG (NULL,
+ * misalignment, negative counts, a stride below the row's width, a workspace too small,
+ * values that are not finite), UNSUPPORTED (widths, heads), CUDA. */
+
+/* Norms of queries and keys for each head, with the position rotation in the same pass.
+ *   y = x / sqrt(mean(x^2) + eps) * gain over a head's channels, then, for
+ *   i < rot_dim / 2, (y_i, y_{i + rot_dim/2}) turned by the angle
+ *   positions[row] * rot_base^(-2 i / rot_dim).
+ *   q, q_out   [n_rows][q_heads][head_dim]; q_out may be q itself (same stride).
+ *   k, k_out   [n_rows][k_heads][head_dim], likewise; NULL with k_heads = 0.
+ *   q_gain, k_gain  device fp32 [head_dim], or NULL (ones).
+ *   positions  device int32 [n_rows], any values (angles keep 2^-32 of a turn however far
+ *              the position); may be NULL with rot_dim = 0.
+ *   rot_dim    a multiple of 16 in [0, head_dim]; the channels from rot_dim on are
+ *              normalised only.  rot_base >= 1, eps > 0. */
+int trackfit_qk_norm(int32_t dtype, const void* q, int64_t q_stride, int32_t q_heads, const void* k,
+                     int64_t k_stride, int32_t k_heads, int32_t head_dim, int64_t n_rows, const float* q_gain,
+                     const float* k_gain, float eps, const int32_t* positions, int32_t rot_dim, double rot_base,
+                     void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
+
+/* Linear attention with a decay for each head: along each sequence, for each head,
+ *   S_t = exp(g_t) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t
+ * with S of key_dim x value_dim: the gated recurrence of Eq. 2 with a matrix for a state.
+ *   q, k        [n_rows][n_heads][key_dim]; v, out [n_rows][n_heads][value_dim].
+ *   log_decay   device fp32 [n_rows][decay_stride], the first n_heads of a row used: g,
+ *               meant to be <= 0; -inf forgets all that was before.
+ *   reverse     0: from a sequence's first row to its last; 1: from its last to its first.
+ *   state_in    fp32 [n_seq][n_heads][key_dim][value_dim] to begin with, or NULL (zeros).
+ *   state_out   the same shape, the state after each sequence, or NULL; may be state_in.
+ *   workspace   trackfit_linear_attention_workspace() bytes, 16-byte aligned (sequences
+ *               of more than 512 rows are cut and their parts joined through it; NULL
+ *               when that is 0). */
+size_t trackfit_linear_attention_workspace(int64_t n_rows, int32_t n_heads, int32_t key_dim, int32_t value_dim);
+int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, const float* log_decay, int64_t decay_stride,
+                              int64_t n_rows, const int64_t* offsets, int64_t n_seq, int32_t n_heads, int32_t key_dim,
+                              int32_t value_dim, float scale, int32_t reverse, const float* state_in,
+                              float* state_out, void* out, int64_t out_stride, void* workspace,
+                              size_t workspace_size, void* stream);
+
+/* One row more of each of n_seq sequences: the step of trackfit_linear_attention.
+ *   q, k, v, log_decay, out   as there, row b for sequence b.
+ *   slots       device int32 [n_seq]: sequence b's state is state_in[slots[b]], and goes to
+ *               state_out[slots[b]]; NULL: state b.  A slot outside [0, n_slots) reads and
+ *               writes no state and gets a NaN row (a padded batch); no slot may occur
+ *               twice.
+ *   state_in, state_out   fp32 [n_slots][n_heads][key_dim][value_dim], n_slots >= n_seq
+ *               without slots; the same array, or two that do not overlap.  Slots that do
+ *               not occur are left as they are. */
+int trackfit_linear_attention_step(int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                   const void* v, int64_t v_stride, const float* log_decay, int64_t decay_stride,
+                                   int64_t n_seq, int32_t n_heads, int32_t key_dim, int32_t value_dim, float scale,
+                                   const int32_t* slots, int64_t n_slots, const float* state_in, float* state_out,
+                                   void* out, int64_t out_stride, void* stream);
+
+/* Attention of the queries of each sequence to the states of the sequence with the same
+ * number in another packed array, of any other length:
+ *   o_i = sum_j softmax_j(scale q_i . k_j) v_j.
+ *   q, out      [n_q_rows][q_heads][head_dim], sequences by q_offsets.
+ *   k, v        [n_kv_rows][kv_heads][head_dim], sequences by kv_offsets; head h of the
+ *               queries reads head h / (q_heads / kv_heads).
+ * A query whose sequence has no states gets zeros.
+ *   workspace   trackfit_cross_attention_workspace() bytes, 16-byte aligned (few queries:
+ *               the states are split and the parts joined through it; NULL when that is
+ *               0). */
+size_t trackfit_cross_attention_workspace(int32_t dtype, int64_t n_q_rows, int64_t n_kv_rows, int64_t n_seq,
+                                          int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, const int64_t* q_offsets,
+                             int64_t n_q_rows, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                             const int64_t* kv_offsets, int64_t n_kv_rows, int64_t n_seq, int32_t q_heads,
+                             int32_t kv_heads, int32_t head_dim, float scale, void* out, int64_t out_stride,
+                             void* workspace, size_t workspace_size, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

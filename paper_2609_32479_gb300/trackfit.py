@@ -27,7 +27,9 @@ EXPORTS = ("trackfit_weight_count", "trackfit_create", "trackfit_forward", "trac
            "trackfit_destroy", "trackfit_strerror", "trackfit_debug_scan", "trackfit_debug_umma",
            "trackfit_profile", "trackfit_profile_read", "trackfit_forward_noalloc",
            "trackfit_debug_schedule", "trackfit_debug_wait_limit", "trackfit_debug_alloc", "trackfit_seed",
-           "trackfit_decode", "trackfit_forward_packed", "trackfit_last_error")
+           "trackfit_decode", "trackfit_forward_packed", "trackfit_last_error", "trackfit_qk_norm",
+           "trackfit_linear_attention", "trackfit_linear_attention_workspace", "trackfit_linear_attention_step",
+           "trackfit_cross_attention", "trackfit_cross_attention_workspace")
 
 
 class Config(ctypes.Structure):
@@ -107,6 +109,23 @@ def load() -> ctypes.CDLL:
     lib.trackfit_decode.restype = ctypes.c_int
     lib.trackfit_forward_packed.argtypes = [vp, vp, i64, vp, i64, vp, vp]
     lib.trackfit_forward_packed.restype = ctypes.c_int
+    f32, f64, size = ctypes.c_float, ctypes.c_double, ctypes.c_size_t
+    lib.trackfit_qk_norm.argtypes = [i32, vp, i64, i32, vp, i64, i32, i32, i64, vp, vp, f32, vp, i32, f64,
+                                     vp, i64, vp, i64, vp]
+    lib.trackfit_qk_norm.restype = ctypes.c_int
+    lib.trackfit_linear_attention_workspace.argtypes = [i64, i32, i32, i32]
+    lib.trackfit_linear_attention_workspace.restype = size
+    lib.trackfit_linear_attention.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, i64, i32, i32, i32, f32,
+                                              i32, vp, vp, vp, i64, vp, size, vp]
+    lib.trackfit_linear_attention.restype = ctypes.c_int
+    lib.trackfit_linear_attention_step.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, f32,
+                                                   vp, i64, vp, vp, vp, i64, vp]
+    lib.trackfit_linear_attention_step.restype = ctypes.c_int
+    lib.trackfit_cross_attention_workspace.argtypes = [i32, i64, i64, i64, i32, i32, i32]
+    lib.trackfit_cross_attention_workspace.restype = size
+    lib.trackfit_cross_attention.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, f32,
+                                             vp, i64, vp, size, vp]
+    lib.trackfit_cross_attention.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -373,3 +392,160 @@ def decode(seed_t, corrections, out, stream=None) -> None:
                                 _dev(out, "torch.float32"), _stream_handle(stream))
     if st != OK:
         raise TrackfitError(st, "trackfit_decode")
+
+
+# ---- operators on packed sequences (include/trackfit.h)
+
+_ROW_TYPES = {"torch.float32": W.PRECISION_FP32, "torch.bfloat16": W.PRECISION_BF16,
+              "torch.float16": W.PRECISION_FP16}
+
+
+class _OpArgs:
+    """Checks the tensors of one operator call: all CUDA, on one device."""
+
+    def __init__(self, what: str, first):
+        self.what, self.device, self.dtype = what, first.device, str(first.dtype)
+        if not first.is_cuda or self.dtype not in _ROW_TYPES:
+            raise ValueError(f"{what}: expected CUDA rows of float32, bfloat16 or float16, got {self.dtype} on "
+                             f"{first.device}")
+
+    def rows(self, name, t, shape):
+        """(pointer, row stride) of [rows, heads, width], heads side by side within a row."""
+        if tuple(t.shape) != tuple(shape) or str(t.dtype) != self.dtype or t.device != self.device:
+            raise ValueError(f"{self.what}: {name} must be {list(shape)} {self.dtype} on {self.device}, got "
+                             f"{list(t.shape)} {t.dtype} on {t.device}")
+        n, h, d = shape
+        if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
+            raise ValueError(f"{self.what}: the heads of a row of {name} must stand side by side, got strides "
+                             f"{tuple(t.stride())}")
+        return t.data_ptr(), t.stride(0) if n > 1 else h * d
+
+    def vector(self, name, t, dtype_name, shape):
+        """Pointer of a contiguous array, None for None."""
+        if t is None:
+            return None
+        if tuple(t.shape) != tuple(shape) or str(t.dtype) != dtype_name or t.device != self.device \
+                or not t.is_contiguous():
+            raise ValueError(f"{self.what}: {name} must be contiguous {list(shape)} {dtype_name} on {self.device}, got "
+                             f"{list(t.shape)} {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    def decay(self, t, n, h):
+        if tuple(t.shape) != (n, h) or str(t.dtype) != "torch.float32" or t.device != self.device \
+                or (h > 1 and t.stride(1) != 1):
+            raise ValueError(f"{self.what}: log_decay must be [{n}, {h}] torch.float32 on {self.device} with unit "
+                             f"stride, got {list(t.shape)} {t.dtype}, strides {tuple(t.stride())}")
+        return t.data_ptr(), t.stride(0) if n > 1 else h
+
+    def call(self, fn, args, stream, need=0, workspace=None):
+        """fn(*args[, workspace, size], stream) with the tensors' device current.  Without a
+        workspace of the caller's, one from torch's allocator, in the order of the stream."""
+        import torch
+        with torch.cuda.device(self.device):
+            if stream is None:
+                handle = torch.cuda.current_stream().cuda_stream
+            else:
+                handle = getattr(stream, "cuda_stream", stream)
+            if need and workspace is None:
+                on = torch.cuda.ExternalStream(handle, device=self.device) if stream is not None else None
+                with torch.cuda.stream(on):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            if workspace is not None:
+                if workspace.device != self.device or not workspace.is_contiguous():
+                    raise ValueError(f"{self.what}: the workspace must be contiguous on {self.device}")
+                args = (*args, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+            elif need is not None:
+                args = (*args, None, 0)
+            st = fn(*args, handle)
+        if st != OK:
+            raise TrackfitError(st, f"trackfit_{self.what}")
+
+
+def qk_norm(q, k, q_out, k_out, q_gain=None, k_gain=None, eps: float = 1e-6, positions=None, rot_dim: int = 0,
+            rot_base: float = 10000.0, stream=None) -> None:
+    """Norms of queries [N, Hq, D] and keys [N, Hk, D] per head, gains [D] f32, and the
+    rotation of the first rot_dim channels by positions [N] i32 -> q_out, k_out (the
+    inputs themselves, or others).  k and k_out may both be None.  The rows' stride is
+    free: q and k may be column blocks of a projection."""
+    n, hq, d = q.shape
+    a = _OpArgs("qk_norm", q)
+    hk = 0 if k is None else int(k.shape[1])
+    if (k is None) != (k_out is None):
+        raise ValueError("qk_norm: k and k_out go together")
+    qp, qs = a.rows("q", q, (n, hq, d))
+    qop, qos = a.rows("q_out", q_out, (n, hq, d))
+    kp, ks = (None, 0) if k is None else a.rows("k", k, (n, hk, d))
+    kop, kos = (None, 0) if k is None else a.rows("k_out", k_out, (n, hk, d))
+    a.call(load().trackfit_qk_norm,
+           (_ROW_TYPES[a.dtype], qp, qs, hq, kp, ks, hk, d, n, a.vector("q_gain", q_gain, "torch.float32", (d,)),
+            a.vector("k_gain", k_gain, "torch.float32", (d,)), float(eps),
+            a.vector("positions", positions, "torch.int32", (n,)), int(rot_dim), float(rot_base), qop, qos, kop, kos),
+           stream, need=None)
+
+
+def linear_attention_workspace(n_rows: int, n_heads: int, key_dim: int, value_dim: int) -> int:
+    """Bytes of workspace of a linear_attention call."""
+    return int(load().trackfit_linear_attention_workspace(n_rows, n_heads, key_dim, value_dim))
+
+
+def linear_attention(q, k, v, log_decay, offsets, out, scale: float = 1.0, reverse: bool = False, state_in=None,
+                     state_out=None, workspace=None, stream=None) -> None:
+    """Linear attention with a decay a head: q, k [N, H, K], v, out [N, H, V], log_decay
+    [N, H] f32, offsets [B + 1] i64; states [B, H, K, V] f32 before and after, or None."""
+    n, h, dk = q.shape
+    dv = int(v.shape[2])
+    b = int(offsets.shape[0]) - 1
+    a = _OpArgs("linear_attention", q)
+    qp, qs = a.rows("q", q, (n, h, dk))
+    kp, ks = a.rows("k", k, (n, h, dk))
+    vp, vs = a.rows("v", v, (n, h, dv))
+    op, os_ = a.rows("out", out, (n, h, dv))
+    gp, gs = a.decay(log_decay, n, h)
+    a.call(load().trackfit_linear_attention,
+           (_ROW_TYPES[a.dtype], qp, qs, kp, ks, vp, vs, gp, gs, n, a.vector("offsets", offsets, "torch.int64", (b + 1,)),
+            b, h, dk, dv, float(scale), int(bool(reverse)),
+            a.vector("state_in", state_in, "torch.float32", (b, h, dk, dv)),
+            a.vector("state_out", state_out, "torch.float32", (b, h, dk, dv)), op, os_),
+           stream, need=linear_attention_workspace(n, h, dk, dv), workspace=workspace)
+
+
+def linear_attention_step(q, k, v, log_decay, state_in, state_out, out, scale: float = 1.0, slots=None,
+                          stream=None) -> None:
+    """One row more of each of B sequences: q, k [B, H, K], v, out [B, H, V], log_decay
+    [B, H] f32; states [slots, H, K, V] f32, taken from and put to slots [B] i32 (None: state
+    b).  A slot outside the states: a NaN row, no state."""
+    b, h, dk = q.shape
+    dv = int(v.shape[2])
+    a = _OpArgs("linear_attention_step", q)
+    ns = int(state_in.shape[0])
+    qp, qs = a.rows("q", q, (b, h, dk))
+    kp, ks = a.rows("k", k, (b, h, dk))
+    vp, vs = a.rows("v", v, (b, h, dv))
+    op, os_ = a.rows("out", out, (b, h, dv))
+    gp, gs = a.decay(log_decay, b, h)
+    a.call(load().trackfit_linear_attention_step,
+           (_ROW_TYPES[a.dtype], qp, qs, kp, ks, vp, vs, gp, gs, b, h, dk, dv, float(scale),
+            a.vector("slots", slots, "torch.int32", (b,)), ns,
+            a.vector("state_in", state_in, "torch.float32", (ns, h, dk, dv)),
+            a.vector("state_out", state_out, "torch.float32", (ns, h, dk, dv)), op, os_),
+           stream, need=None)
+
+
+def cross_attention(q, k, v, q_offsets, kv_offsets, out, scale: Optional[float] = None, workspace=None,
+                    stream=None) -> None:
+    """Attention of queries [Nq, Hq, D] to states k, v [Nk, Hk, D] of the same sequence:
+    q_offsets, kv_offsets [B + 1] i64 -> out [Nq, Hq, D].  scale: 1 / sqrt(D) by default."""
+    nq, hq, d = q.shape
+    nk, hk = int(k.shape[0]), int(k.shape[1])
+    b = int(q_offsets.shape[0]) - 1
+    a = _OpArgs("cross_attention", q)
+    qp, qs = a.rows("q", q, (nq, hq, d))
+    kp, ks = a.rows("k", k, (nk, hk, d))
+    vp, vs = a.rows("v", v, (nk, hk, d))
+    op, os_ = a.rows("out", out, (nq, hq, d))
+    lib, t = load(), _ROW_TYPES[a.dtype]
+    a.call(lib.trackfit_cross_attention,
+           (t, qp, qs, a.vector("q_offsets", q_offsets, "torch.int64", (b + 1,)), nq, kp, ks, vp, vs,
+            a.vector("kv_offsets", kv_offsets, "torch.int64", (b + 1,)), nk, b, hq, hk, d,
+            float(d) ** -0.5 if scale is None else float(scale), op, os_),
+           stream, need=int(lib.trackfit_cross_attention_workspace(t, nq, nk, b, hq, hk, d)), workspace=workspace)
