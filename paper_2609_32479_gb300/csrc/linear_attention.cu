@@ -11,25 +11,6 @@
 namespace {
 using namespace seqops;
 
-constexpr int NW = 4;            // warps of a CTA, each with a unit of its own
-constexpr int COLS = 32;         // channels of v that a warp takes
-
-struct LaArgs {
-  Units u;
-  const void *q, *k, *v;
-  const float* g;
-  void* out;
-  int64_t qs, ks, vs, gs, os;    // row strides in elements
-  const float* state_in;
-  float* state_out;
-  float* ws_state;               // [boundaries][H][K][V]
-  float* ws_decay;               // [boundaries][H], sums of g
-  int32_t* ws_flag;              // [boundaries]: 0 no cut sequence, 1 its first piece, 2 a later one
-  int64_t bounds;                // boundaries 1 .. bounds - 1
-  int H, K, V, slices;
-  float scale;
-};
-
 // A chunk of a piece: up to CH rows, in the direction of the recurrence.
 struct Chunk {
   int64_t row;                   // its first row
@@ -43,6 +24,7 @@ struct Chunk {
 // ---------------------------------------------------------------- CUDA cores
 // A lane holds a column of S: K values in registers.  The rows of q and k are the same for
 // all lanes and come from shared memory as broadcasts.
+constexpr int COLS = 32;         // channels of v that a warp takes
 constexpr int CH = 8, NST = 3;
 
 template <class T, int DK>
@@ -71,7 +53,7 @@ __global__ void __launch_bounds__(NW * 32) la_simt_kernel(const __grid_constant_
   const T* q = (const T*)a.q + h * a.K;
   const T* k = (const T*)a.k + h * a.K;
   const T* v = (const T*)a.v + h * a.V + c0;
-  TilePieces pieces(a.u, tile, lane);
+  TilePieces pieces(a.u, tile, lane, STATE_ONLY);
   Piece p;
   bool more;
   int64_t bound = 0;
@@ -291,8 +273,7 @@ int by_width(const LaArgs& a, cudaStream_t st) {
 template <bool STATE_ONLY>
 int by_type(int32_t dtype, const LaArgs& a, cudaStream_t st) {
   if (dtype == TRACKFIT_FP32) return by_width<float, STATE_ONLY>(a, st);
-  if (dtype == TRACKFIT_BF16_PROJ) return by_width<__nv_bfloat16, STATE_ONLY>(a, st);
-  return by_width<__half, STATE_ONLY>(a, st);
+  return linear_mma(dtype, a, STATE_ONLY, st);
 }
 
 }  // namespace
@@ -332,7 +313,8 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
   a.q = q, a.k = k, a.v = v, a.g = log_decay, a.out = out;
   a.qs = q_stride, a.ks = k_stride, a.vs = v_stride, a.gs = decay_stride, a.os = out_stride;
   a.state_in = state_in, a.state_out = state_out;
-  a.H = n_heads, a.K = key_dim, a.V = value_dim, a.slices = (value_dim + COLS - 1) / COLS;
+  const int cols = dtype == TRACKFIT_FP32 ? COLS : linear_mma_cols(key_dim, value_dim);
+  a.H = n_heads, a.K = key_dim, a.V = value_dim, a.slices = (value_dim + cols - 1) / cols;
   a.scale = scale;
   a.u.offs = offsets, a.u.n_seq = n_seq, a.u.n_rows = n_rows, a.u.reverse = reverse;
   a.u.lseg = rows_a_boundary(n_rows, n_heads, value_dim);

@@ -53,9 +53,10 @@ class Offsets {
 // The pieces of a tile's unit, one after the other (all lanes alike).
 class TilePieces {
  public:
-  __device__ __forceinline__ TilePieces(const Units& u, int64_t tile, int lane)
+  // (idle: no piece will be asked for)
+  __device__ __forceinline__ TilePieces(const Units& u, int64_t tile, int lane, bool idle)
       : u_(u), offs_(u, lane), r0_(tile * u.seg), r1_(tile * u.seg + u.seg), last_(tile + 1 == u.tiles) {
-    b_ = r0_ == 0 ? 0 : first_at_least(u.offs, u.n_seq, r0_, lane);
+    b_ = r0_ == 0 || idle ? 0 : first_at_least(u.offs, u.n_seq, r0_, lane);
     across_ = r0_ != 0 && r0_ % u.lseg == 0 && b_ > 0;
   }
   __device__ __forceinline__ bool next(Piece& p) {
@@ -115,5 +116,27 @@ __device__ __forceinline__ bool boundary_piece(const Units& u, int64_t i, int la
   }
   return true;
 }
+
+constexpr int NW = 4;            // warps of a CTA, each with a unit of its own
+
+struct LaArgs {
+  Units u;
+  const void *q, *k, *v;
+  const float* g;
+  void* out;
+  int64_t qs, ks, vs, gs, os;    // row strides in elements
+  const float* state_in;
+  float* state_out;
+  float* ws_state;               // [boundaries][H][K][V]
+  float* ws_decay;               // [boundaries][H], sums of g
+  int32_t* ws_flag;              // [boundaries]: 0 no cut sequence, 1 its first piece, 2 a later one
+  int64_t bounds;                // boundaries 1 .. bounds - 1
+  int H, K, V, slices;
+  float scale;
+};
+
+// linear_mma.cu: the 16-bit types on the tensor cores.  Channels of v that a warp takes:
+inline int linear_mma_cols(int K, int V) { return V > 16 && K <= 64 ? 32 : 16; }
+int linear_mma(int32_t dtype, const LaArgs& a, bool state_only, cudaStream_t st);
 
 }  // namespace seqops
