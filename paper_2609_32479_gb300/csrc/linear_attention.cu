@@ -11,35 +11,27 @@
 namespace {
 using namespace seqops;
 
-// A chunk of a piece: up to CH rows, in the direction of the recurrence.
-struct Chunk {
-  int64_t row;                   // its first row
-  int64_t seq;
-  int len;                       // rows; 0 only for a sequence without rows
-  bool first, last;              // of its piece
-  int64_t from;
-  bool ends;
-};
-
-// ---------------------------------------------------------------- CUDA cores
+// ---------------------------------------------------------------- fp32, on the CUDA cores
 // A lane holds a column of S: K values in registers.  The rows of q and k are the same for
-// all lanes and come from shared memory as broadcasts.
+// all lanes and come from shared memory as broadcasts, 8 rows at a time through a ring that
+// the warp fills by asynchronous copies.
 constexpr int COLS = 32;         // channels of v that a warp takes
 constexpr int CH = 8, NST = 3;
 
-template <class T, int DK>
-struct SimtSlot {
-  T q[CH][DK], k[CH][DK], v[CH][COLS];
+template <int DK>
+struct __align__(16) SimtSlot {
+  float q[CH][DK], k[CH][DK], v[CH][COLS];
   float g[CH];
+  int row, seq, flags, pad;      // the chunk, its first row in the direction of the recurrence
 };
+enum { LEN = 0xff, FIRST = 0x100, LAST = 0x200, GOES_ON = 0x400, ENDS = 0x800, NONE = 0x1000 };
 
-template <class T, int DK, bool STATE_ONLY>
+template <int DK, bool STATE_ONLY>
 __global__ void __launch_bounds__(NW * 32) la_simt_kernel(const __grid_constant__ LaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  using Slot = SimtSlot<T, DK>;
-  constexpr int VE = 16 / sizeof(T);
+  using Slot = SimtSlot<DK>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t unit = (int64_t)blockIdx.x * NW + warp;
+  const unsigned unit = blockIdx.x * NW + warp;
   const int sl = (int)(unit % a.slices), h = (int)(unit / a.slices % a.H);
   const int64_t tile = unit / a.slices / a.H;
   if (tile >= (STATE_ONLY ? a.bounds - 1 : a.u.tiles)) return;
@@ -50,125 +42,145 @@ __global__ void __launch_bounds__(NW * 32) la_simt_kernel(const __grid_constant_
   for (uint32_t* p = reinterpret_cast<uint32_t*>(slots) + lane; p < reinterpret_cast<uint32_t*>(slots + NST); p += 32) *p = 0;
   __syncwarp();
 
-  const T* q = (const T*)a.q + h * a.K;
-  const T* k = (const T*)a.k + h * a.K;
-  const T* v = (const T*)a.v + h * a.V + c0;
+  const int64_t base = STATE_ONLY ? (tile + 1) * a.u.lseg : tile * a.u.seg;
+  const float* q = (const float*)a.q + base * a.qs + h * a.K;
+  const float* k = (const float*)a.k + base * a.ks + h * a.K;
+  const float* v = (const float*)a.v + base * a.vs + h * a.V + c0;
+  const float* gr = a.g + base * a.gs + h;
+  float* out = (float*)a.out + base * a.os + h * a.V + c0 + lane;
   TilePieces pieces(a.u, tile, lane, STATE_ONLY);
   Piece p;
   bool more;
-  int64_t bound = 0;
   if (STATE_ONLY) {
-    bound = tile + 1;
-    more = boundary_piece(a.u, bound, lane, p);
-    if (sl == 0 && h == 0 && lane == 0) a.ws_flag[bound] = !more ? 0 : p.from < 0 ? 1 : 2;
+    more = boundary_piece(a.u, tile + 1, lane, p);
+    if (sl == 0 && h == 0 && lane == 0) a.ws_flag[tile + 1] = !more ? 0 : p.goes_on ? 2 : 1;
   } else {
     more = pieces.next(p);
   }
-  int64_t done = 0;
-  Chunk ring[NST];
+  int done = 0;
 
-  auto issue = [&](int s) {
-    Chunk& c = ring[s];
-    c.len = -1;
+  auto issue = [&](Slot& w) {
     if (more) {
-      const int64_t left = p.hi - p.lo - done;
-      c.len = (int)(left < CH ? left : CH);
-      c.row = a.u.reverse ? p.hi - 1 - done : p.lo + done;
-      c.first = done == 0, c.last = left <= CH;
-      c.seq = p.seq, c.from = p.from, c.ends = p.ends;
-      Slot& w = slots[s];
-      const int kv = a.K / VE, vv = width / VE;
-      for (int i = lane; i < CH * kv; i += 32) {
-        const int r = i / kv, e = (i - r * kv) * VE;
-        const bool on = r < c.len;
-        const int64_t row = on ? c.row + dir * r : 0;
-        if (!STATE_ONLY) copy16(smem_addr(&w.q[r][e]), q + row * a.qs + e, on);
-        copy16(smem_addr(&w.k[r][e]), k + row * a.ks + e, on);
+      const int left = p.hi - p.lo - done;
+      const int len = left < CH ? left : CH;
+      const int row = a.u.reverse ? p.hi - 1 - done : p.lo + done;
+      if (lane == 0) {
+        w.row = row, w.seq = p.seq;
+        w.flags = len | (done == 0 ? FIRST : 0) | (left <= CH ? LAST : 0) | (p.goes_on ? GOES_ON : 0) | (p.ends ? ENDS : 0);
       }
-      for (int i = lane; i < CH * vv; i += 32) {
-        const int r = i / vv, e = (i - r * vv) * VE;
-        const bool on = r < c.len;
-        copy16(smem_addr(&w.v[r][e]), v + (on ? c.row + dir * r : 0) * a.vs + e, on);
+#pragma unroll
+      for (int i = 0; i < CH * DK / 128; ++i) {
+        const int r = (lane + 32 * i) / (DK / 4), e = (lane + 32 * i) % (DK / 4) * 4;
+        if (e < a.K) {
+          const int64_t at = row + dir * r;
+          if (!STATE_ONLY) copy16(smem_addr(&w.q[r][e]), q + at * a.qs + e, r < len);
+          copy16(smem_addr(&w.k[r][e]), k + at * a.ks + e, r < len);
+        }
       }
-      if (lane < CH) copy4(smem_addr(&w.g[lane]), a.g + (lane < c.len ? c.row + dir * lane : 0) * a.gs + h, lane < c.len);
-      done += c.len;
-      if (c.last) {
+#pragma unroll
+      for (int i = 0; i < CH * COLS / 128; ++i) {
+        const int r = (lane + 32 * i) / (COLS / 4), e = (lane + 32 * i) % (COLS / 4) * 4;
+        if (e < width) copy16(smem_addr(&w.v[r][e]), v + (int64_t)(row + dir * r) * a.vs + e, r < len);
+      }
+      if (lane < CH) copy4(smem_addr(&w.g[lane]), gr + (int64_t)(row + dir * lane) * a.gs, lane < len);
+      done += len;
+      if (left <= CH) {
         done = 0;
         more = STATE_ONLY ? false : pieces.next(p);
       }
+    } else if (lane == 0) {
+      w.flags = NONE;
     }
     copy_commit();
   };
 
-#pragma unroll
-  for (int s = 0; s < NST; ++s) issue(s);
+  for (int s = 0; s < NST; ++s) issue(slots[s]);
   float S[DK];
 #pragma unroll
   for (int i = 0; i < DK; ++i) S[i] = 0.0f;
   float total = 0.0f;
   const int64_t KV = (int64_t)a.K * a.V;
-  for (;;) {
+  for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
+    Slot& w = slots[s];
+    copy_wait<NST - 1>();
+    __syncwarp();
+    const int flags = w.flags, row = w.row, seq = w.seq, len = flags & LEN;
+    if (flags & NONE) break;
+    if (flags & FIRST) {
+      const float* st = nullptr;
+      if (flags & GOES_ON)
+        st = STATE_ONLY ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
+      else if (a.state_in)
+        st = a.state_in + ((int64_t)seq * a.H + h) * KV;
+      st = st && lane < width ? st + c0 + lane : nullptr;
 #pragma unroll
-    for (int s = 0; s < NST; ++s) {
-      const Chunk c = ring[s];
-      if (c.len < 0) return;
-      copy_wait<NST - 1>();
-      __syncwarp();
-      if (c.first) {
-        const float* st = nullptr;
-        if (c.from < 0) st = a.state_in ? a.state_in + (c.seq * a.H + h) * KV : nullptr;
-        else if (!STATE_ONLY) st = a.ws_state + (c.from * a.H + h) * KV;
-        st = st && lane < width ? st + c0 + lane : nullptr;
-#pragma unroll
-        for (int i = 0; i < DK; ++i) S[i] = st && i < a.K ? st[(int64_t)i * a.V] : 0.0f;
-      }
-      const Slot& w = slots[s];
-      for (int r = 0; r < c.len; ++r) {
-        const float e = expf(w.g[r]);
-        const float vr = to_float(w.v[r][lane]);
-        if (STATE_ONLY) total += w.g[r];
-        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < DK; i += 4) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            S[i + j] = fmaf(to_float(w.k[r][i + j]), vr, e * S[i + j]);
-            if (!STATE_ONLY) acc[j] = fmaf(to_float(w.q[r][i + j]), S[i + j], acc[j]);
-          }
-        }
-        if (!STATE_ONLY && lane < width)
-          put((T*)a.out + (c.row + dir * r) * a.os + h * a.V + c0 + lane, a.scale * ((acc[0] + acc[1]) + (acc[2] + acc[3])));
-      }
-      if (c.last && (STATE_ONLY || (c.ends && a.state_out))) {
-        float* st = STATE_ONLY ? a.ws_state + (bound * a.H + h) * KV : a.state_out + (c.seq * a.H + h) * KV;
-        if (lane < width)
-#pragma unroll
-          for (int i = 0; i < DK; ++i)
-            if (i < a.K) st[(int64_t)i * a.V + c0 + lane] = S[i];
-        if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[bound * a.H + h] = total;
-      }
-      __syncwarp();
-      issue(s);
+      for (int i = 0; i < DK; ++i) S[i] = st && i < a.K ? st[(int64_t)i * a.V] : 0.0f;
     }
+    for (int r = 0; r < len; ++r) {
+      const float e = expf(w.g[r]);
+      const float vr = w.v[r][lane];
+      if (STATE_ONLY) total += w.g[r];
+      float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < DK; i += 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          S[i + j] = fmaf(w.k[r][i + j], vr, e * S[i + j]);
+          if (!STATE_ONLY) acc[j] = fmaf(w.q[r][i + j], S[i + j], acc[j]);
+        }
+      }
+      if (!STATE_ONLY && lane < width)
+        out[(int64_t)(row + dir * r) * a.os] = a.scale * ((acc[0] + acc[1]) + (acc[2] + acc[3]));
+    }
+    if ((flags & LAST) && (STATE_ONLY || ((flags & ENDS) && a.state_out))) {
+      float* st = STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV;
+      if (lane < width)
+#pragma unroll
+        for (int i = 0; i < DK; ++i)
+          if (i < a.K) st[(int64_t)i * a.V + c0 + lane] = S[i];
+      if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
+    }
+    __syncwarp();
+    issue(w);
   }
 }
 
 // What crosses each boundary: the pieces' own states, in the direction of the recurrence,
 // each with the decayed state of the boundary before it.  A thread takes one value of a
-// head's state through all boundaries.
-__global__ void __launch_bounds__(128) la_carry_kernel(const __grid_constant__ LaArgs a) {
+// head's state through all boundaries; the CTA looks at 128 boundaries' flags at a time and
+// passes over those that no cut sequence crosses.
+constexpr int CARRY_NT = 128;
+__global__ void __launch_bounds__(CARRY_NT) la_carry_kernel(const __grid_constant__ LaArgs a) {
+  __shared__ int flag[CARRY_NT];
   const int64_t KV = (int64_t)a.K * a.V;
-  const int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (e >= KV * a.H) return;
-  const int h = (int)(e / KV);
+  const int64_t e = (int64_t)blockIdx.x * CARRY_NT + threadIdx.x;
+  const bool on = e < KV * a.H;
+  const int h = on ? (int)(e / KV) : 0;
   float carry = 0.0f;
-  for (int64_t j = 1; j < a.bounds; ++j) {
-    const int64_t i = a.u.reverse ? a.bounds - j : j;
-    const int f = a.ws_flag[i];
-    if (f == 0) continue;
-    float* p = a.ws_state + i * a.H * KV + e;
-    carry = f == 2 ? fmaf(expf(a.ws_decay[i * a.H + h]), carry, *p) : *p;
-    *p = carry;
+  constexpr int AHEAD = 16;      // boundaries whose loads are under way together
+  for (int64_t j0 = 1; j0 < a.bounds; j0 += CARRY_NT) {
+    const int64_t jt = j0 + threadIdx.x;
+    const int mine = jt < a.bounds ? a.ws_flag[a.u.reverse ? a.bounds - jt : jt] : 0;
+    const int any = __syncthreads_or(mine != 0);   // (also: the flags before are done with)
+    if (!any) continue;                            // the next chain begins with a flag of 1
+    flag[threadIdx.x] = mine;
+    __syncthreads();
+    for (int n0 = 0; n0 < CARRY_NT && on; n0 += AHEAD) {
+      float x[AHEAD], d[AHEAD];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) {
+        const int64_t j = j0 + n0 + n, i = a.u.reverse ? a.bounds - j : j;
+        x[n] = d[n] = 0.0f;
+        if (flag[n0 + n] != 0) x[n] = a.ws_state[i * a.H * KV + e], d[n] = a.ws_decay[i * a.H + h];
+      }
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) {
+        if (flag[n0 + n] == 0) continue;           // nothing was written there
+        const int64_t j = j0 + n0 + n, i = a.u.reverse ? a.bounds - j : j;
+        carry = flag[n0 + n] == 2 ? fmaf(expf(d[n]), carry, x[n]) : x[n];
+        a.ws_state[i * a.H * KV + e] = carry;
+      }
+    }
   }
 }
 
@@ -252,28 +264,22 @@ size_t workspace_bytes(int64_t n_rows, int H, int K, int V) {
   return flags + decay + bounds * H * (size_t)K * V * 4;
 }
 
-template <class T, int DK, bool STATE_ONLY>
+template <int DK, bool STATE_ONLY>
 int launch_simt(const LaArgs& a, cudaStream_t st) {
-  const size_t sm = sizeof(SimtSlot<T, DK>) * NST * NW;
-  auto kern = la_simt_kernel<T, DK, STATE_ONLY>;
+  const size_t sm = sizeof(SimtSlot<DK>) * NST * NW;
+  auto kern = la_simt_kernel<DK, STATE_ONLY>;
   const cudaError_t e = tf_allow_smem(kern);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  const int64_t units = (STATE_ONLY ? a.bounds - 1 : a.u.tiles) * a.H * a.slices;
-  if ((units + NW - 1) / NW > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
-  kern<<<(unsigned)((units + NW - 1) / NW), NW * 32, sm, st>>>(a);
+  kern<<<linear_grid(a, STATE_ONLY), NW * 32, sm, st>>>(a);
   return launched();
 }
-template <class T, bool STATE_ONLY>
-int by_width(const LaArgs& a, cudaStream_t st) {
-  if (a.K <= 16) return launch_simt<T, 16, STATE_ONLY>(a, st);
-  if (a.K <= 32) return launch_simt<T, 32, STATE_ONLY>(a, st);
-  if (a.K <= 64) return launch_simt<T, 64, STATE_ONLY>(a, st);
-  return launch_simt<T, 128, STATE_ONLY>(a, st);
-}
 template <bool STATE_ONLY>
-int by_type(int32_t dtype, const LaArgs& a, cudaStream_t st) {
-  if (dtype == TRACKFIT_FP32) return by_width<float, STATE_ONLY>(a, st);
-  return linear_mma(dtype, a, STATE_ONLY, st);
+int run(int32_t dtype, const LaArgs& a, cudaStream_t st) {
+  if (dtype != TRACKFIT_FP32) return linear_mma(dtype, a, STATE_ONLY, st);
+  if (a.K <= 16) return launch_simt<16, STATE_ONLY>(a, st);
+  if (a.K <= 32) return launch_simt<32, STATE_ONLY>(a, st);
+  if (a.K <= 64) return launch_simt<64, STATE_ONLY>(a, st);
+  return launch_simt<128, STATE_ONLY>(a, st);
 }
 
 }  // namespace
@@ -304,7 +310,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
         !rows_ok(v, v_stride, (int64_t)n_heads * value_dim, sz) ||
         !rows_ok(out, out_stride, (int64_t)n_heads * value_dim, sz))
       return TRACKFIT_ERR_INVALID_ARG;
-    if (!log_decay || mis4(log_decay) || decay_stride < n_heads || decay_stride > (int64_t)1 << 40)
+    if (!log_decay || mis4(log_decay) || decay_stride < n_heads || decay_stride > MAX_STRIDE)
       return TRACKFIT_ERR_INVALID_ARG;
   }
   const size_t need = workspace_bytes(n_rows, n_heads, key_dim, value_dim);
@@ -313,7 +319,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
   a.q = q, a.k = k, a.v = v, a.g = log_decay, a.out = out;
   a.qs = q_stride, a.ks = k_stride, a.vs = v_stride, a.gs = decay_stride, a.os = out_stride;
   a.state_in = state_in, a.state_out = state_out;
-  const int cols = dtype == TRACKFIT_FP32 ? COLS : linear_mma_cols(key_dim, value_dim);
+  const int cols = dtype == TRACKFIT_FP32 ? COLS : linear_mma_cols(key_dim);
   a.H = n_heads, a.K = key_dim, a.V = value_dim, a.slices = (value_dim + cols - 1) / cols;
   a.scale = scale;
   a.u.offs = offsets, a.u.n_seq = n_seq, a.u.n_rows = n_rows, a.u.reverse = reverse;
@@ -324,6 +330,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
   while (a.u.seg > 16 && n_rows / a.u.seg * n_heads * a.slices < 2400) a.u.seg /= 2;
   a.u.tiles = n_rows > 0 ? (n_rows + a.u.seg - 1) / a.u.seg : 1;
   a.bounds = 1;
+  if (a.u.tiles > (int64_t)0x7fffffff / (n_heads * a.slices)) return TRACKFIT_ERR_UNSUPPORTED;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (need > 0) {
     a.bounds = (n_rows + a.u.lseg - 1) / a.u.lseg;
@@ -334,17 +341,17 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
     w += (a.bounds * n_heads * 4 + 15) / 16 * 16;
     a.ws_state = reinterpret_cast<float*>(w);
     if (a.bounds > 1) {
-      int rc = by_type<true>(dtype, a, st);
+      int rc = run<true>(dtype, a, st);
       if (rc != TRACKFIT_OK) return rc;
       const int64_t n = (int64_t)n_heads * key_dim * value_dim;
-      la_carry_kernel<<<(unsigned)((n + 127) / 128), 128, 0, st>>>(a);
+      la_carry_kernel<<<(unsigned)((n + CARRY_NT - 1) / CARRY_NT), CARRY_NT, 0, st>>>(a);
       rc = launched();
       if (rc != TRACKFIT_OK) return rc;
     }
   } else {
     a.ws_flag = nullptr, a.ws_decay = a.ws_state = nullptr;
   }
-  return by_type<false>(dtype, a, st);
+  return run<false>(dtype, a, st);
 }
 
 extern "C" int trackfit_linear_attention_step(int32_t dtype, const void* q, int64_t q_stride, const void* k,
@@ -363,7 +370,7 @@ extern "C" int trackfit_linear_attention_step(int32_t dtype, const void* q, int6
       !rows_ok(v, v_stride, (int64_t)n_heads * value_dim, sz) ||
       !rows_ok(out, out_stride, (int64_t)n_heads * value_dim, sz))
     return TRACKFIT_ERR_INVALID_ARG;
-  if (!log_decay || mis4(log_decay) || decay_stride < n_heads || decay_stride > (int64_t)1 << 40)
+  if (!log_decay || mis4(log_decay) || decay_stride < n_heads || decay_stride > MAX_STRIDE)
     return TRACKFIT_ERR_INVALID_ARG;
   if (mis4(slots) || !state_in || !state_out || mis16(state_in) || mis16(state_out)) return TRACKFIT_ERR_INVALID_ARG;
   StepArgs a;

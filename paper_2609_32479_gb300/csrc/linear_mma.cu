@@ -1,6 +1,6 @@
 // Linear attention of the 16-bit types on the tensor cores.
 //
-// A warp takes a unit (linear_units.cuh) of one head and 16 or 32 channels of v, with the
+// A warp takes a unit (linear_units.cuh) of one head and 32 or 16 channels of v, with the
 // state's columns of these channels in registers, and goes through its sequences in chunks of
 // up to 16 rows.  With G_i the sum of g over a chunk's rows up to i and S the state before it:
 //   O   = diag(exp G) Q S + (Q K^T o L) V,    L_ij = exp(G_i - G_j) for j <= i, else 0
@@ -15,9 +15,17 @@
 // 4 (K + V) bytes and its products at K = V = 64 take 17 of the 22 clocks that an SM's share
 // of the memory bandwidth gives it.
 //
-// Every warp runs by itself, with a ring of chunks in shared memory that it fills by
-// asynchronous copies; rows beyond a chunk's are zeros, so that nothing of another sequence
-// enters a product.
+// Operands without a layout in shared memory: lane (g, t) = (l / 4, l % 4) reads 16 bytes,
+// channels 8t .. 8t+7 of each 32, of rows g and g + 8.  A product's k index may be permuted,
+// so these are the operands of Q K^T as they stand (slots 2t, 2t+1 of step i are channels
+// 8t + 4i, + 1, slots 2t+8, 2t+9 the two after); movmatrix turns the words of V (and of K,
+// for the state) to pairs of rows, and the products' columns come out with channels
+// 8t .. 8t+7 in lane t again: 16 bytes to write.  Shared memory is a queue of each lane's own
+// words, filled by asynchronous copies three chunks ahead.  Instructions bound the short
+// chunks: staged through rows in shared memory with ldmatrix and 64-bit row addresses,
+// 131,072 tracks took 700 us.
+//
+// Rows beyond a chunk's are zeros, so that nothing of another sequence enters a product.
 //
 // Roundings: the products' operands are 16 bits.  Q K^T o L is split into two bf16 parts, the
 // decayed V into two, or three where the state is asked for (bf16: 8, 16, 24 bits), so that
@@ -30,18 +38,47 @@
 namespace {
 using namespace seqops;
 
-constexpr int NST = 3;           // chunks in the ring
+constexpr int NST = 3;           // chunks in the queue
 constexpr int C = 16;            // rows of a chunk
 
-template <int DK, int NV>
-struct __align__(16) Slot {
-  static constexpr int PK = DK * 2 + 16, PV = NV * 16 + 16;   // bytes of a row: 16 more, for the banks
-  unsigned char q[C * PK], k[C * PK], v[C * PV];
-  float g[C];
-  int64_t row;                   // the chunk: its first row in the direction of the recurrence
-  int32_t seq, flags;
+struct Chunk {
+  int row, seq, flags;           // its first row in the direction of the recurrence, from the unit's base
 };
-enum { LEN = 0xff, FIRST = 0x100, LAST = 0x200, GOES_ON = 0x400, ENDS = 0x800, NONE = 0x1000 };
+enum { LEN = 0x1f, FIRST = 0x100, LAST = 0x200, GOES_ON = 0x400, ENDS = 0x800, NONE = 0x1000 };
+
+// Bytes of a chunk's place in the queue: q and k, 4 x 16 bytes a lane and group of 32 channels,
+// V, 2 x NV words a lane, and g, a word a lane.
+__host__ __device__ constexpr int slot_bytes(int groups, int nv) { return 32 * (groups * 4 * 16 + 2 * nv * 4 + 4); }
+
+// Words of a lane's 16 (NV = 4) or 8 (NV = 2) bytes of V.
+template <int NV>
+struct Vec {
+  uint32_t w[NV];
+};
+__device__ __forceinline__ void load_shared(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void load_shared(uint32_t (&r)[2], uint32_t addr) {
+  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
+}
+template <int BYTES>
+__device__ __forceinline__ void copy_v(uint32_t dst, const void* src, bool there) {
+  if constexpr (BYTES == 16) copy16(dst, src, there);
+  else copy8(dst, src, there);
+}
+
+// An 8 x 8 tile of 16-bit values with rows and columns exchanged.
+__device__ __forceinline__ uint32_t turned(uint32_t u) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(u));
+  return d;
+}
+__device__ __forceinline__ void write_out(void* p, const uint32_t (&w)[4]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void write_out(void* p, const uint32_t (&w)[2]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+}
 
 __device__ __forceinline__ uint32_t zero_if_finite(uint32_t u, uint32_t sum, __nv_bfloat16) {
   asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(u), "r"(0u));
@@ -78,146 +115,207 @@ __device__ __forceinline__ void add_rows(T, Mul mul, float (&o)[NV][4], const ui
   }
 }
 
-template <class T, int DK, int NV, bool STATE_ONLY, bool EXACT>
-__global__ void __launch_bounds__(NW * 32) la_mma_kernel(const __grid_constant__ LaArgs a) {
+template <class T, int NG, int NV, bool STATE_ONLY, bool EXACT>
+__global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const __grid_constant__ LaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  using S = Slot<DK, NV>;
-  constexpr bool BF = sizeof(T) == 2 && !__is_same(T, __half);
-  constexpr int MT = NV / 2, KT = DK / 8;             // tiles of the state: MT x 16 by KT x 8
+  constexpr bool BF = !__is_same(T, __half);
+  constexpr int MT = NV / 2, KT = NG * 4;             // tiles of the state: MT x 16 by KT x 8
+  constexpr int VC = NV * 2;                           // channels of V a lane
+  constexpr int SLOT = slot_bytes(NG, NV);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t unit = (int64_t)blockIdx.x * NW + warp;
+  const unsigned unit = blockIdx.x * NW + warp;
   const int sl = (int)(unit % a.slices), h = (int)(unit / a.slices % a.H);
   const int64_t tile = unit / a.slices / a.H;
   if (tile >= (STATE_ONLY ? a.bounds - 1 : a.u.tiles)) return;
-  S* slots = reinterpret_cast<S*>(smem) + warp * NST;
   const int c0 = sl * NV * 8, width = a.V - c0 < NV * 8 ? a.V - c0 : NV * 8;
   const int dir = a.u.reverse ? -1 : 1;
   const int g = lane >> 2, t = lane & 3;
+  const int64_t base = STATE_ONLY ? (tile + 1) * a.u.lseg : tile * a.u.seg;
+  // this lane's place in the queue: 16 bytes of each of q [group][row half], k likewise, its V
+  // [row half], g
+  const uint32_t mine = smem_addr(smem) + warp * NST * SLOT + lane * 16;
+  const uint32_t mine_v = smem_addr(smem) + warp * NST * SLOT + NG * 4 * 512 + lane * VC * 2;
+  const uint32_t mine_g = smem_addr(smem) + warp * NST * SLOT + NG * 4 * 512 + 2 * 32 * VC * 2 + lane * 4;
   // channels beyond K and V are zeros from here on: the copies leave them alone
-  if (a.K < DK || width < NV * 8) {
-    for (uint32_t* p = reinterpret_cast<uint32_t*>(slots) + lane; p < reinterpret_cast<uint32_t*>(slots + NST); p += 32) *p = 0;
-    __syncwarp();
+  for (int s = 0; s < NST; ++s) {
+#pragma unroll
+    for (int i = 0; i < NG * 4; ++i)
+      asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(mine + s * SLOT + i * 512), "r"(0) : "memory");
+#pragma unroll
+    for (int i = 0; i < VC; ++i)
+      asm volatile("st.shared.b32 [%0], %1;" ::"r"(mine_v + s * SLOT + i / NV * 32 * VC * 2 + i % NV * 4), "r"(0) : "memory");
   }
-  const T* q = (const T*)a.q + h * a.K;
-  const T* k = (const T*)a.k + h * a.K;
-  const T* v = (const T*)a.v + h * a.V + c0;
   TilePieces pieces(a.u, tile, lane, STATE_ONLY);
   Piece p;
   bool more;
   if (STATE_ONLY) {
     more = boundary_piece(a.u, tile + 1, lane, p);
-    if (sl == 0 && h == 0 && lane == 0) a.ws_flag[tile + 1] = !more ? 0 : p.from < 0 ? 1 : 2;
+    if (sl == 0 && h == 0 && lane == 0) a.ws_flag[tile + 1] = !more ? 0 : p.goes_on ? 2 : 1;
   } else {
     more = pieces.next(p);
   }
-  int64_t done = 0;
+  int done = 0;
+  // bytes from a row to the next in the direction of the recurrence, and this lane's bytes of
+  // the base row: a row's address is one 32 x 32 + 64 bit multiply-add
+  const int qb = dir * (int)a.qs * 2, kb = dir * (int)a.ks * 2, vs = dir * (int)a.vs * 2, gs = dir * (int)a.gs * 4;
+  const int ob = dir * (int)a.os * 2;
+  const char* q0 = reinterpret_cast<const char*>((const T*)a.q + base * a.qs + h * a.K + 8 * t);
+  const char* k0 = reinterpret_cast<const char*>((const T*)a.k + base * a.ks + h * a.K + 8 * t);
+  const char* v0 = reinterpret_cast<const char*>((const T*)a.v + base * a.vs + h * a.V + c0 + VC * t);
+  const char* g0 = reinterpret_cast<const char*>(a.g + base * a.gs + h);
+  char* o0 = reinterpret_cast<char*>((T*)a.out + base * a.os + h * a.V + c0 + VC * t);
+  const bool v_on = VC * t < width;
 
-  auto issue = [&](S& w) {
+  auto issue = [&](int s) {
+    Chunk c;
+    c.flags = NONE;
     if (more) {
-      const int64_t left = p.hi - p.lo - done;
-      const int len = (int)(left < C ? left : C);
-      const int64_t row = a.u.reverse ? p.hi - 1 - done : p.lo + done;
-      if (lane == 0) {
-        w.row = row, w.seq = (int32_t)p.seq;
-        w.flags = len | (done == 0 ? FIRST : 0) | (left <= C ? LAST : 0) | (p.from >= 0 ? GOES_ON : 0) | (p.ends ? ENDS : 0);
-      }
-      constexpr int VK = DK / 8;                       // 16-byte pieces of a row
+      const int left = p.hi - p.lo - done;
+      const int len = left < C ? left : C;
+      c.row = a.u.reverse ? p.hi - 1 - done : p.lo + done;
+      c.seq = p.seq;
+      c.flags = len | (done == 0 ? FIRST : 0) | (left <= C ? LAST : 0) | (p.goes_on ? GOES_ON : 0) | (p.ends ? ENDS : 0);
+      const int r0 = dir * c.row + g, r1 = r0 + 8;     // rows along the direction
+      const bool on0 = g < len, on1 = g + 8 < len;
+      const uint32_t m = mine + s * SLOT;
+      const char* kk0 = k0 + (int64_t)r0 * kb;
+      const char* kk1 = k0 + (int64_t)r1 * kb;
+      const char* qq0 = q0 + (int64_t)r0 * qb;
+      const char* qq1 = q0 + (int64_t)r1 * qb;
 #pragma unroll
-      for (int i = 0; i < C * VK / 32; ++i) {
-        const int r = (lane + 32 * i) / VK, e = (lane + 32 * i) % VK * 8;
-        if (e < a.K) {
-          const bool on = r < len;
-          const int64_t at = on ? row + dir * r : 0;
-          if (!STATE_ONLY) copy16(smem_addr(w.q + r * S::PK + e * 2), q + at * a.qs + e, on);
-          copy16(smem_addr(w.k + r * S::PK + e * 2), k + at * a.ks + e, on);
+      for (int i = 0; i < NG; ++i)
+        if (32 * i + 8 * t < a.K) {
+          if (!STATE_ONLY) {
+            copy16(m + (2 * i) * 512, qq0 + 64 * i, on0);
+            copy16(m + (2 * i + 1) * 512, qq1 + 64 * i, on1);
+          }
+          copy16(m + (2 * NG + 2 * i) * 512, kk0 + 64 * i, on0);
+          copy16(m + (2 * NG + 2 * i + 1) * 512, kk1 + 64 * i, on1);
         }
+      if (v_on) {
+        copy_v<VC * 2>(mine_v + s * SLOT, v0 + (int64_t)r0 * vs, on0);
+        copy_v<VC * 2>(mine_v + s * SLOT + 32 * VC * 2, v0 + (int64_t)r1 * vs, on1);
       }
-#pragma unroll
-      for (int i = 0; i < C * NV / 32; ++i) {
-        const int r = (lane + 32 * i) / NV, e = (lane + 32 * i) % NV * 8;
-        if (e < width) {
-          const bool on = r < len;
-          copy16(smem_addr(w.v + r * S::PV + e * 2), v + (on ? row + dir * r : 0) * a.vs + e, on);
-        }
-      }
-      if (lane < C) copy4(smem_addr(&w.g[lane]), a.g + (lane < len ? row + dir * lane : 0) * a.gs + h, lane < len);
+      const int lr = lane & 15;
+      copy4(mine_g + s * SLOT, g0 + (int64_t)(dir * c.row + lr) * gs, lr < len);
       done += len;
       if (left <= C) {
         done = 0;
         more = STATE_ONLY ? false : pieces.next(p);
       }
-    } else if (lane == 0) {
-      w.flags = NONE;
     }
     copy_commit();
+    return c;
   };
 
-  for (int s = 0; s < NST; ++s) issue(slots[s]);
   float st[MT][KT][4];
-  bool zero = true;                                    // the state before the chunk is zero
+  bool zero = true;                                    // the state before the chunk is zero, and st not set
   float total = 0.0f;
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
+  const int64_t KV = (int64_t)a.K * a.V;
+  // st[m][j][i] is key channel 32 (j/4) + 8t + 2 (j%4) + (i&1), value channel
+  // VC (g/2) + 2 (2m + i/2) + (g&1) of the slice.  Lanes g and g^1 trade halves, so that each
+  // has NV channels side by side
+  const bool odd = g & 1;
+  const int64_t mine_st = (int64_t)(8 * t) * a.V + c0 + VC * (g >> 1) + (odd ? NV : 0);
+  const bool st_on = VC * (g >> 1) < width;
+  auto load_state = [&](const float* src) {
 #pragma unroll
     for (int j = 0; j < KT; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) st[m][j][i] = 0.0f;
-  const int64_t KV = (int64_t)a.K * a.V;
-  // of this lane in operands of 8 x 8 matrices: rows by lane, columns by the matrix
-  const int q_row = lane & 15, q_col = (lane >> 4) * 8;
-  const int n_row = (lane >> 4) * 8 + (lane & 7), n_col = (lane >> 3 & 1) * 8;
-  const int k_row = (lane >> 3 & 1) * 8 + (lane & 7), k_col = (lane >> 4) * 8;
-  int s = 0;
-  for (;;) {
-    S& w = slots[s];
-    copy_wait<NST - 1>();
-    __syncwarp();
-    const int flags = w.flags;
+      for (int i = 0; i < 2; ++i) {
+        float x[NV];
+#pragma unroll
+        for (int n = 0; n < NV; ++n) x[n] = 0.0f;
+        if (st_on && 32 * (j / 4) + 8 * t < a.K) {
+          const float* s = src + mine_st + (32 * (j / 4) + 2 * (j % 4) + i) * a.V;
+          if constexpr (NV == 4) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(s);
+          else *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(s);
+        }
+        // an even lane has the channels of the lower tiles, its own and its neighbour's by turns
+#pragma unroll
+        for (int n = 0; n < NV / 2; ++n) {
+          const float y = __shfl_xor_sync(FULL, odd ? x[2 * n] : x[2 * n + 1], 4);
+          const float own = odd ? x[2 * n + 1] : x[2 * n];
+          const int lo = n, hi = n + NV / 2;           // tiles
+          st[lo / 2][j][(lo & 1) * 2 + i] = odd ? y : own;
+          st[hi / 2][j][(hi & 1) * 2 + i] = odd ? own : y;
+        }
+      }
+  };
+  auto store_state = [&](float* dst) {
+#pragma unroll
+    for (int j = 0; j < KT; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float x[NV];
+#pragma unroll
+        for (int n = 0; n < NV / 2; ++n) {
+          const int lo = n, hi = n + NV / 2;
+          const float u = st[lo / 2][j][(lo & 1) * 2 + i], v = st[hi / 2][j][(hi & 1) * 2 + i];
+          const float y = __shfl_xor_sync(FULL, odd ? u : v, 4);
+          x[2 * n] = odd ? y : u;
+          x[2 * n + 1] = odd ? v : y;
+        }
+        if (st_on && 32 * (j / 4) + 8 * t < a.K) {
+          float* s = dst + mine_st + (32 * (j / 4) + 2 * (j % 4) + i) * a.V;
+          if constexpr (NV == 4) *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(x);
+          else *reinterpret_cast<float2*>(s) = *reinterpret_cast<const float2*>(x);
+        }
+      }
+  };
+
+  Chunk next[NST];
+#pragma unroll
+  for (int s = 0; s < NST; ++s) next[s] = issue(s);
+  for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
+    const Chunk ch = next[0];
+#pragma unroll
+    for (int i = 0; i + 1 < NST; ++i) next[i] = next[i + 1];
+    const int flags = ch.flags, row = ch.row, len = flags & LEN;
     if (flags & NONE) break;
-    const int64_t row = w.row;
-    const int64_t seq = w.seq;
-    const int len = flags & LEN;
+    copy_wait<NST - 1>();
+    uint32_t q[NG][2][4], k[NG][2][4], vb[NV][2];
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (!STATE_ONLY) load_shared(q[i][e], mine + s * SLOT + (2 * i + e) * 512);
+        load_shared(k[i][e], mine + s * SLOT + (2 * NG + 2 * i + e) * 512);
+      }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {                      // V as 16 x 8 tiles, two rows a word
+      Vec<NV> v;
+      load_shared(v.w, mine_v + s * SLOT + e * 32 * VC * 2);
+#pragma unroll
+      for (int n = 0; n < NV; ++n) vb[n][e] = turned(v.w[n]);
+    }
+    // sums of the logarithms (base 2): P up to a row, later Z behind it.  Below 2^-150 a decay is
+    // 0 in fp32; held there, so that the differences of sums stay finite and fine
+    const int lr = lane & 15;
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(mine_g + s * SLOT) : "memory");
+    x *= LOG2E;
+    x = x < -150.0f ? -150.0f : x;
+    __syncwarp();                                      // read: the place is free
+    next[NST - 1] = issue(s);
 
     if (flags & FIRST) {
       const float* src = nullptr;
       if (flags & GOES_ON)
-        src = STATE_ONLY ? nullptr : a.ws_state + ((a.u.reverse ? row + 1 : row) / a.u.lseg * a.H + h) * KV;
+        src = STATE_ONLY ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
       else if (a.state_in)
-        src = a.state_in + (seq * a.H + h) * KV;
+        src = a.state_in + ((int64_t)ch.seq * a.H + h) * KV;
       zero = src == nullptr;
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int j = 0; j < KT; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int kk = j * 8 + 2 * t + (i & 1), c = m * 16 + g + (i >> 1) * 8;
-            st[m][j][i] = src && kk < a.K && c < width ? src[(int64_t)kk * a.V + c0 + c] : 0.0f;
-          }
+      if (!zero) load_state(src);
     }
-
-    // sums of the logarithms (base 2): P up to a row, R behind it.  Below 2^-150 a decay is 0
-    // in fp32; held there, so that the differences of sums stay finite and fine
-    float x = w.g[lane & 15] * LOG2E;
-    x = x < -150.0f ? -150.0f : x;
     if (STATE_ONLY) total += x;                        // summed over lanes at the end
-    float P = x, R = __shfl_down_sync(FULL, x, 1, 16);
-    if ((lane & 15) == 15) R = 0.0f;
+    float P = x;
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) {
-      const float y = __shfl_up_sync(FULL, P, o, 16), z = __shfl_down_sync(FULL, R, o, 16);
-      if ((lane & 15) >= o) P += y;
-      if ((lane & 15) + o < 16) R += z;
+      const float y = __shfl_up_sync(FULL, P, o, 16);
+      if (lr >= o) P += y;
     }
     const bool update = STATE_ONLY || !(flags & LAST) || ((flags & ENDS) && a.state_out);
-
-    uint32_t vb[NV][2];                                // V as 16 x 8 tiles, two rows a word
-#pragma unroll
-    for (int n = 0; n < NV; n += 2) {
-      uint32_t r[4];
-      ldsm4t(r, smem_addr(w.v + k_row * S::PV + (n * 8 + k_col) * 2));
-      vb[n][0] = r[0], vb[n][1] = r[1], vb[n + 1][0] = r[2], vb[n + 1][1] = r[3];
-    }
 
     if (!STATE_ONLY) {
       float o[NV][4];
@@ -227,12 +325,11 @@ __global__ void __launch_bounds__(NW * 32) la_mma_kernel(const __grid_constant__
         for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
       float s0[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int kk = 0; kk < DK / 16; ++kk) {
-        uint32_t qa[4], kb[4];
-        ldsm4(qa, smem_addr(w.q + q_row * S::PK + (kk * 16 + q_col) * 2));
-        ldsm4(kb, smem_addr(w.k + n_row * S::PK + (kk * 16 + n_col) * 2));
-        mma16(s0, qa, kb[0], kb[1], T());
-        mma16(s1, qa, kb[2], kb[3], T());
+      for (int kk = 0; kk < 2 * NG; ++kk) {
+        const int i0 = kk / 2, w = kk % 2 * 2;
+        const uint32_t qa[4] = {q[i0][0][w], q[i0][1][w], q[i0][0][w + 1], q[i0][1][w + 1]};
+        mma16(s0, qa, k[i0][0][w], k[i0][0][w + 1], T());
+        mma16(s1, qa, k[i0][1][w], k[i0][1][w + 1], T());
         if (!zero) {
           if (BF) {
 #pragma unroll
@@ -258,19 +355,19 @@ __global__ void __launch_bounds__(NW * 32) la_mma_kernel(const __grid_constant__
       }
       const float pg = __shfl_sync(FULL, P, g), pg8 = __shfl_sync(FULL, P, g + 8);
       if (!zero) {
-        const float e0 = ex2(pg), e1 = ex2(pg8);
+        const float e0 = a.scale * ex2(pg), e1 = a.scale * ex2(pg8);
 #pragma unroll
         for (int n = 0; n < NV; ++n) o[n][0] *= e0, o[n][1] *= e0, o[n][2] *= e1, o[n][3] *= e1;
       }
       // the decays between rows, and none to a later row
       const float p0 = __shfl_sync(FULL, P, 2 * t), p1 = __shfl_sync(FULL, P, 2 * t + 1);
       const float p8 = __shfl_sync(FULL, P, 2 * t + 8), p9 = __shfl_sync(FULL, P, 2 * t + 9);
-      s0[0] = 2 * t <= g ? s0[0] * ex2(pg - p0) : 0.0f;
-      s0[1] = 2 * t + 1 <= g ? s0[1] * ex2(pg - p1) : 0.0f;
-      s0[2] *= ex2(pg8 - p0);
-      s0[3] *= ex2(pg8 - p1);
-      s1[2] = 2 * t <= g ? s1[2] * ex2(pg8 - p8) : 0.0f;
-      s1[3] = 2 * t + 1 <= g ? s1[3] * ex2(pg8 - p9) : 0.0f;
+      s0[0] = 2 * t <= g ? s0[0] * (a.scale * ex2(pg - p0)) : 0.0f;
+      s0[1] = 2 * t + 1 <= g ? s0[1] * (a.scale * ex2(pg - p1)) : 0.0f;
+      s0[2] *= a.scale * ex2(pg8 - p0);
+      s0[3] *= a.scale * ex2(pg8 - p1);
+      s1[2] = 2 * t <= g ? s1[2] * (a.scale * ex2(pg8 - p8)) : 0.0f;
+      s1[3] = 2 * t + 1 <= g ? s1[3] * (a.scale * ex2(pg8 - p9)) : 0.0f;
       if (BF) {
         uint32_t hi[4] = {pack2(s0[0], s0[1], T()), pack2(s0[2], s0[3], T()), 0u, pack2(s1[2], s1[3], T())};
         uint32_t lo[4];
@@ -296,20 +393,13 @@ __global__ void __launch_bounds__(NW * 32) la_mma_kernel(const __grid_constant__
             },
             o, vb, len, g, t);
       }
-      // out through V's place in the slot: 16 bytes a lane
-      __syncwarp();
+      if (v_on) {
+        const int along = dir * row + g;
+        uint32_t w0[NV], w1[NV];
 #pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        *reinterpret_cast<uint32_t*>(w.v + g * S::PV + (n * 8 + 2 * t) * 2) = pack2(a.scale * o[n][0], a.scale * o[n][1], T());
-        *reinterpret_cast<uint32_t*>(w.v + (g + 8) * S::PV + (n * 8 + 2 * t) * 2) = pack2(a.scale * o[n][2], a.scale * o[n][3], T());
-      }
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < C * NV / 32; ++i) {
-        const int r = (lane + 32 * i) / NV, e = (lane + 32 * i) % NV * 8;
-        if (r < len && e < width)
-          *reinterpret_cast<uint4*>((T*)a.out + (row + dir * r) * a.os + h * a.V + c0 + e) =
-              *reinterpret_cast<const uint4*>(w.v + r * S::PV + e * 2);
+        for (int n = 0; n < NV; ++n) w0[n] = pack2(o[n][0], o[n][1], T()), w1[n] = pack2(o[n][2], o[n][3], T());
+        if (g < len) write_out(o0 + (int64_t)along * ob, w0);
+        if (g + 8 < len) write_out(o0 + (int64_t)(along + 8) * ob, w1);
       }
     }
 
@@ -322,11 +412,25 @@ __global__ void __launch_bounds__(NW * 32) la_mma_kernel(const __grid_constant__
           for (int j = 0; j < KT; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st[m][j][i] *= f;
+      } else {
+        zero = false;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int j = 0; j < KT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st[m][j][i] = 0.0f;
       }
-      zero = false;
-      R = ex2(R);
-      const float w0 = __shfl_sync(FULL, R, 2 * t), w1 = __shfl_sync(FULL, R, 2 * t + 1);
-      const float w8 = __shfl_sync(FULL, R, 2 * t + 8), w9 = __shfl_sync(FULL, R, 2 * t + 9);
+      float Z = __shfl_down_sync(FULL, x, 1, 16);
+      if (lr == 15) Z = 0.0f;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) {
+        const float z = __shfl_down_sync(FULL, Z, o, 16);
+        if (lr + o < 16) Z += z;
+      }
+      Z = ex2(Z);
+      const float w0 = __shfl_sync(FULL, Z, 2 * t), w1 = __shfl_sync(FULL, Z, 2 * t + 1);
+      const float w8 = __shfl_sync(FULL, Z, 2 * t + 8), w9 = __shfl_sync(FULL, Z, 2 * t + 9);
       constexpr int TERMS = BF && EXACT ? 3 : 2;
       uint32_t va[TERMS][MT][4];
 #pragma unroll
@@ -346,28 +450,15 @@ __global__ void __launch_bounds__(NW * 32) la_mma_kernel(const __grid_constant__
           }
         }
 #pragma unroll
-      for (int kk = 0; kk < DK / 16; ++kk) {
-        uint32_t kb[4];
-        ldsm4t(kb, smem_addr(w.k + k_row * S::PK + (kk * 16 + k_col) * 2));
+      for (int j = 0; j < KT; ++j) {
+        const uint32_t b0 = turned(k[j / 4][0][j % 4]), b1 = turned(k[j / 4][1][j % 4]);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int e = 0; e < TERMS; ++e) {
-            mma16(st[m][2 * kk], va[e][m], kb[0], kb[1], T());
-            mma16(st[m][2 * kk + 1], va[e][m], kb[2], kb[3], T());
-          }
+          for (int e = 0; e < TERMS; ++e) mma16(st[m][j], va[e][m], b0, b1, T());
       }
       if ((flags & LAST) && (STATE_ONLY || (flags & ENDS))) {
-        float* dst = STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + (seq * a.H + h) * KV;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int j = 0; j < KT; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int kk = j * 8 + 2 * t + (i & 1), c = m * 16 + g + (i >> 1) * 8;
-              if (kk < a.K && c < width) dst[(int64_t)kk * a.V + c0 + c] = st[m][j][i];
-            }
+        store_state(STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)ch.seq * a.H + h) * KV);
         if (STATE_ONLY) {
 #pragma unroll
           for (int o = 8; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o, 16);
@@ -375,38 +466,31 @@ __global__ void __launch_bounds__(NW * 32) la_mma_kernel(const __grid_constant__
         }
       }
     }
-    __syncwarp();
-    issue(w);
-    s = s + 1 == NST ? 0 : s + 1;
   }
 }
 
-template <class T, int DK, int NV, bool STATE_ONLY, bool EXACT>
+template <class T, int NG, int NV, bool STATE_ONLY, bool EXACT>
 int launch(const LaArgs& a, cudaStream_t st) {
-  auto kern = la_mma_kernel<T, DK, NV, STATE_ONLY, EXACT>;
+  auto kern = la_mma_kernel<T, NG, NV, STATE_ONLY, EXACT>;
   const cudaError_t e = tf_allow_smem(kern);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  const int64_t units = (STATE_ONLY ? a.bounds - 1 : a.u.tiles) * a.H * a.slices;
-  if ((units + NW - 1) / NW > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
-  kern<<<(unsigned)((units + NW - 1) / NW), NW * 32, sizeof(Slot<DK, NV>) * NST * NW, st>>>(a);
+  kern<<<linear_grid(a, STATE_ONLY), NW * 32, NW * NST * slot_bytes(NG, NV), st>>>(a);
   return launched();
 }
-template <class T, int DK, int NV>
+template <class T, int NG, int NV>
 int by_use(const LaArgs& a, bool state_only, cudaStream_t st) {
   // fp16 splits into two parts either way
   if constexpr (!__is_same(T, __half)) {
-    if (a.state_out && state_only) return launch<T, DK, NV, true, true>(a, st);
-    if (a.state_out) return launch<T, DK, NV, false, true>(a, st);
+    if (a.state_out && state_only) return launch<T, NG, NV, true, true>(a, st);
+    if (a.state_out) return launch<T, NG, NV, false, true>(a, st);
   }
-  return state_only ? launch<T, DK, NV, true, false>(a, st) : launch<T, DK, NV, false, false>(a, st);
+  return state_only ? launch<T, NG, NV, true, false>(a, st) : launch<T, NG, NV, false, false>(a, st);
 }
 template <class T>
 int by_width(const LaArgs& a, bool state_only, cudaStream_t st) {
-  const bool wide = linear_mma_cols(a.K, a.V) == 32;
-  if (a.K <= 16) return wide ? by_use<T, 16, 4>(a, state_only, st) : by_use<T, 16, 2>(a, state_only, st);
-  if (a.K <= 32) return wide ? by_use<T, 32, 4>(a, state_only, st) : by_use<T, 32, 2>(a, state_only, st);
-  if (a.K <= 64) return wide ? by_use<T, 64, 4>(a, state_only, st) : by_use<T, 64, 2>(a, state_only, st);
-  return by_use<T, 128, 2>(a, state_only, st);
+  if (a.K <= 32) return by_use<T, 1, 4>(a, state_only, st);
+  if (a.K <= 64) return by_use<T, 2, 4>(a, state_only, st);
+  return by_use<T, 4, 2>(a, state_only, st);
 }
 
 }  // namespace

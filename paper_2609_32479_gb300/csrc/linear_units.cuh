@@ -19,100 +19,105 @@ struct Units {
   int64_t n_seq, n_rows;
   int64_t tiles;           // >= 1
   int seg, lseg;
-  int64_t longest;         // longer sequences are cut
+  int longest;             // longer sequences are cut
   int reverse;
 };
 
-// A run of rows of one sequence, taken in the direction of the recurrence.
+// A run of rows of one sequence, taken in the direction of the recurrence.  Rows count from
+// a base row near them (a tile's or a boundary's), in 32 bits; a sequence's ends that are
+// further than FAR from it are held there.
 struct Piece {
-  int64_t lo, hi;          // rows
-  int64_t seq;
-  int64_t from;            // boundary whose state it goes on from; -1: the sequence's beginning
-  bool ends;               // it reaches the sequence's end
+  int lo, hi;
+  int seq;
+  bool goes_on;            // it does not hold the sequence's beginning
+  bool ends;               // it holds the sequence's end
 };
+constexpr int FAR = 1 << 30;
 
-// The sequences' rows, a warp reading 32 offsets at a time.
+// The sequences' offsets from the base row, a warp reading 32 at a time.
 class Offsets {
  public:
-  __device__ __forceinline__ Offsets(const Units& u, int lane) : u_(u), lane_(lane), base_(-64), mine_(0) {}
-  __device__ __forceinline__ int64_t at(int64_t i) {
-    if (i < base_ || i >= base_ + 32) {
-      base_ = i;
-      const int64_t j = i + lane_ < u_.n_seq ? i + lane_ : u_.n_seq;
-      mine_ = clamp64(u_.offs[j], 0, u_.n_rows);
+  __device__ __forceinline__ Offsets(const Units& u, int64_t base, int lane)
+      : u_(u), base_(base), lane_(lane), first_(0), mine_(0), loaded_(false) {}
+  __device__ __forceinline__ int at(int i) {
+    if (!loaded_ || (unsigned)(i - first_) >= 32u) {
+      loaded_ = true;
+      first_ = i;
+      const int64_t j = (int64_t)i + lane_ < u_.n_seq ? (int64_t)i + lane_ : u_.n_seq;
+      mine_ = (int)clamp64(clamp64(u_.offs[j], 0, u_.n_rows) - base_, -FAR, FAR);
     }
-    return __shfl_sync(FULL, mine_, (int)(i - base_));
+    return __shfl_sync(FULL, mine_, i - first_);
   }
 
  private:
   const Units& u_;
-  int lane_;
-  int64_t base_, mine_;
+  int64_t base_;
+  int lane_, first_, mine_;
+  bool loaded_;
 };
 
-// The pieces of a tile's unit, one after the other (all lanes alike).
+// The pieces of a tile's unit, one after the other (all lanes alike), from the tile's first
+// row.
 class TilePieces {
  public:
   // (idle: no piece will be asked for)
   __device__ __forceinline__ TilePieces(const Units& u, int64_t tile, int lane, bool idle)
-      : u_(u), offs_(u, lane), r0_(tile * u.seg), r1_(tile * u.seg + u.seg), last_(tile + 1 == u.tiles) {
-    b_ = r0_ == 0 || idle ? 0 : first_at_least(u.offs, u.n_seq, r0_, lane);
-    across_ = r0_ != 0 && r0_ % u.lseg == 0 && b_ > 0;
+      : u_(u), offs_(u, tile * u.seg, lane), last_(tile + 1 == u.tiles) {
+    const int64_t r0 = tile * u.seg;
+    b_ = r0 == 0 || idle ? 0 : (int)first_at_least(u.offs, u.n_seq, r0, lane);
+    cut_ = u.lseg - (int)(r0 % u.lseg);
+    across_ = r0 != 0 && cut_ == u.lseg && b_ > 0;
   }
   __device__ __forceinline__ bool next(Piece& p) {
     if (across_) {
       across_ = false;
-      const int64_t lo = offs_.at(b_ - 1), hi = offs_.at(b_);
-      if (hi - lo > u_.longest && lo < r0_ && hi > r0_) {
-        p.seq = b_ - 1, p.lo = r0_, p.hi = hi < r0_ + u_.lseg ? hi : r0_ + u_.lseg;
+      const int lo = offs_.at(b_ - 1), hi = offs_.at(b_);
+      if (hi - lo > u_.longest && lo < 0 && hi > 0) {
+        p.seq = b_ - 1, p.lo = 0, p.hi = hi < u_.lseg ? hi : u_.lseg;
         bounds(p, lo, hi);
         return true;
       }
     }
-    if (b_ >= u_.n_seq) return false;
-    const int64_t lo = offs_.at(b_);
-    if (!(lo < r1_ || last_)) return false;
-    int64_t hi = offs_.at(b_ + 1);
+    if (b_ >= (int)u_.n_seq) return false;
+    const int lo = offs_.at(b_);
+    if (!(lo < u_.seg || last_)) return false;
+    int hi = offs_.at(b_ + 1);
     if (hi < lo) hi = lo;
     p.seq = b_++, p.lo = lo, p.hi = hi;
-    if (hi - lo > u_.longest) {
-      const int64_t cut = (lo / u_.lseg + 1) * u_.lseg;
-      if (cut < hi) p.hi = cut;
-    }
+    if (hi - lo > u_.longest && cut_ < hi) p.hi = cut_ > lo ? cut_ : lo;
     bounds(p, lo, hi);
     return true;
   }
 
  private:
-  __device__ __forceinline__ void bounds(Piece& p, int64_t lo, int64_t hi) {
-    const bool first = u_.reverse ? p.hi == hi : p.lo == lo;
-    p.from = first ? -1 : (u_.reverse ? p.hi : p.lo) / u_.lseg;
+  __device__ __forceinline__ void bounds(Piece& p, int lo, int hi) {
+    p.goes_on = u_.reverse ? p.hi != hi : p.lo != lo;
     p.ends = u_.reverse ? p.lo == lo : p.hi == hi;
   }
   const Units& u_;
   Offsets offs_;
-  int64_t r0_, r1_, b_;
+  int b_, cut_;
   bool last_, across_;
 };
 
-// The piece whose end leaves a state at boundary `i`, if a cut sequence runs across it.
-// `from` is -1 where the piece holds the sequence's beginning; else the state that comes
-// from before is added later.
+// The piece whose end leaves a state at boundary `i`, if a cut sequence runs across it, its
+// rows from the boundary's.  Where it goes on, the state that comes from before is added
+// later.
 __device__ __forceinline__ bool boundary_piece(const Units& u, int64_t i, int lane, Piece& p) {
   const int64_t row = i * u.lseg;
   const int64_t b = first_at_least(u.offs, u.n_seq, row, lane);
   if (b == 0) return false;
-  Offsets offs(u, lane);
-  const int64_t lo = offs.at(b - 1), hi = offs.at(b);
-  if (!(hi - lo > u.longest && lo < row && hi > row)) return false;
-  p.seq = b - 1;
+  Offsets offs(u, row, lane);
+  const int lo = offs.at((int)b - 1), hi = offs.at((int)b);
+  if (!(hi - lo > u.longest && lo < 0 && hi > 0)) return false;
+  p.seq = (int)b - 1;
   p.ends = false;
   if (u.reverse) {
-    p.lo = row, p.hi = hi < row + u.lseg ? hi : row + u.lseg;
-    p.from = p.hi == hi ? -1 : i + 1;
+    p.lo = 0, p.hi = hi < u.lseg ? hi : u.lseg;
+    p.goes_on = p.hi != hi;
   } else {
-    p.lo = lo > row - u.lseg ? lo : row - u.lseg, p.hi = row;
-    p.from = p.lo == lo ? -1 : i - 1;
+    p.lo = lo > -u.lseg ? lo : -u.lseg, p.hi = 0;
+    p.goes_on = p.lo != lo;
   }
   return true;
 }
@@ -135,8 +140,14 @@ struct LaArgs {
   float scale;
 };
 
+// CTAs for all units, fewer than 2^31 of which there are.
+inline unsigned linear_grid(const LaArgs& a, bool state_only) {
+  const int64_t units = (state_only ? a.bounds - 1 : a.u.tiles) * a.H * a.slices;
+  return (unsigned)((units + NW - 1) / NW);
+}
+
 // linear_mma.cu: the 16-bit types on the tensor cores.  Channels of v that a warp takes:
-inline int linear_mma_cols(int K, int V) { return V > 16 && K <= 64 ? 32 : 16; }
+inline int linear_mma_cols(int K) { return K <= 64 ? 32 : 16; }
 int linear_mma(int32_t dtype, const LaArgs& a, bool state_only, cudaStream_t st);
 
 }  // namespace seqops

@@ -16,6 +16,7 @@ constexpr unsigned FULL = 0xffffffffu;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int MAX_DIM = 128;     // width of a head
 constexpr int MAX_HEADS = 256;
+constexpr int64_t MAX_STRIDE = (int64_t)1 << 28;   // elements: a row's bytes fit 32 bits
 
 // ---------------------------------------------------------------- element types
 __device__ __forceinline__ void unpack(const uint4& u, float (&x)[4], float) {
@@ -74,6 +75,9 @@ __device__ __forceinline__ uint32_t smem_addr(const void* p) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
+}
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
@@ -113,7 +117,7 @@ inline bool dim_ok(int32_t d) { return d >= 8 && d <= MAX_DIM && d % 8 == 0; }
 inline bool heads_ok(int32_t h) { return h >= 1 && h <= MAX_HEADS; }
 // A row array [rows][stride] of `width` values a row: 16-byte aligned at every row.
 inline bool rows_ok(const void* p, int64_t stride, int64_t width, int size) {
-  return p && !mis16(p) && stride >= width && stride <= (int64_t)1 << 40 && (stride * size) % 16 == 0;
+  return p && !mis16(p) && stride >= width && stride <= MAX_STRIDE && (stride * size) % 16 == 0;
 }
 inline int launched() {
   const cudaError_t e = cudaPeekAtLastError();
