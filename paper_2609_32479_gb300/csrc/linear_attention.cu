@@ -27,15 +27,14 @@ struct __align__(16) SimtSlot {
 enum { LEN = 0xff, FIRST = 0x100, LAST = 0x200, GOES_ON = 0x400, ENDS = 0x800, NONE = 0x1000 };
 
 template <int DK, bool STATE_ONLY>
-__global__ void __launch_bounds__(NW * 32) la_simt_kernel(const __grid_constant__ LaArgs a) {
+__global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   using Slot = SimtSlot<DK>;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const unsigned unit = blockIdx.x * NW + warp;
+  const int lane = threadIdx.x;
+  const unsigned unit = blockIdx.x;
   const int sl = (int)(unit % a.slices), h = (int)(unit / a.slices % a.H);
   const int64_t tile = unit / a.slices / a.H;
-  if (tile >= (STATE_ONLY ? a.bounds - 1 : a.u.tiles)) return;
-  Slot* slots = reinterpret_cast<Slot*>(smem) + warp * NST;
+  Slot* slots = reinterpret_cast<Slot*>(smem);
   const int c0 = sl * COLS, width = a.V - c0 < COLS ? a.V - c0 : COLS;
   const int dir = a.u.reverse ? -1 : 1;
   // channels beyond K and V are zeros from here on: the copies leave them alone
@@ -188,6 +187,7 @@ __global__ void __launch_bounds__(CARRY_NT) la_carry_kernel(const __grid_constan
 // A warp takes 32 columns of a head's state: 8 lanes hold four columns of a row each, and
 // four rows are read, decayed, added to and written at a time.  The state's two crossings
 // of memory are nearly all of the traffic, and bound it.
+constexpr int NW = 4;            // warps of a CTA
 struct StepArgs {
   const void *q, *k, *v;
   const float* g;
@@ -246,13 +246,12 @@ __global__ void __launch_bounds__(NW * 32) la_step_kernel(const __grid_constant_
 }
 
 // ---------------------------------------------------------------- host
-// Rows a boundary: as many as leave about 1,500 units, the warps that the GPU holds, but not
-// under 256 (a state is written and read twice a boundary) nor over 2,048.
+// Rows a boundary: as many as leave one unit for each of the 152 x 8 warps that the widest
+// kernels keep on the GPU, but not under 256 (a state is written and read twice a boundary).
 int rows_a_boundary(int64_t n_rows, int H, int V) {
-  const int64_t per_row = (int64_t)H * ((V + COLS - 1) / COLS);
-  int l = 256;
-  while (l < 2048 && n_rows / l * per_row > 3000) l *= 2;
-  return l;
+  const int64_t units_a_row = (int64_t)H * ((V + COLS - 1) / COLS);
+  const int64_t l = (n_rows * units_a_row / (152 * 8) + 255) / 256 * 256;
+  return l < 256 ? 256 : l > 2048 ? 2048 : (int)l;
 }
 constexpr int64_t LONGEST = 512;   // longer sequences are cut
 
@@ -266,11 +265,11 @@ size_t workspace_bytes(int64_t n_rows, int H, int K, int V) {
 
 template <int DK, bool STATE_ONLY>
 int launch_simt(const LaArgs& a, cudaStream_t st) {
-  const size_t sm = sizeof(SimtSlot<DK>) * NST * NW;
+  const size_t sm = sizeof(SimtSlot<DK>) * NST;
   auto kern = la_simt_kernel<DK, STATE_ONLY>;
   const cudaError_t e = tf_allow_smem(kern);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  kern<<<linear_grid(a, STATE_ONLY), NW * 32, sm, st>>>(a);
+  kern<<<linear_grid(a, STATE_ONLY), 32, sm, st>>>(a);
   return launched();
 }
 template <bool STATE_ONLY>
@@ -325,9 +324,11 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
   a.u.offs = offsets, a.u.n_seq = n_seq, a.u.n_rows = n_rows, a.u.reverse = reverse;
   a.u.lseg = rows_a_boundary(n_rows, n_heads, value_dim);
   a.u.longest = LONGEST;
-  // few rows: small tiles, so that there are units for every SM
+  // few rows: small tiles, so that there are units for every SM; long sequences: none that
+  // would find nothing to do between two boundaries
   a.u.seg = 256;
   while (a.u.seg > 16 && n_rows / a.u.seg * n_heads * a.slices < 2400) a.u.seg /= 2;
+  if (n_rows / n_seq >= LONGEST) a.u.seg = a.u.lseg;
   a.u.tiles = n_rows > 0 ? (n_rows + a.u.seg - 1) / a.u.seg : 1;
   a.bounds = 1;
   if (a.u.tiles > (int64_t)0x7fffffff / (n_heads * a.slices)) return TRACKFIT_ERR_UNSUPPORTED;

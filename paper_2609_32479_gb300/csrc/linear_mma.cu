@@ -89,26 +89,39 @@ __device__ __forceinline__ uint32_t zero_if_finite(uint32_t u, uint32_t sum, __h
   return sum;
 }
 
-// o += the product of the chunk's weights with V, by mul(d, b0, b1) for 8 channels.  A
+// o += the product of the chunk's weights with V (zero: o is not set yet), by
+// mul(d, b0, b1, anew) for 8 channels.  A
 // weight of zero does not keep an infinity or a NaN of a later row out of an earlier one's
 // sum: where V has any, each row by itself takes the rows up to its own.
 template <class T, int NV, class Mul>
-__device__ __forceinline__ void add_rows(T, Mul mul, float (&o)[NV][4], const uint32_t (&vb)[NV][2], int len, int g, int t) {
+__device__ __forceinline__ void add_rows(T, Mul mul, bool zero, float (&o)[NV][4], const uint32_t (&vb)[NV][2], int len, int g,
+                                         int t) {
   uint32_t sum = 0u;
 #pragma unroll
   for (int n = 0; n < NV; ++n) sum = zero_if_finite(vb[n][0], zero_if_finite(vb[n][1], sum, T()), T());
   if (!__any_sync(FULL, (sum & 0x7fff7fffu) != 0u)) {
+    if (zero) {
 #pragma unroll
-    for (int n = 0; n < NV; ++n) mul(o[n], vb[n][0], vb[n][1]);
+      for (int n = 0; n < NV; ++n) mul(o[n], vb[n][0], vb[n][1], true);
+    } else {
+#pragma unroll
+      for (int n = 0; n < NV; ++n) mul(o[n], vb[n][0], vb[n][1], false);
+    }
     return;
+  }
+  if (zero) {
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
   }
   for (int r = 0; r < len; ++r) {
     const uint32_t m0 = (2 * t <= r ? 0xffffu : 0u) | (2 * t + 1 <= r ? 0xffff0000u : 0u);
     const uint32_t m1 = (2 * t + 8 <= r ? 0xffffu : 0u) | (2 * t + 9 <= r ? 0xffff0000u : 0u);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-      float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      mul(d, vb[n][0] & m0, vb[n][1] & m1);
+      float d[4];
+      mul(d, vb[n][0] & m0, vb[n][1] & m1, true);
       if (g == r) o[n][0] += d[0], o[n][1] += d[1];
       if (g + 8 == r) o[n][2] += d[2], o[n][3] += d[3];
     }
@@ -116,26 +129,28 @@ __device__ __forceinline__ void add_rows(T, Mul mul, float (&o)[NV][4], const ui
 }
 
 template <class T, int NG, int NV, bool STATE_ONLY, bool EXACT>
-__global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const __grid_constant__ LaArgs a) {
+__global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) la_mma_kernel(const __grid_constant__ LaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr bool BF = !__is_same(T, __half);
   constexpr int MT = NV / 2, KT = NG * 4;             // tiles of the state: MT x 16 by KT x 8
+  // With 128 registers a thread (16 warps an SM) q and k are read where they are used; with 255
+  // (8 warps) early, and their place filled again: 221 instead of 305 us at K = 64
+  constexpr bool EARLY = NG == 2;
   constexpr int VC = NV * 2;                           // channels of V a lane
   constexpr int SLOT = slot_bytes(NG, NV);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const unsigned unit = blockIdx.x * NW + warp;
+  const int lane = threadIdx.x;
+  const unsigned unit = blockIdx.x;
   const int sl = (int)(unit % a.slices), h = (int)(unit / a.slices % a.H);
   const int64_t tile = unit / a.slices / a.H;
-  if (tile >= (STATE_ONLY ? a.bounds - 1 : a.u.tiles)) return;
   const int c0 = sl * NV * 8, width = a.V - c0 < NV * 8 ? a.V - c0 : NV * 8;
   const int dir = a.u.reverse ? -1 : 1;
   const int g = lane >> 2, t = lane & 3;
   const int64_t base = STATE_ONLY ? (tile + 1) * a.u.lseg : tile * a.u.seg;
   // this lane's place in the queue: 16 bytes of each of q [group][row half], k likewise, its V
   // [row half], g
-  const uint32_t mine = smem_addr(smem) + warp * NST * SLOT + lane * 16;
-  const uint32_t mine_v = smem_addr(smem) + warp * NST * SLOT + NG * 4 * 512 + lane * VC * 2;
-  const uint32_t mine_g = smem_addr(smem) + warp * NST * SLOT + NG * 4 * 512 + 2 * 32 * VC * 2 + lane * 4;
+  const uint32_t mine = smem_addr(smem) + lane * 16;
+  const uint32_t mine_v = smem_addr(smem) + NG * 4 * 512 + lane * VC * 2;
+  const uint32_t mine_g = smem_addr(smem) + NG * 4 * 512 + 2 * 32 * VC * 2 + lane * 4;
   // channels beyond K and V are zeros from here on: the copies leave them alone
   for (int s = 0; s < NST; ++s) {
 #pragma unroll
@@ -274,14 +289,17 @@ __global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const 
     const int flags = ch.flags, row = ch.row, len = flags & LEN;
     if (flags & NONE) break;
     copy_wait<NST - 1>();
+    const uint32_t slot = mine + s * SLOT;
     uint32_t q[NG][2][4], k[NG][2][4], vb[NV][2];
+    if (EARLY) {
 #pragma unroll
-    for (int i = 0; i < NG; ++i)
+      for (int i = 0; i < NG; ++i)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (!STATE_ONLY) load_shared(q[i][e], mine + s * SLOT + (2 * i + e) * 512);
-        load_shared(k[i][e], mine + s * SLOT + (2 * NG + 2 * i + e) * 512);
-      }
+        for (int e = 0; e < 2; ++e) {
+          if (!STATE_ONLY) load_shared(q[i][e], slot + (2 * i + e) * 512);
+          load_shared(k[i][e], slot + (2 * NG + 2 * i + e) * 512);
+        }
+    }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {                      // V as 16 x 8 tiles, two rows a word
       Vec<NV> v;
@@ -294,11 +312,12 @@ __global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const 
     const int lr = lane & 15;
     float x;
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(mine_g + s * SLOT) : "memory");
+    if (EARLY) {
+      __syncwarp();                                    // read: the place is free
+      next[NST - 1] = issue(s);
+    }
     x *= LOG2E;
     x = x < -150.0f ? -150.0f : x;
-    __syncwarp();                                      // read: the place is free
-    next[NST - 1] = issue(s);
-
     if (flags & FIRST) {
       const float* src = nullptr;
       if (flags & GOES_ON)
@@ -318,18 +337,31 @@ __global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const 
     const bool update = STATE_ONLY || !(flags & LAST) || ((flags & ENDS) && a.state_out);
 
     if (!STATE_ONLY) {
-      float o[NV][4];
+      float o[NV][4], s0[4], s1[4];
+      if (!zero) {
 #pragma unroll
-      for (int n = 0; n < NV; ++n)
+        for (int n = 0; n < NV; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
-      float s0[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
+      }
 #pragma unroll
       for (int kk = 0; kk < 2 * NG; ++kk) {
         const int i0 = kk / 2, w = kk % 2 * 2;
+        if (!EARLY && w == 0) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            load_shared(q[i0][e], slot + (2 * i0 + e) * 512);
+            load_shared(k[i0][e], slot + (2 * NG + 2 * i0 + e) * 512);
+          }
+        }
         const uint32_t qa[4] = {q[i0][0][w], q[i0][1][w], q[i0][0][w + 1], q[i0][1][w + 1]};
-        mma16(s0, qa, k[i0][0][w], k[i0][0][w + 1], T());
-        mma16(s1, qa, k[i0][1][w], k[i0][1][w + 1], T());
+        if (kk == 0) {
+          mma16_new(s0, qa, k[i0][0][w], k[i0][0][w + 1], T());
+          mma16_new(s1, qa, k[i0][1][w], k[i0][1][w + 1], T());
+        } else {
+          mma16(s0, qa, k[i0][0][w], k[i0][0][w + 1], T());
+          mma16(s1, qa, k[i0][1][w], k[i0][1][w + 1], T());
+        }
         if (!zero) {
           if (BF) {
 #pragma unroll
@@ -376,22 +408,24 @@ __global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const 
         lo[2] = 0u, lo[3] = pack2(s1[2] - h3.x, s1[3] - h3.y, T());
         add_rows(
             T(),
-            [&](float(&d)[4], uint32_t b0, uint32_t b1) {
-              mma16(d, hi, b0, b1, T());
+            [&](float(&d)[4], uint32_t b0, uint32_t b1, bool anew) {
+              if (anew) mma16_new(d, hi, b0, b1, T());
+              else mma16(d, hi, b0, b1, T());
               mma16(d, lo, b0, b1, T());
             },
-            o, vb, len, g, t);
+            zero, o, vb, len, g, t);
       } else {
         const uint32_t f0 = tf32(s0[0]), f1 = tf32(s0[1]), f2 = tf32(s0[2]), f3 = tf32(s0[3]);
         const uint32_t f6 = tf32(s1[2]), f7 = tf32(s1[3]);
         add_rows(
             T(),
-            [&](float(&d)[4], uint32_t b0, uint32_t b1) {
+            [&](float(&d)[4], uint32_t b0, uint32_t b1, bool anew) {
+              if (anew) d[0] = d[1] = d[2] = d[3] = 0.0f;
               const float2 v0 = halves(b0, T()), v1 = halves(b1, T());
               mma8(d, f0, f2, f1, f3, __float_as_uint(v0.x), __float_as_uint(v0.y));
               mma8(d, 0u, f6, 0u, f7, __float_as_uint(v1.x), __float_as_uint(v1.y));
             },
-            o, vb, len, g, t);
+            zero, o, vb, len, g, t);
       }
       if (v_on) {
         const int along = dir * row + g;
@@ -451,7 +485,12 @@ __global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const 
         }
 #pragma unroll
       for (int j = 0; j < KT; ++j) {
-        const uint32_t b0 = turned(k[j / 4][0][j % 4]), b1 = turned(k[j / 4][1][j % 4]);
+        const int i0 = j / 4;
+        if (!EARLY && j % 4 == 0) {
+          load_shared(k[i0][0], slot + (2 * NG + 2 * i0) * 512);
+          load_shared(k[i0][1], slot + (2 * NG + 2 * i0 + 1) * 512);
+        }
+        const uint32_t b0 = turned(k[i0][0][j % 4]), b1 = turned(k[i0][1][j % 4]);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -466,6 +505,10 @@ __global__ void __launch_bounds__(NW * 32, NG == 1 ? 3 : 2) la_mma_kernel(const 
         }
       }
     }
+    if (!EARLY) {
+      __syncwarp();
+      next[NST - 1] = issue(s);
+    }
   }
 }
 
@@ -474,7 +517,7 @@ int launch(const LaArgs& a, cudaStream_t st) {
   auto kern = la_mma_kernel<T, NG, NV, STATE_ONLY, EXACT>;
   const cudaError_t e = tf_allow_smem(kern);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  kern<<<linear_grid(a, STATE_ONLY), NW * 32, NW * NST * slot_bytes(NG, NV), st>>>(a);
+  kern<<<linear_grid(a, STATE_ONLY), 32, NST * slot_bytes(NG, NV), st>>>(a);
   return launched();
 }
 template <class T, int NG, int NV>

@@ -122,8 +122,6 @@ __device__ __forceinline__ bool boundary_piece(const Units& u, int64_t i, int la
   return true;
 }
 
-constexpr int NW = 4;            // warps of a CTA, each with a unit of its own
-
 struct LaArgs {
   Units u;
   const void *q, *k, *v;
@@ -140,10 +138,11 @@ struct LaArgs {
   float scale;
 };
 
-// CTAs for all units, fewer than 2^31 of which there are.
+// All units, fewer than 2^31: a CTA of one warp each, so that what a unit is comes from the
+// CTA's number (the same for all lanes, which the compiler then knows), and so that registers
+// are given out by the warp.
 inline unsigned linear_grid(const LaArgs& a, bool state_only) {
-  const int64_t units = (state_only ? a.bounds - 1 : a.u.tiles) * a.H * a.slices;
-  return (unsigned)((units + NW - 1) / NW);
+  return (unsigned)((state_only ? a.bounds - 1 : a.u.tiles) * a.H * a.slices);
 }
 
 // linear_mma.cu: the 16-bit types on the tensor cores.  Channels of v that a warp takes:
