@@ -5,27 +5,17 @@
 //
 // A query whose sequence has no states gets zeros.  Heads of the queries share a head of
 // the states in groups of q_heads / kv_heads.
-#include "seq_ops.cuh"
+#include "cross_units.cuh"
 
 namespace {
 using namespace seqops;
 
 constexpr int NW = 4;
+constexpr int64_t MOST_ROWS = 0x7fffff00;   // of the products, and of states: counted in 32 bits
 
-struct CaArgs {
-  const void *q, *k, *v;
-  void* out;
-  int64_t qs, ks, vs, os;        // row strides in elements
-  const int64_t *qo, *ko;        // offsets [n_seq + 1]
-  int64_t nq, nk, n_seq;
-  int Hq, Hk, D;
-  float scale2;                  // scale * log2(e)
-};
-
-// A warp takes one row of one head: the lanes take a state each for the products with the
-// query, then D / 32 channels each for the sum of the values.
-template <class T>
-__global__ void __launch_bounds__(NW * 32) ca_simt_kernel(const __grid_constant__ CaArgs a) {
+// fp32: a warp takes one row of one head: the lanes take a state each for the products with
+// the query, then D / 32 channels each for the sum of the values.
+__global__ void __launch_bounds__(NW * 32) ca_simt_kernel(const __grid_constant__ CaArgs a, float scale2) {
   __shared__ float sq[NW][MAX_DIM];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t unit = (int64_t)blockIdx.x * NW + warp;
@@ -35,10 +25,10 @@ __global__ void __launch_bounds__(NW * 32) ca_simt_kernel(const __grid_constant_
   const int64_t b = first_at_least(a.qo, a.n_seq, row + 1, lane) - 1;
   if (b < 0 || !(row < a.qo[b + 1])) return;      // a row of no sequence
   const int64_t lo = clamp64(a.ko[b], 0, a.nk), hi = clamp64(a.ko[b + 1], lo, a.nk);
-  const T* q = (const T*)a.q + row * a.qs + h * a.D;
-  const T* k = (const T*)a.k + (h / (a.Hq / a.Hk)) * a.D;
-  const T* v = (const T*)a.v + (h / (a.Hq / a.Hk)) * a.D;
-  for (int i = lane; i < a.D; i += 32) sq[warp][i] = to_float(q[i]) * a.scale2;
+  const float* q = (const float*)a.q + row * a.qs + h * a.D;
+  const float* k = (const float*)a.k + h / a.G * a.D;
+  const float* v = (const float*)a.v + h / a.G * a.D;
+  for (int i = lane; i < a.D; i += 32) sq[warp][i] = q[i] * scale2;
   __syncwarp();
   float m = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int64_t j0 = lo; j0 < hi; j0 += 32) {
@@ -46,7 +36,7 @@ __global__ void __launch_bounds__(NW * 32) ca_simt_kernel(const __grid_constant_
     float s = -INFINITY;
     if (j < hi) {
       s = 0.0f;
-      for (int i = 0; i < a.D; ++i) s = fmaf(sq[warp][i], to_float(k[j * a.ks + i]), s);
+      for (int i = 0; i < a.D; ++i) s = fmaf(sq[warp][i], k[j * a.ks + i], s);
     }
     float mx = s;
 #pragma unroll
@@ -67,29 +57,70 @@ __global__ void __launch_bounds__(NW * 32) ca_simt_kernel(const __grid_constant_
       const float pj = __shfl_sync(FULL, p, jj);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.D) o[c] = fmaf(pj, to_float(v[(j0 + jj) * a.vs + lane + 32 * c]), o[c]);
+        if (lane + 32 * c < a.D) o[c] = fmaf(pj, v[(j0 + jj) * a.vs + lane + 32 * c], o[c]);
     }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // nothing to read, or scores of -inf only: zeros
 #pragma unroll
   for (int c = 0; c < 4; ++c)
-    if (lane + 32 * c < a.D) put((T*)a.out + row * a.os + h * a.D + lane + 32 * c, o[c] * inv);
+    if (lane + 32 * c < a.D) ((float*)a.out)[row * a.os + h * a.D + lane + 32 * c] = o[c] * inv;
 }
 
+// The parts of each row's range joined: a warp a row and head of the states.
 template <class T>
-int launch_simt(const CaArgs& a, cudaStream_t st) {
-  const int64_t units = a.nq * a.Hq;
-  if ((units + NW - 1) / NW > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
-  ca_simt_kernel<T><<<(unsigned)((units + NW - 1) / NW), NW * 32, 0, st>>>(a);
-  return launched();
+__global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant__ CaArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = (int64_t)blockIdx.x * NW + (threadIdx.x >> 5);
+  const int64_t rows = a.nq * a.G, all = rows * a.Hk;
+  if (unit >= all) return;
+  const int hk = (int)(unit % a.Hk);
+  const int64_t row = unit / a.Hk, q = row / a.G;
+  const int64_t b = first_at_least(a.qo, a.n_seq, q + 1, lane) - 1;
+  if (b < 0 || !(q < a.qo[b + 1])) return;      // a row of no sequence: no part has been written
+  // a lane a part (splits <= 32)
+  const float2 ml = lane < a.splits ? a.ws_ml[lane * all + unit] : make_float2(-INFINITY, 0.0f);
+  float m = ml.x;
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, x));
+  const float f = ex2(ml.x - (m == -INFINITY ? 0.0f : m));
+  float l = ml.y * f;
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(FULL, l, x);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < a.splits; ++s) {
+    const float fs = __shfl_sync(FULL, f, s) * inv;
+    const float* p = a.ws_o + (s * all + unit) * a.D;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (lane + 32 * c < a.D) o[c] = fmaf(fs, p[lane + 32 * c], o[c]);
+  }
+  T* out = (T*)a.out + q * a.os + (hk * a.G + row % a.G) * a.D;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    if (lane + 32 * c < a.D) put(out + lane + 32 * c, o[c]);
+}
+
+// Parts of each row's range: as many as give 152 x 12 warps something to do, not under 256
+// states each on average, and at most the 32 that the joining warp has lanes for.
+int splits_of(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk) {
+  if (dtype == TRACKFIT_FP32 || nq <= 0 || n_seq <= 0) return 1;
+  const int64_t units = (nq * (Hq / Hk) + 15) / 16 * Hk;
+  const int64_t most = nk / n_seq / 256;
+  int64_t s = 152 * 12 / units;
+  if (s > most) s = most;
+  return s < 1 ? 1 : s > 32 ? 32 : (int)s;
 }
 
 }  // namespace
 
 extern "C" size_t trackfit_cross_attention_workspace(int32_t dtype, int64_t n_q_rows, int64_t n_kv_rows, int64_t n_seq,
                                                      int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
-  (void)dtype, (void)n_q_rows, (void)n_kv_rows, (void)n_seq, (void)q_heads, (void)kv_heads, (void)head_dim;
-  return 0;
+  if (!type_ok(dtype) || n_q_rows < 0 || n_kv_rows < 0 || n_seq < 0 || !heads_ok(q_heads) || !heads_ok(kv_heads) ||
+      q_heads % kv_heads != 0 || !dim_ok(head_dim) || n_q_rows > MOST_ROWS / (q_heads / kv_heads) || n_kv_rows > MOST_ROWS)
+    return 0;
+  const int s = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
+  return s > 1 ? (size_t)s * n_q_rows * q_heads * (head_dim + 2) * 4 : 0;
 }
 
 extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, const int64_t* q_offsets,
@@ -98,12 +129,10 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
                                         int32_t q_heads, int32_t kv_heads, int32_t head_dim, float scale, void* out,
                                         int64_t out_stride, void* workspace, size_t workspace_size, void* stream) {
   tf_nvtx_range nvtx_range("trackfit_cross_attention");
-  const int64_t most = (int64_t)1 << 40;
-  if (!type_ok(dtype) || n_q_rows < 0 || n_q_rows > most || n_kv_rows < 0 || n_kv_rows > most || n_seq < 0 ||
-      n_seq > 0x7fffffff)
-    return TRACKFIT_ERR_INVALID_ARG;
+  if (!type_ok(dtype) || n_q_rows < 0 || n_kv_rows < 0 || n_seq < 0 || n_seq > 0x7fffffff) return TRACKFIT_ERR_INVALID_ARG;
   if (!heads_ok(q_heads) || !heads_ok(kv_heads) || q_heads % kv_heads != 0 || !dim_ok(head_dim))
     return TRACKFIT_ERR_UNSUPPORTED;
+  if (n_q_rows > MOST_ROWS / (q_heads / kv_heads) || n_kv_rows > MOST_ROWS) return TRACKFIT_ERR_UNSUPPORTED;
   if (!isfinite(scale)) return TRACKFIT_ERR_INVALID_ARG;
   if (n_seq == 0 || n_q_rows == 0) return TRACKFIT_OK;
   const int sz = type_size(dtype);
@@ -122,9 +151,23 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
   a.q = q, a.k = k, a.v = v, a.out = out;
   a.qs = q_stride, a.ks = k_stride, a.vs = v_stride, a.os = out_stride;
   a.qo = q_offsets, a.ko = kv_offsets, a.nq = n_q_rows, a.nk = n_kv_rows, a.n_seq = n_seq;
-  a.Hq = q_heads, a.Hk = kv_heads, a.D = head_dim, a.scale2 = scale * LOG2E;
+  a.Hq = q_heads, a.Hk = kv_heads, a.G = q_heads / kv_heads, a.D = head_dim;
+  a.scale2 = scale == 0.0f ? 1.0f : fabsf(scale) * LOG2E;
+  a.q_and = scale == 0.0f ? 0u : ~0u, a.q_xor = scale < 0.0f ? 0x80008000u : 0u;
+  a.splits = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (need > 0 ? (int64_t)a.splits * n_q_rows * q_heads * head_dim : 0));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (dtype == TRACKFIT_FP32) return launch_simt<float>(a, st);
-  if (dtype == TRACKFIT_BF16_PROJ) return launch_simt<__nv_bfloat16>(a, st);
-  return launch_simt<__half>(a, st);
+  const int64_t warps = n_q_rows * q_heads;       // of the kernels that take a row and head
+  if ((warps + NW - 1) / NW > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
+  const unsigned grid = (unsigned)((warps + NW - 1) / NW);
+  if (dtype == TRACKFIT_FP32) {
+    ca_simt_kernel<<<grid, NW * 32, 0, st>>>(a, scale * LOG2E);
+    return launched();
+  }
+  const int rc = cross_mma(dtype, a, st);
+  if (rc != TRACKFIT_OK || a.splits == 1) return rc;
+  if (dtype == TRACKFIT_BF16_PROJ) ca_join_kernel<__nv_bfloat16><<<grid, NW * 32, 0, st>>>(a);
+  else ca_join_kernel<__half><<<grid, NW * 32, 0, st>>>(a);
+  return launched();
 }

@@ -55,38 +55,10 @@ template <int NV>
 struct Vec {
   uint32_t w[NV];
 };
-__device__ __forceinline__ void load_shared(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void load_shared(uint32_t (&r)[2], uint32_t addr) {
-  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
-}
 template <int BYTES>
 __device__ __forceinline__ void copy_v(uint32_t dst, const void* src, bool there) {
   if constexpr (BYTES == 16) copy16(dst, src, there);
   else copy8(dst, src, there);
-}
-
-// An 8 x 8 tile of 16-bit values with rows and columns exchanged.
-__device__ __forceinline__ uint32_t turned(uint32_t u) {
-  uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(u));
-  return d;
-}
-__device__ __forceinline__ void write_out(void* p, const uint32_t (&w)[4]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void write_out(void* p, const uint32_t (&w)[2]) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-}
-
-__device__ __forceinline__ uint32_t zero_if_finite(uint32_t u, uint32_t sum, __nv_bfloat16) {
-  asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(u), "r"(0u));
-  return sum;
-}
-__device__ __forceinline__ uint32_t zero_if_finite(uint32_t u, uint32_t sum, __half) {
-  asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(u), "r"(0u));
-  return sum;
 }
 
 // o += the product of the chunk's weights with V (zero: o is not set yet), by
