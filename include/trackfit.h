@@ -442,7 +442,8 @@ int trackfit_qk_norm(int32_t dtype, const void* q, int64_t q_stride, int32_t q_h
  *   workspace   trackfit_linear_attention_workspace() bytes, 16-byte aligned (sequences
  *               of more than 512 rows are cut and their parts joined through it; NULL
  *               when that is 0). */
-size_t trackfit_linear_attention_workspace(int64_t n_rows, int32_t n_heads, int32_t key_dim, int32_t value_dim);
+size_t trackfit_linear_attention_workspace(int64_t n_rows, int64_t n_seq, int32_t n_heads, int32_t key_dim,
+                                           int32_t value_dim);
 int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                               const void* v, int64_t v_stride, const float* log_decay, int64_t decay_stride,
                               int64_t n_rows, const int64_t* offsets, int64_t n_seq, int32_t n_heads, int32_t key_dim,

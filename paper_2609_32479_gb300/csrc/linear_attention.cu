@@ -253,10 +253,15 @@ int rows_a_boundary(int64_t n_rows, int H, int V) {
   const int64_t l = (n_rows * units_a_row / (152 * 8) + 255) / 256 * 256;
   return l < 256 ? 256 : l > 2048 ? 2048 : (int)l;
 }
-constexpr int64_t LONGEST = 512;   // longer sequences are cut
+constexpr int LONGEST = 512;   // longer sequences are cut
 
-size_t workspace_bytes(int64_t n_rows, int H, int K, int V) {
-  if (n_rows <= LONGEST) return 0;
+// Whether any may be: not where there are few rows of sequences that are short on average.  The
+// two launches would cost a small call more than a warp's time for the longest sequence that
+// could be among them, 16,384 rows, is likely to (an event of 211 tracks: 13 us instead of 7).
+bool cuts(int64_t n_rows, int64_t n_seq) { return n_rows > LONGEST && (n_rows > 16384 || n_rows > 64 * n_seq); }
+
+size_t workspace_bytes(int64_t n_rows, int64_t n_seq, int H, int K, int V) {
+  if (!cuts(n_rows, n_seq)) return 0;
   const int l = rows_a_boundary(n_rows, H, V);
   const size_t bounds = (size_t)((n_rows + l - 1) / l);
   const size_t flags = (bounds * 4 + 15) / 16 * 16, decay = (bounds * H * 4 + 15) / 16 * 16;
@@ -267,8 +272,7 @@ template <int DK, bool STATE_ONLY>
 int launch_simt(const LaArgs& a, cudaStream_t st) {
   const size_t sm = sizeof(SimtSlot<DK>) * NST;
   auto kern = la_simt_kernel<DK, STATE_ONLY>;
-  const cudaError_t e = tf_allow_smem(kern);
-  if (e != cudaSuccess) return tf_status_from_cuda(e);
+  static_assert(sizeof(SimtSlot<DK>) * NST <= 48 * 1024, "needs no leave");
   kern<<<linear_grid(a, STATE_ONLY), 32, sm, st>>>(a);
   return launched();
 }
@@ -283,10 +287,10 @@ int run(int32_t dtype, const LaArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-extern "C" size_t trackfit_linear_attention_workspace(int64_t n_rows, int32_t n_heads, int32_t key_dim,
-                                                      int32_t value_dim) {
-  if (n_rows < 0 || n_rows > (int64_t)1 << 40 || !heads_ok(n_heads) || !dim_ok(key_dim) || !dim_ok(value_dim)) return 0;
-  return workspace_bytes(n_rows, n_heads, key_dim, value_dim);
+extern "C" size_t trackfit_linear_attention_workspace(int64_t n_rows, int64_t n_seq, int32_t n_heads,
+                                                      int32_t key_dim, int32_t value_dim) {
+  if (n_rows < 0 || n_rows > (int64_t)1 << 40 || n_seq <= 0 || !heads_ok(n_heads) || !dim_ok(key_dim) || !dim_ok(value_dim)) return 0;
+  return workspace_bytes(n_rows, n_seq, n_heads, key_dim, value_dim);
 }
 
 extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q_stride, const void* k,
@@ -312,7 +316,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
     if (!log_decay || mis4(log_decay) || decay_stride < n_heads || decay_stride > MAX_STRIDE)
       return TRACKFIT_ERR_INVALID_ARG;
   }
-  const size_t need = workspace_bytes(n_rows, n_heads, key_dim, value_dim);
+  const size_t need = workspace_bytes(n_rows, n_seq, n_heads, key_dim, value_dim);
   if (need > 0 && (!workspace || mis16(workspace) || workspace_size < need)) return TRACKFIT_ERR_INVALID_ARG;
   LaArgs a;
   a.q = q, a.k = k, a.v = v, a.g = log_decay, a.out = out;
@@ -323,7 +327,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
   a.scale = scale;
   a.u.offs = offsets, a.u.n_seq = n_seq, a.u.n_rows = n_rows, a.u.reverse = reverse;
   a.u.lseg = rows_a_boundary(n_rows, n_heads, value_dim);
-  a.u.longest = LONGEST;
+  a.u.longest = need > 0 ? LONGEST : 0x7fffffff;
   // few rows: small tiles, so that there are units for every SM; long sequences: none that
   // would find nothing to do between two boundaries
   a.u.seg = 256;

@@ -487,8 +487,7 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) la_mma_kernel(const __gr
 template <class T, int NG, int NV, bool STATE_ONLY, bool EXACT>
 int launch(const LaArgs& a, cudaStream_t st) {
   auto kern = la_mma_kernel<T, NG, NV, STATE_ONLY, EXACT>;
-  const cudaError_t e = tf_allow_smem(kern);
-  if (e != cudaSuccess) return tf_status_from_cuda(e);
+  static_assert(NST * slot_bytes(NG, NV) <= 48 * 1024, "needs no leave");
   kern<<<linear_grid(a, STATE_ONLY), 32, NST * slot_bytes(NG, NV), st>>>(a);
   return launched();
 }

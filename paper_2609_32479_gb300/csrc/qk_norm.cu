@@ -19,6 +19,7 @@ namespace {
 using namespace seqops;
 
 constexpr int WARPS = 8;
+constexpr int CTAS = 4;          // of an SM
 constexpr int MAX_ROWS = 4;      // rows that a warp takes at a time
 
 struct QkArgs {
@@ -35,24 +36,23 @@ struct QkArgs {
 };
 
 template <class T, int G>
-__global__ void __launch_bounds__(WARPS * 32) qk_norm_kernel(const __grid_constant__ QkArgs a) {
+__global__ void __launch_bounds__(WARPS * 32, CTAS) qk_norm_kernel(const __grid_constant__ QkArgs a) {
   constexpr int VE = 16 / sizeof(T);
   constexpr int HPP = 32 / G;                       // heads of a pass
-  __shared__ __align__(16) float tab_c[WARPS][MAX_ROWS][MAX_DIM / 2];
-  __shared__ __align__(16) float tab_s[WARPS][MAX_ROWS][MAX_DIM / 2];
+  // cosines, sines and sines with the other sign of a row's angles
+  __shared__ __align__(16) float tab[WARPS][MAX_ROWS][3][MAX_DIM / 2];
+  __shared__ uint64_t freq[MAX_DIM / 2];            // (lanes ask for different ones at once)
+  for (int i = threadIdx.x; i < a.half; i += WARPS * 32) freq[i] = a.freq[i];
+  __syncthreads();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int vi = lane % G, e0 = vi * VE;            // this lane's channels of a head
   const bool in_head = e0 < a.D;
   const int half = a.half, hl = half / VE;          // lanes between the halves of a pair
   const bool lower = e0 < half, turned = e0 < 2 * half;
-  const int ti = lower ? e0 : e0 - half;            // first angle of this lane
   const int mate = turned ? (lower ? lane + hl : lane - hl) : lane;
-  float gq[VE], gk[VE];
-#pragma unroll
-  for (int i = 0; i < VE; ++i) {
-    gq[i] = a.qg && in_head ? a.qg[e0 + i] : 1.0f;
-    gk[i] = a.kg && in_head ? a.kg[e0 + i] : 1.0f;
-  }
+  // the lower half of a pair is a cos - b sin, the upper b cos + a sin
+  const float* tc = &tab[warp][0][0][turned ? (lower ? e0 : e0 - half) : 0];
+  const float* ts = tc + (lower ? 2 : 1) * (MAX_DIM / 2);
   const float inv_d = 1.0f / (float)a.D;
   const int heads = a.hq + a.hk;
   const int passes = (heads + HPP - 1) / HPP;
@@ -61,41 +61,35 @@ __global__ void __launch_bounds__(WARPS * 32) qk_norm_kernel(const __grid_consta
   const int64_t step = (int64_t)gridDim.x * WARPS * a.rows;
   for (int64_t r0 = ((int64_t)blockIdx.x * WARPS + warp) * a.rows; r0 < a.n; r0 += step) {
     const int nr = a.n - r0 < a.rows ? (int)(a.n - r0) : a.rows;
-    if (half > 0) {
-      __syncwarp();
-      for (int i = lane; i < nr << lh; i += 32) {
-        const int f = i & ((1 << lh) - 1), rr = i >> lh;
-        if (f >= half) continue;
-        const uint64_t turn = (uint64_t)(int64_t)a.pos[r0 + rr] * a.freq[f];
-        float s, c;
-        sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &c);   // half turns in [-1, 1)
-        tab_c[warp][rr][f] = c;
-        tab_s[warp][rr][f] = s;
-      }
-      __syncwarp();
-    }
-    const int items = nr * passes;
-    for (int it = 0; it < items; it += 2) {
-      uint4 u[2];
-      bool on[2];
-      const T* src[2];
-      T* dst[2];
-      bool isq[2];
-      int row[2];
+    for (int p = 0; p < passes; ++p) {
+      const int head = p * HPP + lane / G;
+      const bool on = head < heads && in_head, isq = head < a.hq;
+      const T* src = isq ? (const T*)a.q + r0 * a.qs + head * a.D : (const T*)a.k + r0 * a.ks + (head - a.hq) * a.D;
+      T* dst = isq ? (T*)a.qo + r0 * a.qos + head * a.D : (T*)a.ko + r0 * a.kos + (head - a.hq) * a.D;
+      const int64_t from = isq ? a.qs : a.ks, to = isq ? a.qos : a.kos;
+      uint4 u[MAX_ROWS];                            // the rows' loads under way together
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int rr = (it + j) / passes, head = ((it + j) - rr * passes) * HPP + lane / G;
-        on[j] = it + j < items && head < heads && in_head;
-        isq[j] = head < a.hq;
-        row[j] = rr < nr ? rr : 0;
-        const int hh = isq[j] ? head : head - a.hq;
-        const int64_t r = r0 + rr;
-        src[j] = (isq[j] ? (const T*)a.q + r * a.qs : (const T*)a.k + r * a.ks) + hh * a.D + e0;
-        dst[j] = (isq[j] ? (T*)a.qo + r * a.qos : (T*)a.ko + r * a.kos) + hh * a.D + e0;
-        u[j] = on[j] ? *reinterpret_cast<const uint4*>(src[j]) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < MAX_ROWS; ++j)
+        u[j] = on && j < nr ? *reinterpret_cast<const uint4*>(src + j * from + e0) : make_uint4(0, 0, 0, 0);
+      if (p == 0 && half > 0) {                     // the angles, while the rows come
+        __syncwarp();
+        for (int i = lane; i < nr << lh; i += 32) {
+          const int f = i & ((1 << lh) - 1), rr = i >> lh;
+          if (f >= half) continue;
+          const uint64_t turn = (uint64_t)(int64_t)a.pos[r0 + rr] * freq[f];
+          float s, c;
+          sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &c);   // half turns in [-1, 1)
+          tab[warp][rr][0][f] = c, tab[warp][rr][1][f] = s, tab[warp][rr][2][f] = -s;
+        }
+        __syncwarp();
       }
+      const float* gain = isq ? a.qg : a.kg;
+      float gn[VE];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int i = 0; i < VE; ++i) gn[i] = gain && on ? gain[e0 + i] : 1.0f;
+#pragma unroll
+      for (int j = 0; j < MAX_ROWS; ++j) {
+        if (j >= nr) break;
         float x[VE];
         unpack(u[j], x, T());
         float ss = 0.0f;
@@ -105,22 +99,21 @@ __global__ void __launch_bounds__(WARPS * 32) qk_norm_kernel(const __grid_consta
         for (int o = G / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL, ss, o);
         const float inv = rsqrtf(ss * inv_d + a.eps);
 #pragma unroll
-        for (int i = 0; i < VE; ++i) x[i] *= inv * (isq[j] ? gq[i] : gk[i]);
+        for (int i = 0; i < VE; ++i) x[i] *= inv * gn[i];
         if (half > 0) {
           float c[VE], s[VE];
 #pragma unroll
           for (int i = 0; i < VE; i += 4) {
-            *reinterpret_cast<float4*>(&c[i]) = *reinterpret_cast<const float4*>(&tab_c[warp][row[j]][turned ? ti + i : 0]);
-            *reinterpret_cast<float4*>(&s[i]) = *reinterpret_cast<const float4*>(&tab_s[warp][row[j]][turned ? ti + i : 0]);
+            *reinterpret_cast<float4*>(&c[i]) = *reinterpret_cast<const float4*>(tc + j * 3 * (MAX_DIM / 2) + i);
+            *reinterpret_cast<float4*>(&s[i]) = *reinterpret_cast<const float4*>(ts + j * 3 * (MAX_DIM / 2) + i);
           }
 #pragma unroll
           for (int i = 0; i < VE; ++i) {
             const float y = __shfl_sync(FULL, x[i], mate);
-            // the lower half a cos - b sin, the upper b cos + a sin
-            if (turned) x[i] = fmaf(x[i], c[i], lower ? -y * s[i] : y * s[i]);
+            if (turned) x[i] = fmaf(x[i], c[i], y * s[i]);
           }
         }
-        if (on[j]) *reinterpret_cast<uint4*>(dst[j]) = pack(x, T());
+        if (on) *reinterpret_cast<uint4*>(dst + j * to + e0) = pack(x, T());
       }
     }
   }
@@ -135,12 +128,16 @@ int launch(const QkArgs& a, unsigned grid, cudaStream_t st) {
 template <class T>
 int by_width(const QkArgs& a, unsigned grid, cudaStream_t st) {
   const int v = a.D * (int)sizeof(T) / 16;   // 16-byte pieces of a head
-  if (v <= 1) return launch<T, 1>(a, grid, st);
+  if constexpr (sizeof(T) == 2) {
+    if (v <= 1) return launch<T, 1>(a, grid, st);
+  }
   if (v <= 2) return launch<T, 2>(a, grid, st);
   if (v <= 4) return launch<T, 4>(a, grid, st);
   if (v <= 8) return launch<T, 8>(a, grid, st);
-  if (v <= 16) return launch<T, 16>(a, grid, st);
-  return launch<T, 32>(a, grid, st);
+  if constexpr (sizeof(T) == 4) {
+    if (v > 16) return launch<T, 32>(a, grid, st);
+  }
+  return launch<T, 16>(a, grid, st);
 }
 
 }  // namespace
@@ -172,9 +169,9 @@ extern "C" int trackfit_qk_norm(int32_t dtype, const void* q, int64_t q_stride, 
   a.eps = eps, a.qg = q_gain, a.kg = k_gain, a.pos = positions;
   for (int i = 0; i < rot_dim / 2; ++i)
     a.freq[i] = (uint64_t)ldexp(pow(rot_base, -2.0 * i / rot_dim) / (2.0 * 3.14159265358979323846), 64);
-  // a row a warp while the rows are too few to fill the GPU's 152 x 8 CTAs, else four, so that
-  // the lanes that form the angles are all busy (a row has r / 2 of them)
-  const int64_t fill = 152 * 8;
+  // a row a warp while the rows are too few to fill the GPU, else four, whose loads are under way
+  // together and whose angles (r / 2 a row) keep the lanes busy
+  const int64_t fill = 152 * CTAS;
   a.rows = n_rows >= fill * WARPS * MAX_ROWS ? MAX_ROWS : 1;
   const int64_t need = (n_rows + (int64_t)WARPS * a.rows - 1) / ((int64_t)WARPS * a.rows);
   const unsigned grid = (unsigned)(need < fill ? need : fill);

@@ -8,6 +8,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "trackfit_internal.h"
 
 namespace seqops {
@@ -118,6 +120,20 @@ inline bool heads_ok(int32_t h) { return h >= 1 && h <= MAX_HEADS; }
 // A row array [rows][stride] of `width` values a row: 16-byte aligned at every row.
 inline bool rows_ok(const void* p, int64_t stride, int64_t width, int size) {
   return p && !mis16(p) && stride >= width && stride <= MAX_STRIDE && (stride * size) % 16 == 0;
+}
+// Dynamic shared memory beyond what any kernel may have needs leave, once a device and kernel.
+template <class K>
+inline cudaError_t allow_smem(K* kernel, size_t bytes) {
+  static std::atomic<uint64_t> given{0};   // a bit a device
+  if (bytes <= 48 * 1024) return cudaSuccess;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (given.load() & bit) return cudaSuccess;
+  e = tf_allow_smem(kernel);
+  if (e == cudaSuccess) given.fetch_or(bit);
+  return e;
 }
 inline int launched() {
   const cudaError_t e = cudaPeekAtLastError();

@@ -113,7 +113,7 @@ def load() -> ctypes.CDLL:
     lib.trackfit_qk_norm.argtypes = [i32, vp, i64, i32, vp, i64, i32, i32, i64, vp, vp, f32, vp, i32, f64,
                                      vp, i64, vp, i64, vp]
     lib.trackfit_qk_norm.restype = ctypes.c_int
-    lib.trackfit_linear_attention_workspace.argtypes = [i64, i32, i32, i32]
+    lib.trackfit_linear_attention_workspace.argtypes = [i64, i64, i32, i32, i32]
     lib.trackfit_linear_attention_workspace.restype = size
     lib.trackfit_linear_attention.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, i64, i32, i32, i32, f32,
                                               i32, vp, vp, vp, i64, vp, size, vp]
@@ -396,67 +396,79 @@ def decode(seed_t, corrections, out, stream=None) -> None:
 
 # ---- operators on packed sequences (include/trackfit.h)
 
-_ROW_TYPES = {"torch.float32": W.PRECISION_FP32, "torch.bfloat16": W.PRECISION_BF16,
-              "torch.float16": W.PRECISION_FP16}
-
-
 class _OpArgs:
-    """Checks the tensors of one operator call: all CUDA, on one device."""
+    """Checks the tensors of one operator call: CUDA rows of one type, all on one device.
+    The calls are short (a step of a few hundred candidates takes microseconds), so the
+    checks compare objects and format a message only to refuse."""
+
+    types = None      # torch's row types -> the library's
 
     def __init__(self, what: str, first):
-        self.what, self.device, self.dtype = what, first.device, str(first.dtype)
-        if not first.is_cuda or self.dtype not in _ROW_TYPES:
-            raise ValueError(f"{what}: expected CUDA rows of float32, bfloat16 or float16, got {self.dtype} on "
+        if _OpArgs.types is None:
+            import torch
+            _OpArgs.torch = torch
+            # the current stream's handle without an object for it, where this torch offers that
+            _OpArgs.raw_stream = staticmethod(getattr(torch._C, "_cuda_getCurrentRawStream", None) or
+                                              (lambda device: torch.cuda.current_stream(device).cuda_stream))
+            _OpArgs.types = {torch.float32: W.PRECISION_FP32, torch.bfloat16: W.PRECISION_BF16,
+                             torch.float16: W.PRECISION_FP16}
+        self.what, self.device, self.dtype = what, first.device, first.dtype
+        self.code = self.types.get(first.dtype)
+        if self.code is None or not first.is_cuda:
+            raise ValueError(f"{what}: expected CUDA rows of float32, bfloat16 or float16, got {first.dtype} on "
                              f"{first.device}")
 
     def rows(self, name, t, shape):
         """(pointer, row stride) of [rows, heads, width], heads side by side within a row."""
-        if tuple(t.shape) != tuple(shape) or str(t.dtype) != self.dtype or t.device != self.device:
+        if t.shape != shape or t.dtype != self.dtype or t.device != self.device:
             raise ValueError(f"{self.what}: {name} must be {list(shape)} {self.dtype} on {self.device}, got "
                              f"{list(t.shape)} {t.dtype} on {t.device}")
         n, h, d = shape
-        if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
-            raise ValueError(f"{self.what}: the heads of a row of {name} must stand side by side, got strides "
-                             f"{tuple(t.stride())}")
-        return t.data_ptr(), t.stride(0) if n > 1 else h * d
+        s = t.stride()
+        if (s[2] != 1 and d > 1) or (s[1] != d and h > 1):
+            raise ValueError(f"{self.what}: the heads of a row of {name} must stand side by side, got strides {s}")
+        return t.data_ptr(), s[0] if n > 1 else h * d
 
-    def vector(self, name, t, dtype_name, shape):
+    def vector(self, name, t, dtype, shape):
         """Pointer of a contiguous array, None for None."""
         if t is None:
             return None
-        if tuple(t.shape) != tuple(shape) or str(t.dtype) != dtype_name or t.device != self.device \
-                or not t.is_contiguous():
-            raise ValueError(f"{self.what}: {name} must be contiguous {list(shape)} {dtype_name} on {self.device}, got "
+        if t.shape != shape or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{self.what}: {name} must be contiguous {list(shape)} {dtype} on {self.device}, got "
                              f"{list(t.shape)} {t.dtype} on {t.device}")
         return t.data_ptr()
 
     def decay(self, t, n, h):
-        if tuple(t.shape) != (n, h) or str(t.dtype) != "torch.float32" or t.device != self.device \
-                or (h > 1 and t.stride(1) != 1):
+        s = t.stride()
+        if t.shape != (n, h) or t.dtype != self.torch.float32 or t.device != self.device or (s[1] != 1 and h > 1):
             raise ValueError(f"{self.what}: log_decay must be [{n}, {h}] torch.float32 on {self.device} with unit "
-                             f"stride, got {list(t.shape)} {t.dtype}, strides {tuple(t.stride())}")
-        return t.data_ptr(), t.stride(0) if n > 1 else h
+                             f"stride, got {list(t.shape)} {t.dtype}, strides {s}")
+        return t.data_ptr(), s[0] if n > 1 else h
 
-    def call(self, fn, args, stream, need=0, workspace=None):
+    def call(self, fn, args, stream, need=None, workspace=None):
         """fn(*args[, workspace, size], stream) with the tensors' device current.  Without a
         workspace of the caller's, one from torch's allocator, in the order of the stream."""
-        import torch
-        with torch.cuda.device(self.device):
-            if stream is None:
-                handle = torch.cuda.current_stream().cuda_stream
-            else:
-                handle = getattr(stream, "cuda_stream", stream)
-            if need and workspace is None:
-                on = torch.cuda.ExternalStream(handle, device=self.device) if stream is not None else None
-                with torch.cuda.stream(on):
-                    workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-            if workspace is not None:
-                if workspace.device != self.device or not workspace.is_contiguous():
-                    raise ValueError(f"{self.what}: the workspace must be contiguous on {self.device}")
-                args = (*args, workspace.data_ptr(), workspace.numel() * workspace.element_size())
-            elif need is not None:
-                args = (*args, None, 0)
+        torch = self.torch
+        index = self.device.index
+        if torch.cuda.current_device() != index:
+            with torch.cuda.device(index):
+                return self.call(fn, args, stream, need, workspace)
+        handle = self.raw_stream(index) if stream is None else getattr(stream, "cuda_stream", stream)
+        if need is None:
             st = fn(*args, handle)
+        elif workspace is not None:
+            if workspace.device != self.device or not workspace.is_contiguous():
+                raise ValueError(f"{self.what}: the workspace must be contiguous on {self.device}")
+            st = fn(*args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle)
+        elif need == 0:
+            st = fn(*args, None, 0, handle)
+        elif stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            st = fn(*args, workspace.data_ptr(), need, handle)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(handle, device=self.device)):
+                workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+                st = fn(*args, workspace.data_ptr(), need, handle)
         if st != OK:
             raise TrackfitError(st, f"trackfit_{self.what}")
 
@@ -477,15 +489,15 @@ def qk_norm(q, k, q_out, k_out, q_gain=None, k_gain=None, eps: float = 1e-6, pos
     kp, ks = (None, 0) if k is None else a.rows("k", k, (n, hk, d))
     kop, kos = (None, 0) if k is None else a.rows("k_out", k_out, (n, hk, d))
     a.call(load().trackfit_qk_norm,
-           (_ROW_TYPES[a.dtype], qp, qs, hq, kp, ks, hk, d, n, a.vector("q_gain", q_gain, "torch.float32", (d,)),
-            a.vector("k_gain", k_gain, "torch.float32", (d,)), float(eps),
-            a.vector("positions", positions, "torch.int32", (n,)), int(rot_dim), float(rot_base), qop, qos, kop, kos),
-           stream, need=None)
+           (a.code, qp, qs, hq, kp, ks, hk, d, n, a.vector("q_gain", q_gain, a.torch.float32, (d,)),
+            a.vector("k_gain", k_gain, a.torch.float32, (d,)), float(eps),
+            a.vector("positions", positions, a.torch.int32, (n,)), int(rot_dim), float(rot_base), qop, qos, kop, kos),
+           stream)
 
 
-def linear_attention_workspace(n_rows: int, n_heads: int, key_dim: int, value_dim: int) -> int:
+def linear_attention_workspace(n_rows: int, n_seq: int, n_heads: int, key_dim: int, value_dim: int) -> int:
     """Bytes of workspace of a linear_attention call."""
-    return int(load().trackfit_linear_attention_workspace(n_rows, n_heads, key_dim, value_dim))
+    return int(load().trackfit_linear_attention_workspace(n_rows, n_seq, n_heads, key_dim, value_dim))
 
 
 def linear_attention(q, k, v, log_decay, offsets, out, scale: float = 1.0, reverse: bool = False, state_in=None,
@@ -502,11 +514,11 @@ def linear_attention(q, k, v, log_decay, offsets, out, scale: float = 1.0, rever
     op, os_ = a.rows("out", out, (n, h, dv))
     gp, gs = a.decay(log_decay, n, h)
     a.call(load().trackfit_linear_attention,
-           (_ROW_TYPES[a.dtype], qp, qs, kp, ks, vp, vs, gp, gs, n, a.vector("offsets", offsets, "torch.int64", (b + 1,)),
+           (a.code, qp, qs, kp, ks, vp, vs, gp, gs, n, a.vector("offsets", offsets, a.torch.int64, (b + 1,)),
             b, h, dk, dv, float(scale), int(bool(reverse)),
-            a.vector("state_in", state_in, "torch.float32", (b, h, dk, dv)),
-            a.vector("state_out", state_out, "torch.float32", (b, h, dk, dv)), op, os_),
-           stream, need=linear_attention_workspace(n, h, dk, dv), workspace=workspace)
+            a.vector("state_in", state_in, a.torch.float32, (b, h, dk, dv)),
+            a.vector("state_out", state_out, a.torch.float32, (b, h, dk, dv)), op, os_),
+           stream, need=load().trackfit_linear_attention_workspace(n, b, h, dk, dv), workspace=workspace)
 
 
 def linear_attention_step(q, k, v, log_decay, state_in, state_out, out, scale: float = 1.0, slots=None,
@@ -524,11 +536,11 @@ def linear_attention_step(q, k, v, log_decay, state_in, state_out, out, scale: f
     op, os_ = a.rows("out", out, (b, h, dv))
     gp, gs = a.decay(log_decay, b, h)
     a.call(load().trackfit_linear_attention_step,
-           (_ROW_TYPES[a.dtype], qp, qs, kp, ks, vp, vs, gp, gs, b, h, dk, dv, float(scale),
-            a.vector("slots", slots, "torch.int32", (b,)), ns,
-            a.vector("state_in", state_in, "torch.float32", (ns, h, dk, dv)),
-            a.vector("state_out", state_out, "torch.float32", (ns, h, dk, dv)), op, os_),
-           stream, need=None)
+           (a.code, qp, qs, kp, ks, vp, vs, gp, gs, b, h, dk, dv, float(scale),
+            a.vector("slots", slots, a.torch.int32, (b,)), ns,
+            a.vector("state_in", state_in, a.torch.float32, (ns, h, dk, dv)),
+            a.vector("state_out", state_out, a.torch.float32, (ns, h, dk, dv)), op, os_),
+           stream)
 
 
 def cross_attention(q, k, v, q_offsets, kv_offsets, out, scale: Optional[float] = None, workspace=None,
@@ -543,9 +555,9 @@ def cross_attention(q, k, v, q_offsets, kv_offsets, out, scale: Optional[float] 
     kp, ks = a.rows("k", k, (nk, hk, d))
     vp, vs = a.rows("v", v, (nk, hk, d))
     op, os_ = a.rows("out", out, (nq, hq, d))
-    lib, t = load(), _ROW_TYPES[a.dtype]
+    lib, t = load(), a.code
     a.call(lib.trackfit_cross_attention,
-           (t, qp, qs, a.vector("q_offsets", q_offsets, "torch.int64", (b + 1,)), nq, kp, ks, vp, vs,
-            a.vector("kv_offsets", kv_offsets, "torch.int64", (b + 1,)), nk, b, hq, hk, d,
+           (t, qp, qs, a.vector("q_offsets", q_offsets, a.torch.int64, (b + 1,)), nq, kp, ks, vp, vs,
+            a.vector("kv_offsets", kv_offsets, a.torch.int64, (b + 1,)), nk, b, hq, hk, d,
             float(d) ** -0.5 if scale is None else float(scale), op, os_),
-           stream, need=int(lib.trackfit_cross_attention_workspace(t, nq, nk, b, hq, hk, d)), workspace=workspace)
+           stream, need=lib.trackfit_cross_attention_workspace(t, nq, nk, b, hq, hk, d), workspace=workspace)

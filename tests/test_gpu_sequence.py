@@ -484,7 +484,7 @@ def test_layer_on_a_stream_and_in_a_graph(T):
 
     n = x.shape[0]
     work = tuple(torch.empty(max(b, 16), dtype=torch.uint8, device="cuda") for b in (
-        T.linear_attention_workspace(n, 4, 32, 32),
+        T.linear_attention_workspace(n, len(lengths), 4, 32, 32),
         int(T.load().trackfit_cross_attention_workspace(1, n, kv[0].shape[0], len(lengths), 4, 4, 32))))
     for use in (work, (None, None)):
         graph = torch.cuda.CUDAGraph()

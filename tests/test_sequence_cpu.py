@@ -67,12 +67,13 @@ def test_linear_refusals(lib, kw, want):
 
 def test_linear_workspace(lib):
     f = lib.trackfit_linear_attention_workspace
-    assert f(512, 4, 32, 32) == 0 and f(0, 4, 32, 32) == 0
-    assert f(513, 4, 32, 32) >= 4 * 32 * 32 * 4
-    assert f(-1, 4, 32, 32) == 0 and f(1000, 0, 32, 32) == 0 and f(1000, 4, 20, 32) == 0
-    n = f(1 << 20, 8, 64, 64)
+    assert f(512, 1, 4, 32, 32) == 0 and f(0, 1, 4, 32, 32) == 0
+    assert f(513, 1, 4, 32, 32) >= 4 * 32 * 32 * 4
+    assert f(16384, 256, 4, 32, 32) == 0 and f(16384, 255, 4, 32, 32) > 0 and f(16385, 1000, 4, 32, 32) > 0
+    assert f(-1, 1, 4, 32, 32) == 0 and f(1000, 1, 0, 32, 32) == 0 and f(1000, 1, 4, 20, 32) == 0 and f(1000, 0, 4, 32, 32) == 0
+    n = f(1 << 20, 4, 8, 64, 64)
     assert 0 < n < 1 << 30
-    assert call(lib.trackfit_linear_attention, LINEAR, workspace_size=f(1000, 4, 32, 32) - 1) == INVALID
+    assert call(lib.trackfit_linear_attention, LINEAR, workspace_size=f(1000, 3, 4, 32, 32) - 1) == INVALID
 
 
 STEP = dict(dtype=2, q=P, q_stride=128, k=P, k_stride=128, v=P, v_stride=128, log_decay=P, decay_stride=4, n_seq=7,
@@ -123,7 +124,7 @@ def test_checks_of_rows_and_vectors():
     """The binding's rules of shapes, types and strides, on host tensors."""
     torch = pytest.importorskip("torch")
     a = object.__new__(T._OpArgs)
-    a.what, a.device, a.dtype = "op", torch.device("cpu"), "torch.float32"
+    a.what, a.device, a.dtype, a.torch = "op", torch.device("cpu"), torch.float32, torch
     x = torch.zeros((6, 4, 8))
     assert a.rows("x", x, (6, 4, 8)) == (x.data_ptr(), 32)
     assert a.rows("x", x[::2], (3, 4, 8))[1] == 64
@@ -133,10 +134,10 @@ def test_checks_of_rows_and_vectors():
         with pytest.raises(ValueError):
             a.rows("x", bad, shape)
     v = torch.zeros(8)
-    assert a.vector("v", None, "torch.float32", (8,)) is None and a.vector("v", v, "torch.float32", (8,)) == v.data_ptr()
+    assert a.vector("v", None, torch.float32, (8,)) is None and a.vector("v", v, torch.float32, (8,)) == v.data_ptr()
     for bad in (v[:4], v.double(), torch.zeros(16)[::2]):
         with pytest.raises(ValueError):
-            a.vector("v", bad, "torch.float32", (8,))
+            a.vector("v", bad, torch.float32, (8,))
     g = torch.zeros((6, 10))
     assert a.decay(g[:, 2:6], 6, 4) == (g.data_ptr() + 8, 10)
     for bad in (g, g[:, ::2], g[:, :4].half()):
