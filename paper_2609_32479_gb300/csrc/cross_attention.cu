@@ -13,59 +13,6 @@ using namespace seqops;
 constexpr int NW = 4;
 constexpr int64_t MOST_ROWS = 0x7fffff00;   // of the products, and of states: counted in 32 bits
 
-// fp32: a warp takes one row of one head: the lanes take a state each for the products with
-// the query, then D / 32 channels each for the sum of the values.
-__global__ void __launch_bounds__(NW * 32) ca_simt_kernel(const __grid_constant__ CaArgs a, float scale2) {
-  __shared__ float sq[NW][MAX_DIM];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t unit = (int64_t)blockIdx.x * NW + warp;
-  const int h = (int)(unit % a.Hq);
-  const int64_t row = unit / a.Hq;
-  if (row >= a.nq) return;
-  const int64_t b = first_at_least(a.qo, a.n_seq, row + 1, lane) - 1;
-  if (b < 0 || !(row < a.qo[b + 1])) return;      // a row of no sequence
-  const int64_t lo = clamp64(a.ko[b], 0, a.nk), hi = clamp64(a.ko[b + 1], lo, a.nk);
-  const float* q = (const float*)a.q + row * a.qs + h * a.D;
-  const float* k = (const float*)a.k + h / a.G * a.D;
-  const float* v = (const float*)a.v + h / a.G * a.D;
-  for (int i = lane; i < a.D; i += 32) sq[warp][i] = q[i] * scale2;
-  __syncwarp();
-  float m = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int64_t j0 = lo; j0 < hi; j0 += 32) {
-    const int64_t j = j0 + lane;
-    float s = -INFINITY;
-    if (j < hi) {
-      s = 0.0f;
-      for (int i = 0; i < a.D; ++i) s = fmaf(sq[warp][i], k[j * a.ks + i], s);
-    }
-    float mx = s;
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, x));
-    const float mn = fmaxf(m, mx);
-    const float base = mn == -INFINITY ? 0.0f : mn;
-    const float f = exp2f(m - base);
-    const float p = exp2f(s - base);
-    float sum = p;
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(FULL, sum, x);
-    l = fmaf(l, f, sum);
-    m = mn;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) o[c] *= f;
-    const int n = hi - j0 < 32 ? (int)(hi - j0) : 32;
-    for (int jj = 0; jj < n; ++jj) {
-      const float pj = __shfl_sync(FULL, p, jj);
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.D) o[c] = fmaf(pj, v[(j0 + jj) * a.vs + lane + 32 * c], o[c]);
-    }
-  }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // nothing to read, or scores of -inf only: zeros
-#pragma unroll
-  for (int c = 0; c < 4; ++c)
-    if (lane + 32 * c < a.D) ((float*)a.out)[row * a.os + h * a.D + lane + 32 * c] = o[c] * inv;
-}
-
 // The parts of each row's range joined: a warp a row and head of the states.
 template <class T>
 __global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant__ CaArgs a) {
@@ -103,8 +50,8 @@ __global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant_
 
 // Parts of each row's range: as many as give 152 x 12 warps something to do, not under 256
 // states each on average, and at most the 32 that the joining warp has lanes for.
-int splits_of(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk) {
-  if (dtype == TRACKFIT_FP32 || nq <= 0 || n_seq <= 0) return 1;
+int splits_of(int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk) {
+  if (nq <= 0 || n_seq <= 0) return 1;
   const int64_t units = (nq * (Hq / Hk) + 15) / 16 * Hk;
   const int64_t most = nk / n_seq / 256;
   int64_t s = 152 * 12 / units;
@@ -119,7 +66,7 @@ extern "C" size_t trackfit_cross_attention_workspace(int32_t dtype, int64_t n_q_
   if (!type_ok(dtype) || n_q_rows < 0 || n_kv_rows < 0 || n_seq < 0 || !heads_ok(q_heads) || !heads_ok(kv_heads) ||
       q_heads % kv_heads != 0 || !dim_ok(head_dim) || n_q_rows > MOST_ROWS / (q_heads / kv_heads) || n_kv_rows > MOST_ROWS)
     return 0;
-  const int s = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
+  const int s = splits_of(n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
   return s > 1 ? (size_t)s * n_q_rows * q_heads * (head_dim + 2) * 4 : 0;
 }
 
@@ -153,21 +100,18 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
   a.qo = q_offsets, a.ko = kv_offsets, a.nq = n_q_rows, a.nk = n_kv_rows, a.n_seq = n_seq;
   a.Hq = q_heads, a.Hk = kv_heads, a.G = q_heads / kv_heads, a.D = head_dim;
   a.scale2 = scale == 0.0f ? 1.0f : fabsf(scale) * LOG2E;
-  a.q_and = scale == 0.0f ? 0u : ~0u, a.q_xor = scale < 0.0f ? 0x80008000u : 0u;
-  a.splits = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
+  a.q_and = scale == 0.0f ? 0u : ~0u, a.q_xor = scale < 0.0f ? (dtype == TRACKFIT_FP32 ? 0x80000000u : 0x80008000u) : 0u;
+  a.splits = splits_of(n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
+  // all heads of a tile where that leaves ten tiles for each of the 152 x 16 warps
+  a.each = (n_q_rows * a.G + 15) / 16 >= 10 * 152 * 16 ? kv_heads : 1;
   a.ws_o = static_cast<float*>(workspace);
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (need > 0 ? (int64_t)a.splits * n_q_rows * q_heads * head_dim : 0));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const int64_t warps = n_q_rows * q_heads;       // of the kernels that take a row and head
-  if ((warps + NW - 1) / NW > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
-  const unsigned grid = (unsigned)((warps + NW - 1) / NW);
-  if (dtype == TRACKFIT_FP32) {
-    ca_simt_kernel<<<grid, NW * 32, 0, st>>>(a, scale * LOG2E);
-    return launched();
-  }
-  const int rc = cross_mma(dtype, a, st);
+  const int rc = dtype == TRACKFIT_FP32 ? cross_tf32(a, st) : cross_mma(dtype, a, st);
   if (rc != TRACKFIT_OK || a.splits == 1) return rc;
-  if (dtype == TRACKFIT_BF16_PROJ) ca_join_kernel<__nv_bfloat16><<<grid, NW * 32, 0, st>>>(a);
+  const unsigned grid = (unsigned)((n_q_rows * q_heads + NW - 1) / NW);   // (only few rows are split)
+  if (dtype == TRACKFIT_FP32) ca_join_kernel<float><<<grid, NW * 32, 0, st>>>(a);
+  else if (dtype == TRACKFIT_BF16_PROJ) ca_join_kernel<__nv_bfloat16><<<grid, NW * 32, 0, st>>>(a);
   else ca_join_kernel<__half><<<grid, NW * 32, 0, st>>>(a);
   return launched();
 }

@@ -21,7 +21,6 @@ namespace {
 using namespace seqops;
 
 constexpr int KC = 32;           // states of a chunk
-constexpr int FARTHEST = 0x7fffffff;
 
 template <int NG>
 constexpr __host__ __device__ int queue() { return NG == 4 ? 2 : 3; }
@@ -34,8 +33,10 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
   const int lane = threadIdx.x, g = lane >> 2, t = lane & 3;
   const int split = blockIdx.x % a.splits;
   const unsigned unit = blockIdx.x / a.splits;
-  const int hk = unit % a.Hk;
-  const int tile = unit / a.Hk;
+  // a warp takes `each` heads of the states, one after the other: the sequences of the tile's rows
+  // are looked for once
+  const int sets = a.Hk / a.each, first_head = unit % sets * a.each;
+  const int tile = unit / sets;
   const int rows = (int)a.nq * a.G;
   const uint32_t mine = smem_addr(smem) + lane * 16;
   if (a.D < NG * 32) {                                 // channels beyond D stay zero: the copies leave them alone
@@ -43,233 +44,216 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
       asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(mine + i * 512), "r"(0) : "memory");
   }
 
-  // the sequences of the tile's rows: lane l < 16 looks for row l's, lanes g and g + 8 are asked
-  const int row_l = tile * 16 + (lane & 15);
-  const int64_t ql = row_l < rows ? row_l / a.G : a.nq - 1;
-  int64_t b = 0;
-  {
-    const int64_t q0 = (int64_t)(tile * 16) / a.G;
-    int64_t first = first_at_least(a.qo, a.n_seq, q0 + 1, lane) - 1;   // the last that begins at or before q0
-    if (first < 0) first = 0;
-    // the following offsets, 32 at a time: how many are at or before the lane's query
-    b = first;
-    for (int64_t at = first + 1;; at += 32) {
-      const int64_t o = at + lane < a.n_seq ? a.qo[at + lane] : INT64_MAX;
-      int n = 0;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) n += __shfl_sync(FULL, o, i) <= ql;
-      b += n;
-      if (!__any_sync(FULL, n == 32)) break;
-    }
-  }
-  bool in = row_l < rows && a.qo[b] <= ql && ql < a.qo[b + 1];
-  int lo_l = 0, hi_l = 0;
-  if (in) {
-    const int64_t lo = clamp64(a.ko[b], 0, a.nk), hi = clamp64(a.ko[b + 1], lo, a.nk);
-    lo_l = (int)(lo + (hi - lo) * split / a.splits), hi_l = (int)(lo + (hi - lo) * (split + 1) / a.splits);
-  }
+  bool in;
+  int lo_l, hi_l;
+  find_rows(a, tile, split, lane, in, lo_l, hi_l);
   const int lo0 = __shfl_sync(FULL, lo_l, g), hi0 = __shfl_sync(FULL, hi_l, g);
   const int lo1 = __shfl_sync(FULL, lo_l, g + 8), hi1 = __shfl_sync(FULL, hi_l, g + 8);
   const bool in0 = __shfl_sync(FULL, (int)in, g), in1 = __shfl_sync(FULL, (int)in, g + 8);
   const int row0 = tile * 16 + g, row1 = row0 + 8;
   const int end = __reduce_max_sync(FULL, hi0 > hi1 ? hi0 : hi1);
-  // the first state from `pos` on that a row reads
-  auto wanted = [&](int pos) {
-    const int c0 = hi0 > pos && hi0 > lo0 ? (lo0 > pos ? lo0 : pos) : FARTHEST;
-    const int c1 = hi1 > pos && hi1 > lo1 ? (lo1 > pos ? lo1 : pos) : FARTHEST;
-    return __reduce_min_sync(FULL, c0 < c1 ? c0 : c1);
-  };
+  auto wanted = [&](int pos) { return first_wanted(pos, lo0, hi0, lo1, hi1); };
 
-  uint32_t q[NG][2][4];
-  {
-    const T* p0 = (const T*)a.q + (int64_t)(in0 ? row0 / a.G : 0) * a.qs + (hk * a.G + row0 % a.G) * a.D + 8 * t;
-    const T* p1 = (const T*)a.q + (int64_t)(in1 ? row1 / a.G : 0) * a.qs + (hk * a.G + row1 % a.G) * a.D + 8 * t;
+  for (int hk = first_head; hk < first_head + a.each; ++hk) {
+    uint32_t q[NG][2][4];
+    {
+      const T* p0 = (const T*)a.q + (int64_t)(in0 ? row0 / a.G : 0) * a.qs + (hk * a.G + row0 % a.G) * a.D + 8 * t;
+      const T* p1 = (const T*)a.q + (int64_t)(in1 ? row1 / a.G : 0) * a.qs + (hk * a.G + row1 % a.G) * a.D + 8 * t;
 #pragma unroll
-    for (int i = 0; i < NG; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if ((e ? in1 : in0) && 32 * i + 8 * t < a.D) u = *reinterpret_cast<const uint4*>((e ? p1 : p0) + 32 * i);
-        q[i][e][0] = (u.x & a.q_and) ^ a.q_xor, q[i][e][1] = (u.y & a.q_and) ^ a.q_xor;
-        q[i][e][2] = (u.z & a.q_and) ^ a.q_xor, q[i][e][3] = (u.w & a.q_and) ^ a.q_xor;
-      }
-  }
-  const int kb = (int)a.ks * 2, vb = (int)a.vs * 2;
-  const char* k0 = reinterpret_cast<const char*>((const T*)a.k + hk * a.D + 8 * t);
-  const char* v0 = reinterpret_cast<const char*>((const T*)a.v + hk * a.D + 8 * t);
-  int ahead = wanted(0);                               // the next chunk to fetch
-  int at[NST];                                         // first states of the chunks in the queue
-  auto issue = [&](int s) {
-    const int pos = ahead;
-    if (pos != FARTHEST) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = pos + 8 * r + g;
-        const bool on = row < end;
-        const char* kp = k0 + (int64_t)row * kb;
-        const char* vp = v0 + (int64_t)row * vb;
-#pragma unroll
-        for (int i = 0; i < NG; ++i)
-          if (32 * i + 8 * t < a.D) {
-            copy16(mine + s * SLOT + (4 * i + r) * 512, kp + 64 * i, on);
-            copy16(mine + s * SLOT + (4 * NG + 4 * i + r) * 512, vp + 64 * i, on);
-          }
-      }
-      ahead = wanted(pos + KC);
-    }
-    copy_commit();
-    return pos;
-  };
-#pragma unroll
-  for (int s = 0; s < NST; ++s) at[s] = issue(s);
-
-  float o[NG * 4][4];
-#pragma unroll
-  for (int n = 0; n < NG * 4; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
-  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;   // m: score * scale2
-  for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
-    const int pos = at[0];
-#pragma unroll
-    for (int i = 0; i + 1 < NST; ++i) at[i] = at[i + 1];
-    if (pos == FARTHEST) break;
-    copy_wait<NST - 1>();
-    const uint32_t slot = mine + s * SLOT;
-    float x[4][4];
-#pragma unroll
-    for (int i = 0; i < NG; ++i)
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        uint32_t k[4];
-        load_shared(k, slot + (4 * i + n) * 512);
-#pragma unroll
-        for (int w = 0; w < 4; w += 2) {
-          const uint32_t qa[4] = {q[i][0][w], q[i][1][w], q[i][0][w + 1], q[i][1][w + 1]};
-          if (i == 0 && w == 0) mma16_new(x[n], qa, k[w], k[w + 1], T());
-          else mma16(x[n], qa, k[w], k[w + 1], T());
-        }
-      }
-    // states that are not a row's own count nothing
-    const bool whole0 = lo0 <= pos && pos + KC <= hi0, whole1 = lo1 <= pos && pos + KC <= hi1;
-    const bool whole = __all_sync(FULL, whole0 && whole1);
-    if (!whole) {
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
+      for (int i = 0; i < NG; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int j = pos + 8 * n + 2 * t + e;
-          if (j < lo0 || j >= hi0) x[n][e] = -INFINITY;
-          if (j < lo1 || j >= hi1) x[n][2 + e] = -INFINITY;
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if ((e ? in1 : in0) && 32 * i + 8 * t < a.D) u = *reinterpret_cast<const uint4*>((e ? p1 : p0) + 32 * i);
+          q[i][e][0] = (u.x & a.q_and) ^ a.q_xor, q[i][e][1] = (u.y & a.q_and) ^ a.q_xor;
+          q[i][e][2] = (u.z & a.q_and) ^ a.q_xor, q[i][e][3] = (u.w & a.q_and) ^ a.q_xor;
         }
     }
-    float t0 = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1])), fmaxf(fmaxf(x[2][0], x[2][1]), fmaxf(x[3][0], x[3][1])));
-    float t1 = fmaxf(fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3])), fmaxf(fmaxf(x[2][2], x[2][3]), fmaxf(x[3][2], x[3][3])));
+    const int kb = (int)a.ks * 2, vb = (int)a.vs * 2;
+    const char* k0 = reinterpret_cast<const char*>((const T*)a.k + hk * a.D + 8 * t);
+    const char* v0 = reinterpret_cast<const char*>((const T*)a.v + hk * a.D + 8 * t);
+    int ahead = wanted(0);                               // the next chunk to fetch
+    int at[NST];                                         // first states of the chunks in the queue
+    auto issue = [&](int s) {
+      const int pos = ahead;
+      if (pos != FARTHEST) {
 #pragma unroll
-    for (int y = 1; y <= 2; y <<= 1) {
-      t0 = fmaxf(t0, __shfl_xor_sync(FULL, t0, y));
-      t1 = fmaxf(t1, __shfl_xor_sync(FULL, t1, y));
-    }
-    t0 = fmaxf(m0, t0 * a.scale2), t1 = fmaxf(m1, t1 * a.scale2);
-    const float n0 = t0 == -INFINITY ? 0.0f : t0, n1 = t1 == -INFINITY ? 0.0f : t1;
-    if (__any_sync(FULL, t0 != m0 || t1 != m1)) {
-      const float f0 = ex2(m0 - n0), f1 = ex2(m1 - n1);
-      l0 *= f0, l1 *= f1;
+        for (int r = 0; r < 4; ++r) {
+          const int row = pos + 8 * r + g;
+          const bool on = row < end;
+          const char* kp = k0 + (int64_t)row * kb;
+          const char* vp = v0 + (int64_t)row * vb;
 #pragma unroll
-      for (int n = 0; n < NG * 4; ++n) o[n][0] *= f0, o[n][1] *= f0, o[n][2] *= f1, o[n][3] *= f1;
-      m0 = t0, m1 = t1;
-    }
+          for (int i = 0; i < NG; ++i)
+            if (32 * i + 8 * t < a.D) {
+              copy16(mine + s * SLOT + (4 * i + r) * 512, kp + 64 * i, on);
+              copy16(mine + s * SLOT + (4 * NG + 4 * i + r) * 512, vp + 64 * i, on);
+            }
+        }
+        ahead = wanted(pos + KC);
+      }
+      copy_commit();
+      return pos;
+    };
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      x[n][0] = ex2(fmaf(x[n][0], a.scale2, -n0)), x[n][1] = ex2(fmaf(x[n][1], a.scale2, -n0));
-      x[n][2] = ex2(fmaf(x[n][2], a.scale2, -n1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, -n1));
-      l0 += x[n][0] + x[n][1], l1 += x[n][2] + x[n][3];
-    }
-    uint32_t pa[2][4];
+    for (int s = 0; s < NST; ++s) at[s] = issue(s);
+
+    float o[NG * 4][4];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      pa[e][0] = pack2(x[2 * e][0], x[2 * e][1], T()), pa[e][1] = pack2(x[2 * e][2], x[2 * e][3], T());
-      pa[e][2] = pack2(x[2 * e + 1][0], x[2 * e + 1][1], T()), pa[e][3] = pack2(x[2 * e + 1][2], x[2 * e + 1][3], T());
-    }
+    for (int n = 0; n < NG * 4; ++n)
 #pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      uint32_t v[4][4], sum = 0u;
+      for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;   // m: score * scale2
+    for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
+      const int pos = at[0];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) load_shared(v[r], slot + (4 * NG + 4 * i + r) * 512);
-      bool mixed = false;
+      for (int i = 0; i + 1 < NST; ++i) at[i] = at[i + 1];
+      if (pos == FARTHEST) break;
+      copy_wait<NST - 1>();
+      const uint32_t slot = mine + s * SLOT;
+      // nothing in the chunk's upper half (looked at for narrow heads, whose chunks of a track are
+      // short; the branches cost the wide ones a fifth)
+      const bool lower = NG == 1 && pos + 16 >= end;
+      float x[4][4];
+#pragma unroll
+      for (int i = 0; i < NG; ++i)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          if (n >= 2 && lower) {
+            if (i == 0) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.0f;
+            continue;
+          }
+          uint32_t k[4];
+          load_shared(k, slot + (4 * i + n) * 512);
+#pragma unroll
+          for (int w = 0; w < 4; w += 2) {
+            const uint32_t qa[4] = {q[i][0][w], q[i][1][w], q[i][0][w + 1], q[i][1][w + 1]};
+            if (i == 0 && w == 0) mma16_new(x[n], qa, k[w], k[w + 1], T());
+            else mma16(x[n], qa, k[w], k[w + 1], T());
+          }
+        }
+      // states that are not a row's own count nothing
+      const bool whole0 = lo0 <= pos && pos + KC <= hi0, whole1 = lo1 <= pos && pos + KC <= hi1;
+      const bool whole = __all_sync(FULL, whole0 && whole1);
       if (!whole) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int n = 0; n < 4; ++n)
 #pragma unroll
-          for (int w = 0; w < 4; ++w) sum = zero_if_finite(v[r][w], sum, T());
-        mixed = __any_sync(FULL, (sum & 0x7fff7fffu) != 0u);
+          for (int e = 0; e < 2; ++e) {
+            const int j = pos + 8 * n + 2 * t + e;
+            if (j < lo0 || j >= hi0) x[n][e] = -INFINITY;
+            if (j < lo1 || j >= hi1) x[n][2 + e] = -INFINITY;
+          }
       }
-      if (!mixed) {
+      float t0 = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1])), fmaxf(fmaxf(x[2][0], x[2][1]), fmaxf(x[3][0], x[3][1])));
+      float t1 = fmaxf(fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3])), fmaxf(fmaxf(x[2][2], x[2][3]), fmaxf(x[3][2], x[3][3])));
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
+      for (int y = 1; y <= 2; y <<= 1) {
+        t0 = fmaxf(t0, __shfl_xor_sync(FULL, t0, y));
+        t1 = fmaxf(t1, __shfl_xor_sync(FULL, t1, y));
+      }
+      t0 = fmaxf(m0, t0 * a.scale2), t1 = fmaxf(m1, t1 * a.scale2);
+      const float n0 = t0 == -INFINITY ? 0.0f : t0, n1 = t1 == -INFINITY ? 0.0f : t1;
+      if (__any_sync(FULL, t0 != m0 || t1 != m1)) {
+        const float f0 = ex2(m0 - n0), f1 = ex2(m1 - n1);
+        l0 *= f0, l1 *= f1;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) mma16(o[4 * i + w], pa[e], turned(v[2 * e][w]), turned(v[2 * e + 1][w]), T());
-      } else {
-        for (int r = 0; r < 16; ++r) {
-          const int rl = __shfl_sync(FULL, lo_l, r) - pos, rh = __shfl_sync(FULL, hi_l, r) - pos;
+        for (int n = 0; n < NG * 4; ++n) o[n][0] *= f0, o[n][1] *= f0, o[n][2] *= f1, o[n][3] *= f1;
+        m0 = t0, m1 = t1;
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        x[n][0] = ex2(fmaf(x[n][0], a.scale2, -n0)), x[n][1] = ex2(fmaf(x[n][1], a.scale2, -n0));
+        x[n][2] = ex2(fmaf(x[n][2], a.scale2, -n1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, -n1));
+        l0 += x[n][0] + x[n][1], l1 += x[n][2] + x[n][3];
+      }
+      uint32_t pa[2][4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        pa[e][0] = pack2(x[2 * e][0], x[2 * e][1], T()), pa[e][1] = pack2(x[2 * e][2], x[2 * e][3], T());
+        pa[e][2] = pack2(x[2 * e + 1][0], x[2 * e + 1][1], T()), pa[e][3] = pack2(x[2 * e + 1][2], x[2 * e + 1][3], T());
+      }
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        uint32_t v[4][4], sum = 0u;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) load_shared(v[r], slot + (4 * NG + 4 * i + r) * 512);
+        bool mixed = false;
+        if (!whole) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sum = zero_if_finite(v[r][w], sum, T());
+          mixed = __any_sync(FULL, (sum & 0x7fff7fffu) != 0u);
+        }
+        if (!mixed) {
 #pragma unroll
           for (int w = 0; w < 4; ++w)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              uint32_t u[2];
+            for (int e = 0; e < 2; ++e)
+            if (e == 0 || !lower) mma16(o[4 * i + w], pa[e], turned(v[2 * e][w]), turned(v[2 * e + 1][w]), T());
+        } else {
+          for (int r = 0; r < 16; ++r) {
+            const int rl = __shfl_sync(FULL, lo_l, r) - pos, rh = __shfl_sync(FULL, hi_l, r) - pos;
 #pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const int j = 16 * e + 8 * c + 2 * t;
-                u[c] = turned(v[2 * e + c][w]) & ((j >= rl && j < rh ? 0xffffu : 0u) | (j + 1 >= rl && j + 1 < rh ? 0xffff0000u : 0u));
+            for (int w = 0; w < 4; ++w)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                uint32_t u[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                  const int j = 16 * e + 8 * c + 2 * t;
+                  u[c] = turned(v[2 * e + c][w]) & ((j >= rl && j < rh ? 0xffffu : 0u) | (j + 1 >= rl && j + 1 < rh ? 0xffff0000u : 0u));
+                }
+                float d[4];
+                mma16_new(d, pa[e], u[0], u[1], T());
+                if (g == r) o[4 * i + w][0] += d[0], o[4 * i + w][1] += d[1];
+                if (g + 8 == r) o[4 * i + w][2] += d[2], o[4 * i + w][3] += d[3];
               }
-              float d[4];
-              mma16_new(d, pa[e], u[0], u[1], T());
-              if (g == r) o[4 * i + w][0] += d[0], o[4 * i + w][1] += d[1];
-              if (g + 8 == r) o[4 * i + w][2] += d[2], o[4 * i + w][3] += d[3];
-            }
+          }
         }
       }
+      __syncwarp();                                      // read: the place is free
+      at[NST - 1] = issue(s);
     }
-    __syncwarp();                                      // read: the place is free
-    at[NST - 1] = issue(s);
-  }
 #pragma unroll
-  for (int y = 1; y <= 2; y <<= 1) {
-    l0 += __shfl_xor_sync(FULL, l0, y);
-    l1 += __shfl_xor_sync(FULL, l1, y);
-  }
-  if (a.splits == 1) {
-    const float f0 = l0 == 0.0f ? 0.0f : 1.0f / l0, f1 = l1 == 0.0f ? 0.0f : 1.0f / l1;
-    T* p0 = (T*)a.out + (int64_t)(row0 / a.G) * a.os + (hk * a.G + row0 % a.G) * a.D + 8 * t;
-    T* p1 = (T*)a.out + (int64_t)(row1 / a.G) * a.os + (hk * a.G + row1 % a.G) * a.D + 8 * t;
+    for (int y = 1; y <= 2; y <<= 1) {
+      l0 += __shfl_xor_sync(FULL, l0, y);
+      l1 += __shfl_xor_sync(FULL, l1, y);
+    }
+    if (a.splits == 1) {
+      const float f0 = l0 == 0.0f ? 0.0f : 1.0f / l0, f1 = l1 == 0.0f ? 0.0f : 1.0f / l1;
+      T* p0 = (T*)a.out + (int64_t)(row0 / a.G) * a.os + (hk * a.G + row0 % a.G) * a.D + 8 * t;
+      T* p1 = (T*)a.out + (int64_t)(row1 / a.G) * a.os + (hk * a.G + row1 % a.G) * a.D + 8 * t;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        if (32 * i + 8 * t >= a.D) continue;
+        uint32_t w0[4], w1[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          w0[w] = pack2(o[4 * i + w][0] * f0, o[4 * i + w][1] * f0, T());
+          w1[w] = pack2(o[4 * i + w][2] * f1, o[4 * i + w][3] * f1, T());
+        }
+        if (in0) write_out(p0 + 32 * i, w0);
+        if (in1) write_out(p1 + 32 * i, w1);
+      }
+      continue;
+    }
+    const int64_t part = (int64_t)split * rows;
+    const int64_t r0 = (part + row0) * a.Hk + hk, r1 = (part + row1) * a.Hk + hk;
+    if (t == 0) {
+      if (in0) a.ws_ml[r0] = make_float2(m0, l0);
+      if (in1) a.ws_ml[r1] = make_float2(m1, l1);
+    }
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
       if (32 * i + 8 * t >= a.D) continue;
-      uint32_t w0[4], w1[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        w0[w] = pack2(o[4 * i + w][0] * f0, o[4 * i + w][1] * f0, T());
-        w1[w] = pack2(o[4 * i + w][2] * f1, o[4 * i + w][3] * f1, T());
+      for (int w = 0; w < 4; w += 2) {
+        const int c = 32 * i + 8 * t + 2 * w;
+        if (in0) *reinterpret_cast<float4*>(a.ws_o + r0 * a.D + c) = make_float4(o[4 * i + w][0], o[4 * i + w][1], o[4 * i + w + 1][0], o[4 * i + w + 1][1]);
+        if (in1) *reinterpret_cast<float4*>(a.ws_o + r1 * a.D + c) = make_float4(o[4 * i + w][2], o[4 * i + w][3], o[4 * i + w + 1][2], o[4 * i + w + 1][3]);
       }
-      if (in0) write_out(p0 + 32 * i, w0);
-      if (in1) write_out(p1 + 32 * i, w1);
-    }
-    return;
-  }
-  const int64_t part = (int64_t)split * rows;
-  const int64_t r0 = (part + row0) * a.Hk + hk, r1 = (part + row1) * a.Hk + hk;
-  if (t == 0) {
-    if (in0) a.ws_ml[r0] = make_float2(m0, l0);
-    if (in1) a.ws_ml[r1] = make_float2(m1, l1);
-  }
-#pragma unroll
-  for (int i = 0; i < NG; ++i) {
-    if (32 * i + 8 * t >= a.D) continue;
-#pragma unroll
-    for (int w = 0; w < 4; w += 2) {
-      const int c = 32 * i + 8 * t + 2 * w;
-      if (in0) *reinterpret_cast<float4*>(a.ws_o + r0 * a.D + c) = make_float4(o[4 * i + w][0], o[4 * i + w][1], o[4 * i + w + 1][0], o[4 * i + w + 1][1]);
-      if (in1) *reinterpret_cast<float4*>(a.ws_o + r1 * a.D + c) = make_float4(o[4 * i + w][2], o[4 * i + w][3], o[4 * i + w + 1][2], o[4 * i + w + 1][3]);
     }
   }
 }
@@ -280,7 +264,7 @@ int launch(const CaArgs& a, cudaStream_t st) {
   const size_t smem = queue<NG>() * NG * 8 * 512;
   const cudaError_t e = allow_smem(kern, smem);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  const int64_t units = (a.nq * a.G + 15) / 16 * a.Hk * a.splits;
+  const int64_t units = (a.nq * a.G + 15) / 16 * (a.Hk / a.each) * a.splits;
   if (units > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
   kern<<<(unsigned)units, 32, smem, st>>>(a);
   return launched();

@@ -19,13 +19,49 @@ struct CaArgs {
   int64_t nq, nk, n_seq;
   int Hq, Hk, G, D;
   float scale2;                  // |scale| * log2(e), or 1 with a scale of 0
-  uint32_t q_and, q_xor;         // on two 16-bit queries: zeroed with a scale of 0, negated below it
+  uint32_t q_and, q_xor;         // on queries (two of 16 bits): zeroed with a scale of 0, negated below it
   int splits;
+  int each;                      // heads of the states that a warp takes one after the other
   float* ws_o;                   // [splits][rows][Hk][D], sums not yet divided
   float2* ws_ml;                 // [splits][rows][Hk]: the largest score (base 2), the sum of weights
 };
 
-// cross_mma.cu: the 16-bit types on the tensor cores.
+constexpr int FARTHEST = 0x7fffffff;
+
+// The states that row (lane & 15) of a tile reads, [lo, hi), and whether it is a query of a
+// sequence at all.
+__device__ __forceinline__ void find_rows(const CaArgs& a, int tile, int split, int lane, bool& in, int& lo, int& hi) {
+  const int row = tile * 16 + (lane & 15);
+  const bool there = row < (int)(a.nq * a.G);
+  const int64_t q = there ? row / a.G : a.nq - 1;
+  int64_t b = first_at_least(a.qo, a.n_seq, (int64_t)(tile * 16) / a.G + 1, lane) - 1;   // the last that begins at
+  if (b < 0) b = 0;                                                                      // or before the first row
+  // the offsets that follow, 32 at a time: how many are at or before the row's query
+  for (int64_t at = b + 1;; at += 32) {
+    const int64_t o = at + lane < a.n_seq ? a.qo[at + lane] : INT64_MAX;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) n += __shfl_sync(FULL, o, i) <= q;
+    b += n;
+    if (!__any_sync(FULL, n == 32)) break;
+  }
+  in = there && a.qo[b] <= q && q < a.qo[b + 1];
+  lo = hi = 0;
+  if (in) {
+    const int64_t l = clamp64(a.ko[b], 0, a.nk), h = clamp64(a.ko[b + 1], l, a.nk);
+    lo = (int)(l + (h - l) * split / a.splits), hi = (int)(l + (h - l) * (split + 1) / a.splits);
+  }
+}
+
+// The first state from `pos` on that a row of the tile reads, by all lanes' two rows.
+__device__ __forceinline__ int first_wanted(int pos, int lo0, int hi0, int lo1, int hi1) {
+  const int c0 = hi0 > pos && hi0 > lo0 ? (lo0 > pos ? lo0 : pos) : FARTHEST;
+  const int c1 = hi1 > pos && hi1 > lo1 ? (lo1 > pos ? lo1 : pos) : FARTHEST;
+  return __reduce_min_sync(FULL, c0 < c1 ? c0 : c1);
+}
+
+// cross_mma.cu: the 16-bit types on the tensor cores; cross_tf32.cu: fp32, likewise.
 int cross_mma(int32_t dtype, const CaArgs& a, cudaStream_t st);
+int cross_tf32(const CaArgs& a, cudaStream_t st);
 
 }  // namespace seqops

@@ -12,10 +12,12 @@ namespace {
 using namespace seqops;
 
 // ---------------------------------------------------------------- fp32, on the CUDA cores
-// A lane holds a column of S: K values in registers.  The rows of q and k are the same for
-// all lanes and come from shared memory as broadcasts, 8 rows at a time through a ring that
-// the warp fills by asynchronous copies.
-constexpr int COLS = 32;         // channels of v that a warp takes
+// A lane holds half a column of S, K / 2 values in registers, two to a 64-bit word for the packed
+// fp32 instructions; the lanes l and l + 16 have a column's halves.  The rows of q and k are the
+// same for all columns and come from shared memory as broadcasts, 8 rows at a time through a ring
+// that the warp fills by asynchronous copies.  The multiply-adds bound it (three a value of the
+// state and row); whole columns a lane left half of the lanes idle at V = 48.
+constexpr int COLS = 16;         // channels of v that a warp takes
 constexpr int CH = 8, NST = 3;
 
 template <int DK>
@@ -25,6 +27,27 @@ struct __align__(16) SimtSlot {
   int row, seq, flags, pad;      // the chunk, its first row in the direction of the recurrence
 };
 enum { LEN = 0xff, FIRST = 0x100, LAST = 0x200, GOES_ON = 0x400, ENDS = 0x800, NONE = 0x1000 };
+
+__device__ __forceinline__ uint64_t both(float a, float b) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ float2 parts(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
 
 template <int DK, bool STATE_ONLY>
 __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaArgs a) {
@@ -37,6 +60,8 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   Slot* slots = reinterpret_cast<Slot*>(smem);
   const int c0 = sl * COLS, width = a.V - c0 < COLS ? a.V - c0 : COLS;
   const int dir = a.u.reverse ? -1 : 1;
+  constexpr int HALF = DK / 2;
+  const int col = lane & 15, part = lane >> 4, i0 = part * HALF;   // this lane's column, and its first key channel
   // channels beyond K and V are zeros from here on: the copies leave them alone
   for (uint32_t* p = reinterpret_cast<uint32_t*>(slots) + lane; p < reinterpret_cast<uint32_t*>(slots + NST); p += 32) *p = 0;
   __syncwarp();
@@ -46,7 +71,7 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   const float* k = (const float*)a.k + base * a.ks + h * a.K;
   const float* v = (const float*)a.v + base * a.vs + h * a.V + c0;
   const float* gr = a.g + base * a.gs + h;
-  float* out = (float*)a.out + base * a.os + h * a.V + c0 + lane;
+  float* out = (float*)a.out + base * a.os + h * a.V + c0 + col;
   TilePieces pieces(a.u, tile, lane, STATE_ONLY);
   Piece p;
   bool more;
@@ -94,9 +119,9 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   };
 
   for (int s = 0; s < NST; ++s) issue(slots[s]);
-  float S[DK];
+  uint64_t S[HALF / 2];
 #pragma unroll
-  for (int i = 0; i < DK; ++i) S[i] = 0.0f;
+  for (int i = 0; i < HALF / 2; ++i) S[i] = 0;
   float total = 0.0f;
   const int64_t KV = (int64_t)a.K * a.V;
   for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
@@ -111,32 +136,44 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
         st = STATE_ONLY ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
       else if (a.state_in)
         st = a.state_in + ((int64_t)seq * a.H + h) * KV;
-      st = st && lane < width ? st + c0 + lane : nullptr;
+      st = st && col < width ? st + i0 * a.V + c0 + col : nullptr;
 #pragma unroll
-      for (int i = 0; i < DK; ++i) S[i] = st && i < a.K ? st[(int64_t)i * a.V] : 0.0f;
+      for (int i = 0; i < HALF; i += 2)
+        S[i / 2] = st && i0 + i < a.K ? both(st[i * a.V], st[(i + 1) * a.V]) : 0;
     }
     for (int r = 0; r < len; ++r) {
-      const float e = expf(w.g[r]);
-      const float vr = w.v[r][lane];
+      const float e = expf(w.g[r]), x = w.v[r][col];
+      const uint64_t ee = both(e, e), xx = both(x, x);
       if (STATE_ONLY) total += w.g[r];
-      float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      uint64_t acc[2] = {0, 0};
 #pragma unroll
-      for (int i = 0; i < DK; i += 4) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          S[i + j] = fmaf(w.k[r][i + j], vr, e * S[i + j]);
-          if (!STATE_ONLY) acc[j] = fmaf(w.q[r][i + j], S[i + j], acc[j]);
+      for (int i = 0; i < HALF; i += 4) {
+        const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(&w.k[r][i0 + i]);
+        S[i / 2] = fma2(kk.x, xx, mul2(ee, S[i / 2]));
+        S[i / 2 + 1] = fma2(kk.y, xx, mul2(ee, S[i / 2 + 1]));
+        if (!STATE_ONLY) {
+          const ulonglong2 qq = *reinterpret_cast<const ulonglong2*>(&w.q[r][i0 + i]);
+          acc[0] = fma2(qq.x, S[i / 2], acc[0]);
+          acc[1] = fma2(qq.y, S[i / 2 + 1], acc[1]);
         }
       }
-      if (!STATE_ONLY && lane < width)
-        out[(int64_t)(row + dir * r) * a.os] = a.scale * ((acc[0] + acc[1]) + (acc[2] + acc[3]));
+      if (!STATE_ONLY) {
+        const float2 o0 = parts(acc[0]), o1 = parts(acc[1]);
+        float o = (o0.x + o0.y) + (o1.x + o1.y);
+        o += __shfl_xor_sync(FULL, o, 16);
+        if (part == 0 && col < width) out[(int64_t)(row + dir * r) * a.os] = a.scale * o;
+      }
     }
     if ((flags & LAST) && (STATE_ONLY || ((flags & ENDS) && a.state_out))) {
       float* st = STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV;
-      if (lane < width)
+      if (col < width)
 #pragma unroll
-        for (int i = 0; i < DK; ++i)
-          if (i < a.K) st[(int64_t)i * a.V + c0 + lane] = S[i];
+        for (int i = 0; i < HALF; i += 2)
+          if (i0 + i < a.K) {
+            const float2 s2 = parts(S[i / 2]);
+            float* d = st + (i0 + i) * a.V + c0 + col;
+            d[0] = s2.x, d[a.V] = s2.y;
+          }
       if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
     }
     __syncwarp();
@@ -188,6 +225,7 @@ __global__ void __launch_bounds__(CARRY_NT) la_carry_kernel(const __grid_constan
 // four rows are read, decayed, added to and written at a time.  The state's two crossings
 // of memory are nearly all of the traffic, and bound it.
 constexpr int NW = 4;            // warps of a CTA
+constexpr int STEP_COLS = 32;    // columns that a warp takes
 struct StepArgs {
   const void *q, *k, *v;
   const float* g;
@@ -208,7 +246,7 @@ __global__ void __launch_bounds__(NW * 32) la_step_kernel(const __grid_constant_
   const int sl = (int)(unit % a.slices), h = (int)(unit / a.slices % a.H);
   const int64_t b = unit / a.slices / a.H;
   if (b >= a.n) return;
-  const int c = sl * COLS + (lane & 7) * 4, r0 = lane >> 3;
+  const int c = sl * STEP_COLS + (lane & 7) * 4, r0 = lane >> 3;
   const bool on = c < a.V;
   T* out = (T*)a.out + b * a.os + h * a.V + c;
   const int64_t slot = a.slots ? a.slots[b] : b;
@@ -249,7 +287,7 @@ __global__ void __launch_bounds__(NW * 32) la_step_kernel(const __grid_constant_
 // Rows a boundary: as many as leave one unit for each of the 152 x 8 warps that the widest
 // kernels keep on the GPU, but not under 256 (a state is written and read twice a boundary).
 int rows_a_boundary(int64_t n_rows, int H, int V) {
-  const int64_t units_a_row = (int64_t)H * ((V + COLS - 1) / COLS);
+  const int64_t units_a_row = (int64_t)H * ((V + 31) / 32);
   const int64_t l = (n_rows * units_a_row / (152 * 8) + 255) / 256 * 256;
   return l < 256 ? 256 : l > 2048 ? 2048 : (int)l;
 }
@@ -382,7 +420,7 @@ extern "C" int trackfit_linear_attention_step(int32_t dtype, const void* q, int6
   a.q = q, a.k = k, a.v = v, a.g = log_decay, a.out = out;
   a.qs = q_stride, a.ks = k_stride, a.vs = v_stride, a.gs = decay_stride, a.os = out_stride;
   a.slots = slots, a.state_in = state_in, a.state_out = state_out, a.n = n_seq, a.n_slots = n_slots;
-  a.H = n_heads, a.K = key_dim, a.V = value_dim, a.slices = (value_dim + COLS - 1) / COLS, a.scale = scale;
+  a.H = n_heads, a.K = key_dim, a.V = value_dim, a.slices = (value_dim + STEP_COLS - 1) / STEP_COLS, a.scale = scale;
   const int64_t units = n_seq * n_heads * a.slices;
   if ((units + NW - 1) / NW > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
   const unsigned grid = (unsigned)((units + NW - 1) / NW);
