@@ -12,17 +12,16 @@ namespace {
 using namespace seqops;
 
 // ---------------------------------------------------------------- fp32, on the CUDA cores
-// A lane holds half a column of S, K / 2 values in registers, two to a 64-bit word for the packed
-// fp32 instructions; the lanes l and l + 16 have a column's halves.  The rows of q and k are the
-// same for all columns and come from shared memory as broadcasts, 8 rows at a time through a ring
-// that the warp fills by asynchronous copies.  The multiply-adds bound it (three a value of the
-// state and row); whole columns a lane left half of the lanes idle at V = 48.
-constexpr int COLS = 16;         // channels of v that a warp takes
+// A lane holds halves of CPL columns of S, K / 2 values each in registers, two to a 64-bit word for
+// the packed fp32 instructions; the lanes l and l + 16 have a column's halves.  The rows of q and
+// k are the same for all columns and come from shared memory as broadcasts, 8 rows at a time
+// through a ring that the warp fills by asynchronous copies.  Several columns a lane share what a
+// row costs whatever its columns (loads, exponential, addresses: 90 of 116 instructions with one).
 constexpr int CH = 8, NST = 3;
 
-template <int DK>
+template <int DK, int CPL>
 struct __align__(16) SimtSlot {
-  float q[CH][DK], k[CH][DK], v[CH][COLS];
+  float q[CH][DK], k[CH][DK], v[CH][16 * CPL];
   float g[CH];
   int row, seq, flags, pad;      // the chunk, its first row in the direction of the recurrence
 };
@@ -49,10 +48,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return d;
 }
 
-template <int DK, bool STATE_ONLY>
+template <int DK, int CPL, bool STATE_ONLY>
 __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  using Slot = SimtSlot<DK>;
+  using Slot = SimtSlot<DK, CPL>;
+  constexpr int COLS = 16 * CPL;
   const int lane = threadIdx.x;
   const unsigned unit = blockIdx.x;
   const int sl = (int)(unit % a.slices), h = (int)(unit / a.slices % a.H);
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   const int c0 = sl * COLS, width = a.V - c0 < COLS ? a.V - c0 : COLS;
   const int dir = a.u.reverse ? -1 : 1;
   constexpr int HALF = DK / 2;
-  const int col = lane & 15, part = lane >> 4, i0 = part * HALF;   // this lane's column, and its first key channel
+  const int col = lane & 15, part = lane >> 4, i0 = part * HALF;   // this lane's columns: col + 16 j; first key channel
   // channels beyond K and V are zeros from here on: the copies leave them alone
   for (uint32_t* p = reinterpret_cast<uint32_t*>(slots) + lane; p < reinterpret_cast<uint32_t*>(slots + NST); p += 32) *p = 0;
   __syncwarp();
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
         }
       }
 #pragma unroll
-      for (int i = 0; i < CH * COLS / 128; ++i) {
+      for (int i = 0; i < CPL; ++i) {
         const int r = (lane + 32 * i) / (COLS / 4), e = (lane + 32 * i) % (COLS / 4) * 4;
         if (e < width) copy16(smem_addr(&w.v[r][e]), v + (int64_t)(row + dir * r) * a.vs + e, r < len);
       }
@@ -119,9 +119,11 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   };
 
   for (int s = 0; s < NST; ++s) issue(slots[s]);
-  uint64_t S[HALF / 2];
+  uint64_t S[CPL][HALF / 2];
 #pragma unroll
-  for (int i = 0; i < HALF / 2; ++i) S[i] = 0;
+  for (int j = 0; j < CPL; ++j)
+#pragma unroll
+    for (int i = 0; i < HALF / 2; ++i) S[j][i] = 0;
   float total = 0.0f;
   const int64_t KV = (int64_t)a.K * a.V;
   for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
@@ -136,42 +138,58 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
         st = STATE_ONLY ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
       else if (a.state_in)
         st = a.state_in + ((int64_t)seq * a.H + h) * KV;
-      st = st && col < width ? st + i0 * a.V + c0 + col : nullptr;
+      if (st) st += i0 * a.V + c0 + col;
 #pragma unroll
-      for (int i = 0; i < HALF; i += 2)
-        S[i / 2] = st && i0 + i < a.K ? both(st[i * a.V], st[(i + 1) * a.V]) : 0;
+      for (int j = 0; j < CPL; ++j)
+#pragma unroll
+        for (int i = 0; i < HALF; i += 2)
+          S[j][i / 2] = st && col + 16 * j < width && i0 + i < a.K ? both(st[i * a.V + 16 * j], st[(i + 1) * a.V + 16 * j]) : 0;
     }
     for (int r = 0; r < len; ++r) {
-      const float e = expf(w.g[r]), x = w.v[r][col];
-      const uint64_t ee = both(e, e), xx = both(x, x);
+      const float e = expf(w.g[r]);
+      const uint64_t ee = both(e, e);
+      uint64_t x[CPL], acc[CPL][2];
+#pragma unroll
+      for (int j = 0; j < CPL; ++j) {
+        x[j] = both(w.v[r][col + 16 * j], w.v[r][col + 16 * j]);
+        acc[j][0] = acc[j][1] = 0;
+      }
       if (STATE_ONLY) total += w.g[r];
-      uint64_t acc[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < HALF; i += 4) {
         const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(&w.k[r][i0 + i]);
-        S[i / 2] = fma2(kk.x, xx, mul2(ee, S[i / 2]));
-        S[i / 2 + 1] = fma2(kk.y, xx, mul2(ee, S[i / 2 + 1]));
-        if (!STATE_ONLY) {
-          const ulonglong2 qq = *reinterpret_cast<const ulonglong2*>(&w.q[r][i0 + i]);
-          acc[0] = fma2(qq.x, S[i / 2], acc[0]);
-          acc[1] = fma2(qq.y, S[i / 2 + 1], acc[1]);
+        ulonglong2 qq;
+        if (!STATE_ONLY) qq = *reinterpret_cast<const ulonglong2*>(&w.q[r][i0 + i]);
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) {
+          S[j][i / 2] = fma2(kk.x, x[j], mul2(ee, S[j][i / 2]));
+          S[j][i / 2 + 1] = fma2(kk.y, x[j], mul2(ee, S[j][i / 2 + 1]));
+          if (!STATE_ONLY) {
+            acc[j][0] = fma2(qq.x, S[j][i / 2], acc[j][0]);
+            acc[j][1] = fma2(qq.y, S[j][i / 2 + 1], acc[j][1]);
+          }
         }
       }
       if (!STATE_ONLY) {
-        const float2 o0 = parts(acc[0]), o1 = parts(acc[1]);
-        float o = (o0.x + o0.y) + (o1.x + o1.y);
-        o += __shfl_xor_sync(FULL, o, 16);
-        if (part == 0 && col < width) out[(int64_t)(row + dir * r) * a.os] = a.scale * o;
+        float* o = out + (int64_t)(row + dir * r) * a.os;
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) {
+          const float2 o0 = parts(acc[j][0]), o1 = parts(acc[j][1]);
+          float y = (o0.x + o0.y) + (o1.x + o1.y);
+          y += __shfl_xor_sync(FULL, y, 16);
+          if (part == 0 && col + 16 * j < width) o[16 * j] = a.scale * y;
+        }
       }
     }
     if ((flags & LAST) && (STATE_ONLY || ((flags & ENDS) && a.state_out))) {
       float* st = STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV;
-      if (col < width)
+#pragma unroll
+      for (int j = 0; j < CPL; ++j)
 #pragma unroll
         for (int i = 0; i < HALF; i += 2)
-          if (i0 + i < a.K) {
-            const float2 s2 = parts(S[i / 2]);
-            float* d = st + (i0 + i) * a.V + c0 + col;
+          if (col + 16 * j < width && i0 + i < a.K) {
+            const float2 s2 = parts(S[j][i / 2]);
+            float* d = st + (i0 + i) * a.V + c0 + col + 16 * j;
             d[0] = s2.x, d[a.V] = s2.y;
           }
       if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
@@ -306,21 +324,38 @@ size_t workspace_bytes(int64_t n_rows, int64_t n_seq, int H, int K, int V) {
   return flags + decay + bounds * H * (size_t)K * V * 4;
 }
 
-template <int DK, bool STATE_ONLY>
+template <int DK, int CPL, bool STATE_ONLY>
 int launch_simt(const LaArgs& a, cudaStream_t st) {
-  const size_t sm = sizeof(SimtSlot<DK>) * NST;
-  auto kern = la_simt_kernel<DK, STATE_ONLY>;
-  static_assert(sizeof(SimtSlot<DK>) * NST <= 48 * 1024, "needs no leave");
+  const size_t sm = sizeof(SimtSlot<DK, CPL>) * NST;
+  auto kern = la_simt_kernel<DK, CPL, STATE_ONLY>;
+  static_assert(sizeof(SimtSlot<DK, CPL>) * NST <= 48 * 1024, "needs no leave");
   kern<<<linear_grid(a, STATE_ONLY), 32, sm, st>>>(a);
   return launched();
+}
+// Columns a lane, at most 64 registers of state, the slices alike.
+int columns_a_lane(int K, int V) {
+  const int most = K <= 32 ? 4 : K <= 64 ? 2 : 1, all = (V + 15) / 16, slices = (all + most - 1) / most;
+  return (all + slices - 1) / slices;
+}
+template <int DK, bool STATE_ONLY>
+int by_columns(const LaArgs& a, cudaStream_t st) {
+  const int c = columns_a_lane(a.K, a.V);
+  if constexpr (DK <= 32) {
+    if (c == 4) return launch_simt<DK, 4, STATE_ONLY>(a, st);
+    if (c == 3) return launch_simt<DK, 3, STATE_ONLY>(a, st);
+  }
+  if constexpr (DK <= 64) {
+    if (c == 2) return launch_simt<DK, 2, STATE_ONLY>(a, st);
+  }
+  return launch_simt<DK, 1, STATE_ONLY>(a, st);
 }
 template <bool STATE_ONLY>
 int run(int32_t dtype, const LaArgs& a, cudaStream_t st) {
   if (dtype != TRACKFIT_FP32) return linear_mma(dtype, a, STATE_ONLY, st);
-  if (a.K <= 16) return launch_simt<16, STATE_ONLY>(a, st);
-  if (a.K <= 32) return launch_simt<32, STATE_ONLY>(a, st);
-  if (a.K <= 64) return launch_simt<64, STATE_ONLY>(a, st);
-  return launch_simt<128, STATE_ONLY>(a, st);
+  if (a.K <= 16) return by_columns<16, STATE_ONLY>(a, st);
+  if (a.K <= 32) return by_columns<32, STATE_ONLY>(a, st);
+  if (a.K <= 64) return by_columns<64, STATE_ONLY>(a, st);
+  return by_columns<128, STATE_ONLY>(a, st);
 }
 
 }  // namespace
@@ -360,7 +395,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
   a.q = q, a.k = k, a.v = v, a.g = log_decay, a.out = out;
   a.qs = q_stride, a.ks = k_stride, a.vs = v_stride, a.gs = decay_stride, a.os = out_stride;
   a.state_in = state_in, a.state_out = state_out;
-  const int cols = dtype == TRACKFIT_FP32 ? COLS : linear_mma_cols(key_dim);
+  const int cols = dtype == TRACKFIT_FP32 ? 16 * columns_a_lane(key_dim, value_dim) : linear_mma_cols(key_dim);
   a.H = n_heads, a.K = key_dim, a.V = value_dim, a.slices = (value_dim + cols - 1) / cols;
   a.scale = scale;
   a.u.offs = offsets, a.u.n_seq = n_seq, a.u.n_rows = n_rows, a.u.reverse = reverse;

@@ -29,7 +29,7 @@
 //
 // Roundings: the products' operands are 16 bits.  Q K^T o L is split into two bf16 parts, the
 // decayed V into two, or three where the state is asked for (bf16: 8, 16, 24 bits), so that
-// the states keep fp32; the state's operand of Q S is rounded once, which the output's own
+// the states keep fp32 (asked for, they also add each chunk's sum outside the products); the state's operand of Q S is rounded once, which the output's own
 // rounding exceeds.  fp16 has the bits but not the range for Q K^T and S: these go through
 // tf32 products (11 bits, fp32's range), the decayed V, no larger than V, is split in two.
 #include "linear_units.cuh"
@@ -101,7 +101,7 @@ __device__ __forceinline__ void add_rows(T, Mul mul, bool zero, float (&o)[NV][4
 }
 
 template <class T, int NG, int NV, bool STATE_ONLY, bool EXACT>
-__global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) la_mma_kernel(const __grid_constant__ LaArgs a) {
+__global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kernel(const __grid_constant__ LaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr bool BF = !__is_same(T, __half);
   constexpr int MT = NV / 2, KT = NG * 4;             // tiles of the state: MT x 16 by KT x 8
@@ -411,22 +411,22 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) la_mma_kernel(const __gr
 
     if (update) {
       const float f = ex2(__shfl_sync(FULL, P, 15));
-      if (!zero) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int j = 0; j < KT; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st[m][j][i] *= f;
-      } else {
-        zero = false;
+      if (zero) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int j = 0; j < KT; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st[m][j][i] = 0.0f;
+      } else if (!EXACT) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int j = 0; j < KT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st[m][j][i] *= f;
       }
+      zero = false;
       float Z = __shfl_down_sync(FULL, x, 1, 16);
       if (lr == 15) Z = 0.0f;
 #pragma unroll
@@ -464,9 +464,21 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) la_mma_kernel(const __gr
         }
         const uint32_t b0 = turned(k[i0][0][j % 4]), b1 = turned(k[i0][1][j % 4]);
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m) {
+          if (EXACT) {
+            // a chunk's own sum first: the products' accumulation cuts bits off, and on the state
+            // itself that would shrink it a little with every chunk
+            float d[4];
+            mma16_new(d, va[0][m], b0, b1, T());
 #pragma unroll
-          for (int e = 0; e < TERMS; ++e) mma16(st[m][j], va[e][m], b0, b1, T());
+            for (int e = 1; e < TERMS; ++e) mma16(d, va[e][m], b0, b1, T());
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st[m][j][i] = fmaf(st[m][j][i], f, d[i]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) mma16(st[m][j], va[e][m], b0, b1, T());
+          }
+        }
       }
       if ((flags & LAST) && (STATE_ONLY || (flags & ENDS))) {
         store_state(STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)ch.seq * a.H + h) * KV);
@@ -493,12 +505,8 @@ int launch(const LaArgs& a, cudaStream_t st) {
 }
 template <class T, int NG, int NV>
 int by_use(const LaArgs& a, bool state_only, cudaStream_t st) {
-  // fp16 splits into two parts either way
-  if constexpr (!__is_same(T, __half)) {
-    if (a.state_out && state_only) return launch<T, NG, NV, true, true>(a, st);
-    if (a.state_out) return launch<T, NG, NV, false, true>(a, st);
-  }
-  return state_only ? launch<T, NG, NV, true, false>(a, st) : launch<T, NG, NV, false, false>(a, st);
+  if (state_only) return a.state_out ? launch<T, NG, NV, true, true>(a, st) : launch<T, NG, NV, true, false>(a, st);
+  return a.state_out ? launch<T, NG, NV, false, true>(a, st) : launch<T, NG, NV, false, false>(a, st);
 }
 template <class T>
 int by_width(const LaArgs& a, bool state_only, cudaStream_t st) {
