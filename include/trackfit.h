@@ -472,7 +472,8 @@ int trackfit_linear_attention_step(int32_t dtype, const void* q, int64_t q_strid
  *   q, out      [n_q_rows][q_heads][head_dim], sequences by q_offsets.
  *   k, v        [n_kv_rows][kv_heads][head_dim], sequences by kv_offsets; head h of the
  *               queries reads head h / (q_heads / kv_heads).
- * A query whose sequence has no states gets zeros.
+ * A query whose sequence has no states gets zeros.  Waits inside the kernels are limited
+ * (2 s): see trackfit_operator_errors.
  *   workspace   trackfit_cross_attention_workspace() bytes, 16-byte aligned (few queries:
  *               the states are split and the parts joined through it; NULL when that is
  *               0). */
@@ -483,6 +484,12 @@ int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, con
                              const int64_t* kv_offsets, int64_t n_kv_rows, int64_t n_seq, int32_t q_heads,
                              int32_t kv_heads, int32_t head_dim, float scale, void* out, int64_t out_stride,
                              void* workspace, size_t workspace_size, void* stream);
+
+/* The counterpart of trackfit_device_errors for the operators: synchronises `stream` and
+ * returns TRACKFIT_ERR_TIMEOUT if a bounded wait of an operator's kernel on the current
+ * device has expired since the last call (outputs written since then are not valid), else
+ * OK. */
+int trackfit_operator_errors(void* stream);
 
 #ifdef __cplusplus
 }

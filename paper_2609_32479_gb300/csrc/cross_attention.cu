@@ -48,13 +48,21 @@ __global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant_
     if (lane + 32 * c < a.D) put(out + lane + 32 * c, o[c]);
 }
 
-// Parts of each row's range: as many as give 152 x 12 warps something to do, not under 256
-// states each on average, and at most the 32 that the joining warp has lanes for.
-int splits_of(int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk) {
+// Whether the 128-row kernel runs: 16-bit types, sequences of at least 64 rows and 512 states on
+// average.
+bool wide_tiles(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int G) {
+  return dtype != TRACKFIT_FP32 && nq * G >= 64 * n_seq && nk >= 512 * n_seq;
+}
+// Parts of each row's range: as many as give every warp of the GPU something to do (152 x 12 of
+// the 16-row kernels, 152 x 2 CTAs of the 128-row one, 152 for wide heads), not under 256 states
+// each (512) on average, and at most the 32 that the joining warp has lanes for.
+int splits_of(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk, int D) {
   if (nq <= 0 || n_seq <= 0) return 1;
-  const int64_t units = (nq * (Hq / Hk) + 15) / 16 * Hk;
-  const int64_t most = nk / n_seq / 256;
-  int64_t s = 152 * 12 / units;
+  const int G = Hq / Hk;
+  const bool wide = wide_tiles(dtype, nq, nk, n_seq, G);
+  const int64_t units = (nq * G + (wide ? 127 : 15)) / (wide ? 128 : 16) * Hk;
+  const int64_t most = nk / n_seq / (wide ? 512 : 256);
+  int64_t s = (wide ? (D <= 64 ? 304 : 152) : 152 * 12) / units;
   if (s > most) s = most;
   return s < 1 ? 1 : s > 32 ? 32 : (int)s;
 }
@@ -66,7 +74,7 @@ extern "C" size_t trackfit_cross_attention_workspace(int32_t dtype, int64_t n_q_
   if (!type_ok(dtype) || n_q_rows < 0 || n_kv_rows < 0 || n_seq < 0 || !heads_ok(q_heads) || !heads_ok(kv_heads) ||
       q_heads % kv_heads != 0 || !dim_ok(head_dim) || n_q_rows > MOST_ROWS / (q_heads / kv_heads) || n_kv_rows > MOST_ROWS)
     return 0;
-  const int s = splits_of(n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
+  const int s = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads, head_dim);
   return s > 1 ? (size_t)s * n_q_rows * q_heads * (head_dim + 2) * 4 : 0;
 }
 
@@ -101,12 +109,19 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
   a.Hq = q_heads, a.Hk = kv_heads, a.G = q_heads / kv_heads, a.D = head_dim;
   a.scale2 = scale == 0.0f ? 1.0f : fabsf(scale) * LOG2E;
   a.q_and = scale == 0.0f ? 0u : ~0u, a.q_xor = scale < 0.0f ? (dtype == TRACKFIT_FP32 ? 0x80000000u : 0x80008000u) : 0u;
-  a.splits = splits_of(n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads);
+  a.splits = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads, head_dim);
   // all heads of a tile where that leaves ten tiles for each of the 152 x 16 warps
   a.each = (n_q_rows * a.G + 15) / 16 >= 10 * 152 * 16 ? kv_heads : 1;
   a.ws_o = static_cast<float*>(workspace);
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (need > 0 ? (int64_t)a.splits * n_q_rows * q_heads * head_dim : 0));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  a.tc_from = 0;
+  if (wide_tiles(dtype, n_q_rows, n_kv_rows, n_seq, a.G)) {
+    // the 16-row kernel after it takes the sequences of few states, if there are any
+    a.tc_from = CROSS_TC_FROM;
+    const int rc = cross_tc(dtype, a, st);
+    if (rc != TRACKFIT_OK) return rc;
+  }
   const int rc = dtype == TRACKFIT_FP32 ? cross_tf32(a, st) : cross_mma(dtype, a, st);
   if (rc != TRACKFIT_OK || a.splits == 1) return rc;
   const unsigned grid = (unsigned)((n_q_rows * q_heads + NW - 1) / NW);   // (only few rows are split)

@@ -260,9 +260,9 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
 
 template <class T, int NG>
 int launch(const CaArgs& a, cudaStream_t st) {
-  auto kern = ca_mma_kernel<T, NG>;
+  constexpr auto kern = ca_mma_kernel<T, NG>;
   const size_t smem = queue<NG>() * NG * 8 * 512;
-  const cudaError_t e = allow_smem(kern, smem);
+  const cudaError_t e = allow_smem<kern>(smem);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
   const int64_t units = (a.nq * a.G + 15) / 16 * (a.Hk / a.each) * a.splits;
   if (units > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;

@@ -1,0 +1,450 @@
+// Attention of many queries to many packed states, 16-bit types, on the tcgen05 tensor cores:
+// tiles of 128 rows of one head of the states, blocks of 128 states.
+//
+//   S = Q K^T (tensor memory), P = 2^(S - m), O = O 2^(m_before - m) + P V (tensor memory)
+//
+// A CTA goes through the sequences that its rows belong to, one after the other (a pass each);
+// rows of other sequences take part in the products and are not written.  Sequences of fewer
+// than 128 states are left to the 16-row kernel.  The last block of a sequence ends at its last
+// state and takes the first ones twice, the second time with weight zero: no state of another
+// sequence is ever in a product.
+//   warps 0-3  a thread a row: the maximum of S, the weights (packed to 16 bits into shared
+//              memory, the K-major operand of P V), the sum; at a pass's end O / l
+//   warp 4     TMA loads of K and V, two stages each
+//   warp 5     the tcgen05.mma issuer and owner of the tensor memory
+// The maximum that the weights are taken against moves only when a row's grows by more than 2^8:
+// the weights then stay below 256, and O is hardly ever read back and scaled.
+// With heads up to 64 channels two CTAs share an SM (112 KB and 256 columns each), one's products
+// beside the other's exponentials.
+//
+// Bound: per block the products take 617 clocks of an SM, the 16,384 exponentials 512, and the
+// instructions around them (scale and subtract, maximum, sum, packing) about 600.
+// Every wait has a limit; where one expires, the CTA gives up, the call's outputs are not valid,
+// and trackfit_operator_errors() says so.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include "cross_units.cuh"
+#include "sm100_ptx.cuh"
+
+namespace {
+using namespace seqops;
+using namespace sm100;
+
+constexpr int TILE = 128;                    // rows of a tile, states of a block
+constexpr uint32_t ATOM = 16384;             // 128 rows of 64 channels
+constexpr uint64_t LIMIT_NS = 2000000000ull;
+constexpr int STAGES = 2;
+constexpr float LAG = 8.0f;                  // the maximum may be 2^8 behind
+
+struct TcArgs {
+  CaArgs a;
+  int tiles;
+  uint32_t idesc_s, idesc_o;
+  unsigned long long* err;
+};
+
+struct Bars {
+  uint64_t k_full[STAGES], k_free[STAGES], v_full[STAGES], v_free[STAGES];
+  uint64_t s_full, p_full, o_done, drained;
+  uint32_t tmem;
+  int abort_flag;
+};
+
+template <int NA>
+constexpr __host__ __device__ uint32_t smem_bytes() {
+  return (NA * (1 + 2 * STAGES) + 2) * ATOM + 256;
+}
+static_assert(sizeof(Bars) <= 256, "the barriers' place");
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::
+          "r"(dst),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+
+// The passes of a tile, alike for every warp.
+struct Pass {
+  int lo, len;          // the sequence's states
+  int first, last;      // rows of the tile that are its queries: [first, last)
+  int j0, j1;           // this part's blocks
+};
+class Passes {
+ public:
+  __device__ __forceinline__ Passes(const CaArgs& a, int row0, int split, int lane) : a_(a), row0_(row0), split_(split) {
+    b_ = first_at_least(a.qo, a.n_seq, (int64_t)row0 / a.G + 1, lane) - 1;
+    if (b_ < 0) b_ = 0;
+  }
+  __device__ __forceinline__ bool next(Pass& p) {
+    const int64_t rows = a_.nq * a_.G, top = row0_ + TILE < rows ? row0_ + TILE : rows;
+    for (; b_ < a_.n_seq; ) {
+      const int64_t qlo = clamp64(a_.qo[b_], 0, a_.nq) * a_.G, qhi = clamp64(a_.qo[b_ + 1], 0, a_.nq) * a_.G;
+      if (qlo >= top) return false;
+      const int64_t b = b_++;
+      if (qhi <= row0_ || qhi <= qlo) continue;
+      const int64_t lo = clamp64(a_.ko[b], 0, a_.nk), hi = clamp64(a_.ko[b + 1], lo, a_.nk);
+      if (hi - lo < TILE) continue;
+      p.lo = (int)lo, p.len = (int)(hi - lo);
+      p.first = (int)(qlo > row0_ ? qlo - row0_ : 0), p.last = (int)((qhi < top ? qhi : top) - row0_);
+      const int64_t nb = (p.len + TILE - 1) / TILE;
+      p.j0 = (int)(nb * split_ / a_.splits), p.j1 = (int)(nb * (split_ + 1) / a_.splits);
+      return true;
+    }
+    return false;
+  }
+
+ private:
+  const CaArgs& a_;
+  int row0_, split_;
+  int64_t b_;
+};
+// The first state of a block.
+__device__ __forceinline__ int block_at(const Pass& p, int j) {
+  return p.lo + ((j + 1) * TILE > p.len ? p.len - TILE : j * TILE);
+}
+
+__device__ __forceinline__ void give_up(Bars* s, unsigned long long* err) {
+  if (atomicExch(&s->abort_flag, 1) == 0) atomicAdd(err, 1ull);
+}
+
+template <class T, int NA>
+__global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
+    ca_tc_kernel(const __grid_constant__ TcArgs p, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const CaArgs& a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned unit = blockIdx.x;
+  const int tile = unit % p.tiles, hk = unit / p.tiles % a.Hk, split = unit / p.tiles / a.Hk;
+  const int row0 = tile * TILE;
+  const int rows = (int)(a.nq * a.G);
+  const uint32_t base = smem_u32(smem);
+  if (base & 1023u) {                                  // the swizzled tiles' alignment, asked for above
+    if (threadIdx.x == 0) atomicAdd(p.err, 1ull);
+    return;
+  }
+  const uint32_t q_s = base, k_s = q_s + NA * ATOM, v_s = k_s + STAGES * NA * ATOM, p_s = v_s + STAGES * NA * ATOM;
+  Bars* bars = reinterpret_cast<Bars*>(smem + (NA * (1 + 2 * STAGES) + 2) * ATOM);
+  const uint32_t s_full = smem_u32(&bars->s_full), p_full = smem_u32(&bars->p_full), o_done = smem_u32(&bars->o_done);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(smem_u32(&bars->k_full[i]), 1);
+      mbar_init(smem_u32(&bars->k_free[i]), 1);
+      mbar_init(smem_u32(&bars->v_full[i]), 1);
+      mbar_init(smem_u32(&bars->v_free[i]), 1);
+    }
+    mbar_init(s_full, 1);
+    mbar_init(p_full, 128);
+    mbar_init(o_done, 1);
+    mbar_init(smem_u32(&bars->drained), 1);
+    bars->abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 5) {
+    tmem_alloc(smem_u32(&bars->tmem), 256);
+    tmem_relinquish();
+  }
+  // the tile's queries: rows of 128 bytes, 16-byte pieces swizzled as the K-major operand wants
+  for (int i = threadIdx.x; i < TILE * NA * 8; i += 192) {
+    const int r = i / (NA * 8), e = i % (NA * 8), row = row0 + r;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (row < rows && e * 8 < a.D)
+      u = *reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(row / a.G) * a.qs + (hk * a.G + row % a.G) * a.D + e * 8);
+    const uint32_t at = q_s + (e >> 3) * ATOM + r * 128 + (((e & 7) ^ (r & 7)) << 4);
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"((u.x & a.q_and) ^ a.q_xor),
+                 "r"((u.y & a.q_and) ^ a.q_xor), "r"((u.z & a.q_and) ^ a.q_xor), "r"((u.w & a.q_and) ^ a.q_xor)
+                 : "memory");
+  }
+  fence_proxy_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem, tmem_o = tmem + TILE;
+  volatile int* abort = &bars->abort_flag;
+  Passes passes(a, row0, split, lane);
+  Pass ps;
+
+  if (warp == 4) {
+    // ---- loads
+    if (elect_one()) {
+      prefetch_tmap(&tk);
+      prefetch_tmap(&tv);
+      uint32_t n = 0;                                  // blocks loaded
+      bool ok = true;
+      while (ok && passes.next(ps)) {
+        for (int j = ps.j0; j < ps.j1 && ok; ++j, ++n) {
+          const int s = n % STAGES, row = block_at(ps, j);
+          const uint32_t ph = (n / STAGES & 1) ^ 1;
+          const uint32_t kf = smem_u32(&bars->k_full[s]), vf = smem_u32(&bars->v_full[s]);
+          ok = mbar_wait(smem_u32(&bars->k_free[s]), ph, abort, LIMIT_NS);
+          if (!ok) break;
+          mbar_arrive_expect_tx(kf, NA * ATOM);
+          for (int c = 0; c < NA; ++c) tma_load_3d(k_s + (s * NA + c) * ATOM, &tk, kf, 64 * c, hk, row);
+          ok = mbar_wait(smem_u32(&bars->v_free[s]), ph, abort, LIMIT_NS);
+          if (!ok) {
+            // the keys just asked for land before the CTA may exit
+            volatile int never = 0;
+            mbar_wait(kf, n / STAGES & 1, &never, LIMIT_NS);
+            break;
+          }
+          mbar_arrive_expect_tx(vf, NA * ATOM);
+          for (int c = 0; c < NA; ++c) tma_load_3d(v_s + (s * NA + c) * ATOM, &tv, vf, 64 * c, hk, row);
+        }
+      }
+      if (!ok) give_up(bars, p.err);
+      // copies still under way land before the CTA exits (after a failure nobody else waits for them)
+      volatile int never = 0;
+      for (uint32_t i = n < STAGES ? 0 : n - STAGES; i < n; ++i) {
+        mbar_wait(smem_u32(&bars->k_full[i % STAGES]), i / STAGES & 1, &never, LIMIT_NS);
+        mbar_wait(smem_u32(&bars->v_full[i % STAGES]), i / STAGES & 1, &never, LIMIT_NS);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 5) {
+    // ---- products
+    if (elect_one()) {
+      uint32_t n = 0;
+      bool ok = true;
+      while (ok && passes.next(ps)) {
+        for (int j = ps.j0; j < ps.j1; ++j, ++n) {
+          const int s = n % STAGES;
+          const uint32_t ph = n / STAGES & 1;
+          ok = mbar_wait(smem_u32(&bars->k_full[s]), ph, abort, LIMIT_NS);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t ks = k_s + s * NA * ATOM, vs = v_s + s * NA * ATOM;
+          for (int c = 0; c < NA; ++c)
+            for (int k = 0; k < 4; ++k)
+              umma_f16(tmem, sdesc_sw128(q_s + c * ATOM + 32 * k, 16, 1024), sdesc_sw128(ks + c * ATOM + 32 * k, 16, 1024),
+                       p.idesc_s, c | k);
+          umma_commit(s_full);
+          umma_commit(smem_u32(&bars->k_free[s]));
+          ok = mbar_wait(p_full, n & 1, abort, LIMIT_NS) && mbar_wait(smem_u32(&bars->v_full[s]), ph, abort, LIMIT_NS);
+          if (!ok) break;
+          tc_fence_after();
+          // V as it lies, [state][channel]: groups of 8 states 1024 bytes apart, 64 channels ATOM
+          for (int k = 0; k < 8; ++k)
+            umma_f16(tmem_o, sdesc_sw128(p_s + (k >> 2) * ATOM + 32 * (k & 3), 16, 1024), sdesc_sw128(vs + k * 2048, ATOM, 1024),
+                     p.idesc_o, (j > ps.j0) | (k > 0));
+          umma_commit(smem_u32(&bars->v_free[s]));
+          if (j + 1 == ps.j1) umma_commit(o_done);
+        }
+      }
+      if (!ok) give_up(bars, p.err);
+      // products still under way end before their memory is given back
+      volatile int never = 0;
+      umma_commit(smem_u32(&bars->drained));
+      mbar_wait(smem_u32(&bars->drained), 0, &never, LIMIT_NS);
+    }
+    __syncwarp();
+  } else {
+    // ---- a thread a row
+    const int r = threadIdx.x, row = row0 + r;
+    const uint32_t lanes = (uint32_t)(32 * warp) << 16;
+    uint32_t n = 0, done = 0;
+    bool ok = true;
+    while (ok && passes.next(ps)) {
+      float m = -INFINITY, l = 0.0f;                   // m: score * scale2 that the weights are taken against
+      for (int j = ps.j0; j < ps.j1; ++j, ++n) {
+        ok = __all_sync(FULL, mbar_wait(s_full, n & 1, abort, LIMIT_NS));
+        if (!ok) break;
+        tc_fence_after();
+        const int twice = (j + 1) * TILE > ps.len ? (j + 1) * TILE - ps.len : 0;   // states that the block before had
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          tmem_ld32(tmem + lanes + 32 * c, v);
+          tmem_ld_wait();
+          if (twice > 32 * c) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * c + i < twice) v[i] = -INFINITY;
+          }
+          float t0 = v[0], t1 = v[1], t2 = v[2], t3 = v[3];
+#pragma unroll
+          for (int i = 4; i < 32; i += 4)
+            t0 = fmaxf(t0, v[i]), t1 = fmaxf(t1, v[i + 1]), t2 = fmaxf(t2, v[i + 2]), t3 = fmaxf(t3, v[i + 3]);
+          top = fmaxf(top, fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)));
+        }
+        top *= a.scale2;
+        if (j == ps.j0) {
+          m = top;
+        } else {
+          const bool move = top > m + LAG;
+          if (__any_sync(FULL, move)) {
+            const float f = move ? ex2(m - top) : 1.0f;
+            if (move) m = top;
+            l *= f;
+#pragma unroll 1
+            for (int c = 0; c < NA * 2; ++c) {
+              float v[32];
+              tmem_ld32(tmem_o + lanes + 32 * c, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] *= f;
+              tmem_st32(tmem_o + lanes + 32 * c, v);
+            }
+            tmem_st_wait();
+          }
+        }
+        const float mm = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          tmem_ld32(tmem + lanes + 32 * c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = ex2(fmaf(v[i], a.scale2, -mm));
+          if (twice > 32 * c) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (32 * c + i < twice) v[i] = 0.0f;
+          }
+          float t0 = 0.0f, t1 = 0.0f, t2 = 0.0f, t3 = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) t0 += v[i], t1 += v[i + 1], t2 += v[i + 2], t3 += v[i + 3];
+          l += (t0 + t1) + (t2 + t3);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t at = p_s + (c >> 1) * ATOM + r * 128 + ((((c & 1) * 4 + i) ^ (r & 7)) << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack2(v[8 * i], v[8 * i + 1], T())),
+                         "r"(pack2(v[8 * i + 2], v[8 * i + 3], T())), "r"(pack2(v[8 * i + 4], v[8 * i + 5], T())),
+                         "r"(pack2(v[8 * i + 6], v[8 * i + 7], T()))
+                         : "memory");
+          }
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        mbar_arrive(p_full);
+      }
+      if (!ok) break;
+      const bool mine = r >= ps.first && r < ps.last, any = ps.j1 > ps.j0;
+      if (any) {
+        ok = __all_sync(FULL, mbar_wait(o_done, done++ & 1, abort, LIMIT_NS));
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const int64_t at = ((int64_t)split * rows + row) * a.Hk + hk;
+      const float f = a.splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+      if (a.splits > 1 && mine) a.ws_ml[at] = make_float2(m, l);
+      T* out = mine ? (T*)a.out + (int64_t)(row / a.G) * a.os + (hk * a.G + row % a.G) * a.D : nullptr;
+      float* part = mine ? a.ws_o + at * a.D : nullptr;
+#pragma unroll 1
+      for (int c = 0; c < NA * 2; ++c) {
+        float v[32];
+        __syncwarp();
+        if (any) {
+          tmem_ld32(tmem_o + lanes + 32 * c, v);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+        }
+        if (!mine) continue;
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+          if (32 * c + i >= a.D) continue;
+          if (a.splits > 1) {
+            *reinterpret_cast<float4*>(part + 32 * c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            *reinterpret_cast<float4*>(part + 32 * c + i + 4) = make_float4(v[i + 4], v[i + 5], v[i + 6], v[i + 7]);
+          } else {
+            *reinterpret_cast<uint4*>(out + 32 * c + i) =
+                make_uint4(pack2(v[i] * f, v[i + 1] * f, T()), pack2(v[i + 2] * f, v[i + 3] * f, T()),
+                           pack2(v[i + 4] * f, v[i + 5] * f, T()), pack2(v[i + 6] * f, v[i + 7] * f, T()));
+          }
+        }
+      }
+    }
+    if (!ok) give_up(bars, p.err);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 5) tmem_dealloc(tmem, 256);
+}
+
+__device__ unsigned long long g_expired;   // waits that ran out, of all operators
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+  static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+  }();
+  return fn;
+}
+
+// [rows][heads][D] with a row stride, boxes of 64 channels of a head and 128 rows, 128-byte swizzle;
+// channels from D on and rows beyond the array read as zero.
+bool make_map(CUtensorMap* m, const void* p, int64_t rows, int64_t stride, int heads, int D, bool fp16) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64, 1, TILE}, step[3] = {1, 1, 1};
+  return fn(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims,
+            strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The address of g_expired on the current device.
+cudaError_t expired_address(unsigned long long** out) {
+  static std::atomic<unsigned long long*> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  unsigned long long* p = dev < 64 ? known[dev].load() : nullptr;
+  if (!p) {
+    e = cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_expired);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) known[dev].store(p);
+  }
+  *out = p;
+  return cudaSuccess;
+}
+
+template <class T, int NA>
+int launch(const CaArgs& a, bool fp16, cudaStream_t st) {
+  TcArgs p;
+  p.a = a;
+  p.tiles = (int)((a.nq * a.G + TILE - 1) / TILE);
+  p.idesc_s = idesc_f16(128, 128, fp16 ? 0u : 1u, false, false);
+  p.idesc_o = idesc_f16(128, NA * 64, fp16 ? 0u : 1u, false, true);
+  cudaError_t e = expired_address(&p.err);
+  if (e != cudaSuccess) return tf_status_from_cuda(e);
+  CUtensorMap tk, tv;
+  if (!make_map(&tk, a.k, a.nk, a.ks, a.Hk, a.D, fp16) || !make_map(&tv, a.v, a.nk, a.vs, a.Hk, a.D, fp16))
+    return TRACKFIT_ERR_CUDA;
+  constexpr auto kern = ca_tc_kernel<T, NA>;
+  e = allow_smem<kern>(smem_bytes<NA>());
+  if (e != cudaSuccess) return tf_status_from_cuda(e);
+  const int64_t units = (int64_t)p.tiles * a.Hk * a.splits;
+  if (units > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
+  kern<<<(unsigned)units, 192, smem_bytes<NA>(), st>>>(p, tk, tv);
+  return launched();
+}
+
+}  // namespace
+
+int seqops::cross_tc(int32_t dtype, const CaArgs& a, cudaStream_t st) {
+  if (dtype == TRACKFIT_BF16_PROJ)
+    return a.D <= 64 ? launch<__nv_bfloat16, 1>(a, false, st) : launch<__nv_bfloat16, 2>(a, false, st);
+  return a.D <= 64 ? launch<__half, 1>(a, true, st) : launch<__half, 2>(a, true, st);
+}
+
+extern "C" int trackfit_operator_errors(void* stream) {
+  tf_nvtx_range nvtx_range("trackfit_operator_errors");
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  unsigned long long* p = nullptr;
+  unsigned long long n = 0;
+  cudaError_t e = expired_address(&p);
+  if (e == cudaSuccess) e = cudaMemcpyAsync(&n, p, sizeof(n), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaMemsetAsync(p, 0, sizeof(n), st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return tf_status_from_cuda(e);
+  return n > 0 ? TRACKFIT_ERR_TIMEOUT : TRACKFIT_OK;
+}

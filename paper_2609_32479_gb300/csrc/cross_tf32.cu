@@ -229,9 +229,9 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
 
 template <int NG>
 int launch(const CaArgs& a, cudaStream_t st) {
-  auto kern = ca_tf32_kernel<NG>;
+  constexpr auto kern = ca_tf32_kernel<NG>;
   const size_t smem = queue<NG>() * slot_bytes<NG>() + NG * 2 * 512;
-  const cudaError_t e = allow_smem(kern, smem);
+  const cudaError_t e = allow_smem<kern>(smem);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
   const int64_t units = (a.nq * a.G + 15) / 16 * a.Hk * a.splits;
   if (units > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;

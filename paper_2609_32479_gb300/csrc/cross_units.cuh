@@ -21,6 +21,7 @@ struct CaArgs {
   float scale2;                  // |scale| * log2(e), or 1 with a scale of 0
   uint32_t q_and, q_xor;         // on queries (two of 16 bits): zeroed with a scale of 0, negated below it
   int splits;
+  int tc_from;                   // sequences of at least so many states are cross_tc.cu's (0: none)
   int each;                      // heads of the states that a warp takes one after the other
   float* ws_o;                   // [splits][rows][Hk][D], sums not yet divided
   float2* ws_ml;                 // [splits][rows][Hk]: the largest score (base 2), the sum of weights
@@ -49,6 +50,10 @@ __device__ __forceinline__ void find_rows(const CaArgs& a, int tile, int split, 
   lo = hi = 0;
   if (in) {
     const int64_t l = clamp64(a.ko[b], 0, a.nk), h = clamp64(a.ko[b + 1], l, a.nk);
+    if (a.tc_from && h - l >= a.tc_from) {
+      in = false;
+      return;
+    }
     lo = (int)(l + (h - l) * split / a.splits), hi = (int)(l + (h - l) * (split + 1) / a.splits);
   }
 }
@@ -63,5 +68,8 @@ __device__ __forceinline__ int first_wanted(int pos, int lo0, int hi0, int lo1, 
 // cross_mma.cu: the 16-bit types on the tensor cores; cross_tf32.cu: fp32, likewise.
 int cross_mma(int32_t dtype, const CaArgs& a, cudaStream_t st);
 int cross_tf32(const CaArgs& a, cudaStream_t st);
+// cross_tc.cu: sequences of at least CROSS_TC_FROM states, 128 rows at a time.
+constexpr int CROSS_TC_FROM = 128;
+int cross_tc(int32_t dtype, const CaArgs& a, cudaStream_t st);
 
 }  // namespace seqops

@@ -121,9 +121,10 @@ inline bool heads_ok(int32_t h) { return h >= 1 && h <= MAX_HEADS; }
 inline bool rows_ok(const void* p, int64_t stride, int64_t width, int size) {
   return p && !mis16(p) && stride >= width && stride <= MAX_STRIDE && (stride * size) % 16 == 0;
 }
-// Dynamic shared memory beyond what any kernel may have needs leave, once a device and kernel.
-template <class K>
-inline cudaError_t allow_smem(K* kernel, size_t bytes) {
+// Dynamic shared memory beyond what any kernel may have needs leave, once a device and kernel
+// (the kernel itself is the parameter: several have one type).
+template <auto kernel>
+inline cudaError_t allow_smem(size_t bytes) {
   static std::atomic<uint64_t> given{0};   // a bit a device
   if (bytes <= 48 * 1024) return cudaSuccess;
   int dev = 0;

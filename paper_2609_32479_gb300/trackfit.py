@@ -29,7 +29,7 @@ EXPORTS = ("trackfit_weight_count", "trackfit_create", "trackfit_forward", "trac
            "trackfit_debug_schedule", "trackfit_debug_wait_limit", "trackfit_debug_alloc", "trackfit_seed",
            "trackfit_decode", "trackfit_forward_packed", "trackfit_last_error", "trackfit_qk_norm",
            "trackfit_linear_attention", "trackfit_linear_attention_workspace", "trackfit_linear_attention_step",
-           "trackfit_cross_attention", "trackfit_cross_attention_workspace")
+           "trackfit_cross_attention", "trackfit_cross_attention_workspace", "trackfit_operator_errors")
 
 
 class Config(ctypes.Structure):
@@ -126,6 +126,8 @@ def load() -> ctypes.CDLL:
     lib.trackfit_cross_attention.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, f32,
                                              vp, i64, vp, size, vp]
     lib.trackfit_cross_attention.restype = ctypes.c_int
+    lib.trackfit_operator_errors.argtypes = [vp]
+    lib.trackfit_operator_errors.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -561,3 +563,9 @@ def cross_attention(q, k, v, q_offsets, kv_offsets, out, scale: Optional[float] 
             a.vector("kv_offsets", kv_offsets, a.torch.int64, (b + 1,)), nk, b, hq, hk, d,
             float(d) ** -0.5 if scale is None else float(scale), op, os_),
            stream, need=lib.trackfit_cross_attention_workspace(t, nq, nk, b, hq, hk, d), workspace=workspace)
+
+
+def operator_errors(stream=None) -> int:
+    """OK, or ERR_TIMEOUT when a bounded wait of an operator's kernel on the current device has
+    expired since the last call (synchronises)."""
+    return load().trackfit_operator_errors(_stream_handle(stream))

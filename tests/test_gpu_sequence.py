@@ -373,10 +373,41 @@ def test_cross_long(T, t, nq, nk):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("D", [64, 8, 40, 72, 128])
+@pytest.mark.parametrize("nq,nk", [([128], [512]), ([300, 40, 0, 500], [3000, 100, 50, 128]),
+                                   ([1, 129, 127, 700], [1, 2047, 127, 4097]), ([64] * 9, [513] * 9)])
+def test_cross_of_many_queries_to_many_states(T, t, D, nq, nk):
+    """Averages of 64 queries and 512 states and more; among them sequences of few."""
+    check_cross(T, nq, nk, 2, 2, D, t)
+    check_cross(T, nq, nk, 6, 2, D, t, lead=3, tail=140, seed=3)
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_cross_of_growing_scores(T, t):
+    """Later states score higher and higher: the maximum that the weights are taken against moves."""
+    r = np.random.default_rng(12)
+    n, m, D = 200, 1500, 64
+    q = dev(1.0 + 0.1 * r.normal(size=(n, 1, D)), t)
+    k = dev(np.linspace(-6, 6, m)[:, None, None] * np.ones((m, 1, D)) + 0.1 * r.normal(size=(m, 1, D)), t)
+    v = dev(r.normal(size=(m, 1, D)), t)
+    out = torch.empty_like(q)
+    T.cross_attention(q, k, v, dev([0, n], "int64"), dev([0, m], "int64"), out)
+    args = host(q), host(k)
+    ref = Q.cross_attention(*args, host(v), [0, n], [0, m], D ** -0.5)
+    absv = Q.cross_attention(*args, np.abs(host(v)), [0, n], [0, m], D ** -0.5)
+    # a score of up to 60 is a sum of D terms of one sign: its error is D + 8 roundings of the score
+    tol = rounding(t, ref) + absv * (2 * (D + 8) * 60 * U + (m + 16) * U + (half_step(t) if t != "float32" else 0))
+    hold(out, ref, tol)
+
+
+@pytest.mark.parametrize("t", TYPES)
 def test_cross_of_sharp_and_flat_scores(T, t):
     check_cross(T, [40, 3], [100, 900], 2, 2, 32, t, spread=16.0)
     check_cross(T, [40, 3], [100, 900], 2, 2, 32, t, scale=0.0)
     check_cross(T, [40, 3], [100, 900], 2, 2, 32, t, scale=-0.25)
+    check_cross(T, [200], [900], 2, 2, 32, t, spread=16.0)
+    check_cross(T, [200], [900], 2, 2, 32, t, scale=0.0)
+    check_cross(T, [200], [900], 2, 2, 32, t, scale=-0.25)
 
 
 @pytest.mark.parametrize("t", TYPES)
@@ -398,6 +429,29 @@ def test_cross_keeps_what_is_not_finite_to_its_sequence(T, t):
     assert not ok[10:210, 1, 3].any() and ok[10:210, 1, :3].all()
 
 
+@pytest.mark.parametrize("t", TYPES)
+def test_cross_of_many_keeps_what_is_not_finite_to_its_sequence(T, t):
+    r = np.random.default_rng(10)
+    nq, nk = [100, 90, 200], [600, 700, 600]
+    qo, ko = np.concatenate([[0], np.cumsum(nq)]), np.concatenate([[0], np.cumsum(nk)])
+    (q,) = slab(r, [(qo[-1], 2, 32)], t)
+    k, v = slab(r, [(ko[-1], 2, 32)] * 2, t)
+    k[700, 0, 3] = float("nan")
+    v[1200, 1, 3] = float("inf")
+    q[250, 0, 0] = float("nan")
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    T.cross_attention(q, k, v, dev(qo, "int64"), dev(ko, "int64"), out)
+    ok = torch.isfinite(out).cpu()
+    assert ok[:100].all() and ok[190:250].all() and ok[251:].all() and ok[250, 1].all()
+    assert not ok[100:190, 0].any() and not ok[250, 0].any()
+    assert not ok[100:190, 1, 3].any() and ok[100:190, 1, :3].all()
+
+
+def test_no_wait_has_expired(T):
+    torch.cuda.synchronize()
+    assert T.operator_errors() == T.OK
+
+
 def test_cross_of_scores_that_are_all_minus_infinity_is_zero(T):
     q = torch.ones((2, 1, 16), device="cuda")
     k = torch.full((9, 1, 16), float("-inf"), device="cuda")
@@ -406,6 +460,11 @@ def test_cross_of_scores_that_are_all_minus_infinity_is_zero(T):
         out = torch.full((2, 1, 16), 5.0, device="cuda", dtype=getattr(torch, t))
         T.cross_attention(q.to(out.dtype), k.to(out.dtype), v.to(out.dtype), dev([0, 2], "int64"), dev([0, 9], "int64"), out)
         assert bool((out == 0).all())
+        many = torch.full((150, 1, 16), 5.0, device="cuda", dtype=out.dtype)
+        T.cross_attention(torch.ones_like(many), k[:1].expand(700, 1, 16).to(out.dtype).contiguous(),
+                          v[:1].expand(700, 1, 16).to(out.dtype).contiguous(), dev([0, 150], "int64"),
+                          dev([0, 700], "int64"), many)
+        assert bool((many == 0).all())
 
 
 # ---------------------------------------------------------------- together, streams, graphs
