@@ -1,24 +1,30 @@
 // Attention of many queries to many packed states, 16-bit types, on the tcgen05 tensor cores:
-// tiles of 128 rows of one head of the states, blocks of 128 states.
+// tiles of 128 rows of one head of the states, blocks of 64 states.
 //
 //   S = Q K^T (tensor memory), P = 2^(S - m), O = O 2^(m_before - m) + P V (tensor memory)
 //
 // A CTA goes through the sequences that its rows belong to, one after the other (a pass each);
 // rows of other sequences take part in the products and are not written.  Sequences of fewer
-// than 128 states are left to the 16-row kernel.  The last block of a sequence ends at its last
+// than 64 states are left to the 16-row kernel.  The last block of a sequence ends at its last
 // state and takes the first ones twice, the second time with weight zero: no state of another
 // sequence is ever in a product.
 //   warps 0-3  a thread a row: the maximum of S, the weights (packed to 16 bits into shared
 //              memory, the K-major operand of P V), the sum; at a pass's end O / l
-//   warp 4     TMA loads of K and V, two stages each
+//   warp 4     TMA loads of K and V
 //   warp 5     the tcgen05.mma issuer and owner of the tensor memory
+// S and P have two places each: the scores of the next block are formed while the weights of
+// this one are, and P V runs behind.  (In one place, with blocks of 128 states, the chain of
+// product, weights and product left the tensor cores idle most of the time: 448 us for 4,099
+// queries and 30,011 states of 8 heads of 64.)  A thread holds a block's 64 scores in registers:
+// one read of the tensor memory.
 // The maximum that the weights are taken against moves only when a row's grows by more than 2^8:
 // the weights then stay below 256, and O is hardly ever read back and scaled.
 // With heads up to 64 channels two CTAs share an SM (112 KB and 256 columns each), one's products
 // beside the other's exponentials.
 //
-// Bound: per block the products take 617 clocks of an SM, the 16,384 exponentials 512, and the
-// instructions around them (scale and subtract, maximum, sum, packing) about 600.
+// Bound: per 128 states the products take 617 clocks of an SM by their operations and 770 by
+// their operands' reads of shared memory, the 16,384 exponentials 512, and the instructions
+// around them (scale and subtract, maximum, sum, packing) about 550.
 // Every wait has a limit; where one expires, the CTA gives up, the call's outputs are not valid,
 // and trackfit_operator_errors() says so.
 #include <cuda.h>
@@ -31,10 +37,13 @@ namespace {
 using namespace seqops;
 using namespace sm100;
 
-constexpr int TILE = 128;                    // rows of a tile, states of a block
-constexpr uint32_t ATOM = 16384;             // 128 rows of 64 channels
+constexpr int TILE = 128;                    // rows of a tile
+constexpr int BLOCK = CROSS_TC_FROM;         // states of a block
+constexpr uint32_t ATOM_Q = TILE * 128;      // 128 rows of 64 channels, or of 64 weights
+constexpr uint32_t ATOM = BLOCK * 128;       // 64 states of 64 channels
 constexpr uint64_t LIMIT_NS = 2000000000ull;
-constexpr int STAGES = 2;
+constexpr int STAGES = 4;
+static_assert(BLOCK == 64, "a block's weights are one swizzled row of 128 bytes");
 constexpr float LAG = 8.0f;                  // the maximum may be 2^8 behind
 
 struct TcArgs {
@@ -46,14 +55,14 @@ struct TcArgs {
 
 struct Bars {
   uint64_t k_full[STAGES], k_free[STAGES], v_full[STAGES], v_free[STAGES];
-  uint64_t s_full, p_full, o_done, drained;
+  uint64_t s_full[2], p_full[2], p_free[2], o_done, drained;
   uint32_t tmem;
   int abort_flag;
 };
 
 template <int NA>
 constexpr __host__ __device__ uint32_t smem_bytes() {
-  return (NA * (1 + 2 * STAGES) + 2) * ATOM + 256;
+  return (NA + 2) * ATOM_Q + 2 * STAGES * NA * ATOM + 256;
 }
 static_assert(sizeof(Bars) <= 256, "the barriers' place");
 
@@ -85,10 +94,10 @@ class Passes {
       const int64_t b = b_++;
       if (qhi <= row0_ || qhi <= qlo) continue;
       const int64_t lo = clamp64(a_.ko[b], 0, a_.nk), hi = clamp64(a_.ko[b + 1], lo, a_.nk);
-      if (hi - lo < TILE) continue;
+      if (hi - lo < BLOCK) continue;
       p.lo = (int)lo, p.len = (int)(hi - lo);
       p.first = (int)(qlo > row0_ ? qlo - row0_ : 0), p.last = (int)((qhi < top ? qhi : top) - row0_);
-      const int64_t nb = (p.len + TILE - 1) / TILE;
+      const int64_t nb = (p.len + BLOCK - 1) / BLOCK;
       p.j0 = (int)(nb * split_ / a_.splits), p.j1 = (int)(nb * (split_ + 1) / a_.splits);
       return true;
     }
@@ -102,7 +111,7 @@ class Passes {
 };
 // The first state of a block.
 __device__ __forceinline__ int block_at(const Pass& p, int j) {
-  return p.lo + ((j + 1) * TILE > p.len ? p.len - TILE : j * TILE);
+  return p.lo + ((int64_t)(j + 1) * BLOCK > p.len ? p.len - BLOCK : j * BLOCK);
 }
 
 __device__ __forceinline__ void give_up(Bars* s, unsigned long long* err) {
@@ -124,9 +133,10 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     if (threadIdx.x == 0) atomicAdd(p.err, 1ull);
     return;
   }
-  const uint32_t q_s = base, k_s = q_s + NA * ATOM, v_s = k_s + STAGES * NA * ATOM, p_s = v_s + STAGES * NA * ATOM;
-  Bars* bars = reinterpret_cast<Bars*>(smem + (NA * (1 + 2 * STAGES) + 2) * ATOM);
-  const uint32_t s_full = smem_u32(&bars->s_full), p_full = smem_u32(&bars->p_full), o_done = smem_u32(&bars->o_done);
+  const uint32_t q_s = base, p_s = q_s + NA * ATOM_Q, k_s = p_s + 2 * ATOM_Q, v_s = k_s + STAGES * NA * ATOM;
+  Bars* bars = reinterpret_cast<Bars*>(smem + smem_bytes<NA>() - 256);
+  const uint32_t s_full = smem_u32(bars->s_full), p_full = smem_u32(bars->p_full), p_free = smem_u32(bars->p_free);
+  const uint32_t o_done = smem_u32(&bars->o_done);
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) {
       mbar_init(smem_u32(&bars->k_full[i]), 1);
@@ -134,8 +144,11 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
       mbar_init(smem_u32(&bars->v_full[i]), 1);
       mbar_init(smem_u32(&bars->v_free[i]), 1);
     }
-    mbar_init(s_full, 1);
-    mbar_init(p_full, 128);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_full + 8 * i, 128);
+      mbar_init(p_free + 8 * i, 1);
+    }
     mbar_init(o_done, 1);
     mbar_init(smem_u32(&bars->drained), 1);
     bars->abort_flag = 0;
@@ -151,7 +164,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     uint4 u = make_uint4(0, 0, 0, 0);
     if (row < rows && e * 8 < a.D)
       u = *reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(row / a.G) * a.qs + (hk * a.G + row % a.G) * a.D + e * 8);
-    const uint32_t at = q_s + (e >> 3) * ATOM + r * 128 + (((e & 7) ^ (r & 7)) << 4);
+    const uint32_t at = q_s + (e >> 3) * ATOM_Q + r * 128 + (((e & 7) ^ (r & 7)) << 4);
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"((u.x & a.q_and) ^ a.q_xor),
                  "r"((u.y & a.q_and) ^ a.q_xor), "r"((u.z & a.q_and) ^ a.q_xor), "r"((u.w & a.q_and) ^ a.q_xor)
                  : "memory");
@@ -160,7 +173,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = bars->tmem, tmem_o = tmem + TILE;
+  const uint32_t tmem = bars->tmem, tmem_o = tmem + 2 * BLOCK;   // after the two places of S
   volatile int* abort = &bars->abort_flag;
   Passes passes(a, row0, split, lane);
   Pass ps;
@@ -204,32 +217,43 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
   } else if (warp == 5) {
     // ---- products
     if (elect_one()) {
-      uint32_t n = 0;
+      uint32_t n = 0;                                  // blocks of the passes before
       bool ok = true;
+      // the scores of block m of all, in place m & 1 (whose scores before have been read: their
+      // weights have been waited for)
+      auto scores = [&](uint32_t m) {
+        const int s = m % STAGES;
+        ok = mbar_wait(smem_u32(&bars->k_full[s]), m / STAGES & 1, abort, LIMIT_NS);
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t ks = k_s + s * NA * ATOM;
+        for (int c = 0; c < NA; ++c)
+          for (int k = 0; k < 4; ++k)
+            umma_f16(tmem + (m & 1) * BLOCK, sdesc_sw128(q_s + c * ATOM_Q + 32 * k, 16, 1024),
+                     sdesc_sw128(ks + c * ATOM + 32 * k, 16, 1024), p.idesc_s, c | k);
+        umma_commit(s_full + 8 * (m & 1));
+        umma_commit(smem_u32(&bars->k_free[s]));
+      };
       while (ok && passes.next(ps)) {
-        for (int j = ps.j0; j < ps.j1; ++j, ++n) {
-          const int s = n % STAGES;
-          const uint32_t ph = n / STAGES & 1;
-          ok = mbar_wait(smem_u32(&bars->k_full[s]), ph, abort, LIMIT_NS);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t ks = k_s + s * NA * ATOM, vs = v_s + s * NA * ATOM;
-          for (int c = 0; c < NA; ++c)
-            for (int k = 0; k < 4; ++k)
-              umma_f16(tmem, sdesc_sw128(q_s + c * ATOM + 32 * k, 16, 1024), sdesc_sw128(ks + c * ATOM + 32 * k, 16, 1024),
-                       p.idesc_s, c | k);
-          umma_commit(s_full);
-          umma_commit(smem_u32(&bars->k_free[s]));
-          ok = mbar_wait(p_full, n & 1, abort, LIMIT_NS) && mbar_wait(smem_u32(&bars->v_full[s]), ph, abort, LIMIT_NS);
+        const uint32_t blocks = ps.j1 - ps.j0;
+        if (blocks > 0) scores(n);
+        for (uint32_t j = 0; j < blocks && ok; ++j) {
+          const uint32_t m = n + j;
+          const int s = m % STAGES;
+          if (j + 1 < blocks) scores(m + 1);
+          ok = ok && mbar_wait(p_full + 8 * (m & 1), m >> 1 & 1, abort, LIMIT_NS) &&
+               mbar_wait(smem_u32(&bars->v_full[s]), m / STAGES & 1, abort, LIMIT_NS);
           if (!ok) break;
           tc_fence_after();
           // V as it lies, [state][channel]: groups of 8 states 1024 bytes apart, 64 channels ATOM
-          for (int k = 0; k < 8; ++k)
-            umma_f16(tmem_o, sdesc_sw128(p_s + (k >> 2) * ATOM + 32 * (k & 3), 16, 1024), sdesc_sw128(vs + k * 2048, ATOM, 1024),
-                     p.idesc_o, (j > ps.j0) | (k > 0));
+          for (int k = 0; k < BLOCK / 16; ++k)
+            umma_f16(tmem_o, sdesc_sw128(p_s + (m & 1) * ATOM_Q + 32 * k, 16, 1024),
+                     sdesc_sw128(v_s + s * NA * ATOM + k * 2048, ATOM, 1024), p.idesc_o, (j > 0) | (k > 0));
+          umma_commit(p_free + 8 * (m & 1));
           umma_commit(smem_u32(&bars->v_free[s]));
-          if (j + 1 == ps.j1) umma_commit(o_done);
+          if (j + 1 == blocks) umma_commit(o_done);
         }
+        n += blocks;
       }
       if (!ok) give_up(bars, p.err);
       // products still under way end before their memory is given back
@@ -247,77 +271,72 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     while (ok && passes.next(ps)) {
       float m = -INFINITY, l = 0.0f;                   // m: score * scale2 that the weights are taken against
       for (int j = ps.j0; j < ps.j1; ++j, ++n) {
-        ok = __all_sync(FULL, mbar_wait(s_full, n & 1, abort, LIMIT_NS));
+        const uint32_t place = n & 1, phase = n >> 1 & 1;
+        ok = __all_sync(FULL, mbar_wait(s_full + 8 * place, phase, abort, LIMIT_NS));
         if (!ok) break;
         tc_fence_after();
-        const int twice = (j + 1) * TILE > ps.len ? (j + 1) * TILE - ps.len : 0;   // states that the block before had
-        float top = -INFINITY;
+        float v[2][32];
+        tmem_ld32(tmem + lanes + place * BLOCK, v[0]);
+        tmem_ld32(tmem + lanes + place * BLOCK + 32, v[1]);
+        tmem_ld_wait();
+        if ((int64_t)(j + 1) * BLOCK > ps.len) {       // the last block: states that the one before had
+          const int twice = (int)((int64_t)(j + 1) * BLOCK - ps.len);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float v[32];
-          tmem_ld32(tmem + lanes + 32 * c, v);
-          tmem_ld_wait();
-          if (twice > 32 * c) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (32 * c + i < twice) v[i] = -INFINITY;
-          }
-          float t0 = v[0], t1 = v[1], t2 = v[2], t3 = v[3];
-#pragma unroll
-          for (int i = 4; i < 32; i += 4)
-            t0 = fmaxf(t0, v[i]), t1 = fmaxf(t1, v[i + 1]), t2 = fmaxf(t2, v[i + 2]), t3 = fmaxf(t3, v[i + 3]);
-          top = fmaxf(top, fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)));
+          for (int i = 0; i < BLOCK; ++i)
+            if (i < twice) v[i / 32][i % 32] = -INFINITY;
         }
-        top *= a.scale2;
+        float t0 = v[0][0], t1 = v[0][1], t2 = v[0][2], t3 = v[0][3];
+#pragma unroll
+        for (int i = 4; i < BLOCK; i += 4) {
+          t0 = fmaxf(t0, v[i / 32][i % 32]), t1 = fmaxf(t1, v[i / 32][i % 32 + 1]);
+          t2 = fmaxf(t2, v[i / 32][i % 32 + 2]), t3 = fmaxf(t3, v[i / 32][i % 32 + 3]);
+        }
+        const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * a.scale2;
         if (j == ps.j0) {
           m = top;
         } else {
           const bool move = top > m + LAG;
           if (__any_sync(FULL, move)) {
+            // the product before this block adds to O until then
+            ok = __all_sync(FULL, mbar_wait(p_free + 8 * (place ^ 1), (n - 1) >> 1 & 1, abort, LIMIT_NS));
+            if (!ok) break;
+            tc_fence_after();
             const float f = move ? ex2(m - top) : 1.0f;
             if (move) m = top;
             l *= f;
 #pragma unroll 1
-            for (int c = 0; c < NA * 2; ++c) {
-              float v[32];
-              tmem_ld32(tmem_o + lanes + 32 * c, v);
+            for (int c = 0; c < NA * 4; ++c) {
+              float o[16];
+              tmem_ld16(tmem_o + lanes + 16 * c, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] *= f;
-              tmem_st32(tmem_o + lanes + 32 * c, v);
+              for (int i = 0; i < 16; ++i) o[i] *= f;
+              tmem_st16(tmem_o + lanes + 16 * c, o);
             }
             tmem_st_wait();
           }
         }
         const float mm = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float v[32];
-          tmem_ld32(tmem + lanes + 32 * c, v);
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = ex2(fmaf(v[i], a.scale2, -mm));
-          if (twice > 32 * c) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (32 * c + i < twice) v[i] = 0.0f;
-          }
-          float t0 = 0.0f, t1 = 0.0f, t2 = 0.0f, t3 = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) t0 += v[i], t1 += v[i + 1], t2 += v[i + 2], t3 += v[i + 3];
-          l += (t0 + t1) + (t2 + t3);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t at = p_s + (c >> 1) * ATOM + r * 128 + ((((c & 1) * 4 + i) ^ (r & 7)) << 4);
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack2(v[8 * i], v[8 * i + 1], T())),
-                         "r"(pack2(v[8 * i + 2], v[8 * i + 3], T())), "r"(pack2(v[8 * i + 4], v[8 * i + 5], T())),
-                         "r"(pack2(v[8 * i + 6], v[8 * i + 7], T()))
-                         : "memory");
-          }
+        if (n >= 2) {                                  // the weights' place is free
+          ok = __all_sync(FULL, mbar_wait(p_free + 8 * place, phase ^ 1, abort, LIMIT_NS));
+          if (!ok) break;
         }
+        float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = ex2(fmaf(v[c / 4][c % 4 * 8 + i], a.scale2, -mm));
+          s0 += x[0] + x[4], s1 += x[1] + x[5], s2 += x[2] + x[6], s3 += x[3] + x[7];
+          const uint32_t at = p_s + place * ATOM_Q + r * 128 + ((c ^ (r & 7)) << 4);
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack2(x[0], x[1], T())),
+                       "r"(pack2(x[2], x[3], T())), "r"(pack2(x[4], x[5], T())), "r"(pack2(x[6], x[7], T()))
+                       : "memory");
+        }
+        l += (s0 + s1) + (s2 + s3);
         fence_proxy_async_smem();
         tc_fence_before();
-        mbar_arrive(p_full);
+        mbar_arrive(p_full + 8 * place);
       }
       if (!ok) break;
       const bool mine = r >= ps.first && r < ps.last, any = ps.j1 > ps.j0;
@@ -378,14 +397,14 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// [rows][heads][D] with a row stride, boxes of 64 channels of a head and 128 rows, 128-byte swizzle;
+// [rows][heads][D] with a row stride, boxes of 64 channels of a head and 64 rows, 128-byte swizzle;
 // channels from D on and rows beyond the array read as zero.
 bool make_map(CUtensorMap* m, const void* p, int64_t rows, int64_t stride, int heads, int D, bool fp16) {
   auto fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)rows};
   const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
-  const cuuint32_t box[3] = {64, 1, TILE}, step[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, 1, BLOCK}, step[3] = {1, 1, 1};
   return fn(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims,
             strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -412,7 +431,7 @@ int launch(const CaArgs& a, bool fp16, cudaStream_t st) {
   TcArgs p;
   p.a = a;
   p.tiles = (int)((a.nq * a.G + TILE - 1) / TILE);
-  p.idesc_s = idesc_f16(128, 128, fp16 ? 0u : 1u, false, false);
+  p.idesc_s = idesc_f16(128, BLOCK, fp16 ? 0u : 1u, false, false);
   p.idesc_o = idesc_f16(128, NA * 64, fp16 ? 0u : 1u, false, true);
   cudaError_t e = expired_address(&p.err);
   if (e != cudaSuccess) return tf_status_from_cuda(e);

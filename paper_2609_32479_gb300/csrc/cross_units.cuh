@@ -69,7 +69,7 @@ __device__ __forceinline__ int first_wanted(int pos, int lo0, int hi0, int lo1, 
 int cross_mma(int32_t dtype, const CaArgs& a, cudaStream_t st);
 int cross_tf32(const CaArgs& a, cudaStream_t st);
 // cross_tc.cu: sequences of at least CROSS_TC_FROM states, 128 rows at a time.
-constexpr int CROSS_TC_FROM = 128;
+constexpr int CROSS_TC_FROM = 64;
 int cross_tc(int32_t dtype, const CaArgs& a, cudaStream_t st);
 
 }  // namespace seqops
