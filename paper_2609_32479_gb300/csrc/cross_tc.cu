@@ -287,11 +287,14 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
         }
         float t0 = v[0][0], t1 = v[0][1], t2 = v[0][2], t3 = v[0][3];
 #pragma unroll
-        for (int i = 4; i < BLOCK; i += 4) {
-          t0 = fmaxf(t0, v[i / 32][i % 32]), t1 = fmaxf(t1, v[i / 32][i % 32 + 1]);
-          t2 = fmaxf(t2, v[i / 32][i % 32 + 2]), t3 = fmaxf(t3, v[i / 32][i % 32 + 3]);
+        for (int i = 4; i < BLOCK - 4; i += 8) {
+          t0 = max3(t0, v[i / 32][i % 32], v[(i + 1) / 32][(i + 1) % 32]);
+          t1 = max3(t1, v[(i + 2) / 32][(i + 2) % 32], v[(i + 3) / 32][(i + 3) % 32]);
+          t2 = max3(t2, v[(i + 4) / 32][(i + 4) % 32], v[(i + 5) / 32][(i + 5) % 32]);
+          t3 = max3(t3, v[(i + 6) / 32][(i + 6) % 32], v[(i + 7) / 32][(i + 7) % 32]);
         }
-        const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * a.scale2;
+        t0 = max3(t0, v[1][28], v[1][29]), t1 = max3(t1, v[1][30], v[1][31]);
+        const float top = fmaxf(max3(t0, t1, t2), t3) * a.scale2;
         if (j == ps.j0) {
           m = top;
         } else {
@@ -321,19 +324,25 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
           ok = __all_sync(FULL, mbar_wait(p_free + 8 * place, phase ^ 1, abort, LIMIT_NS));
           if (!ok) break;
         }
-        float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+        const uint64_t scale = both(a.scale2, a.scale2), minus = both(-mm, -mm);
+        uint64_t s0 = 0, s1 = 0;
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-          float x[8];
+          uint32_t w[4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = ex2(fmaf(v[c / 4][c % 4 * 8 + i], a.scale2, -mm));
-          s0 += x[0] + x[4], s1 += x[1] + x[5], s2 += x[2] + x[6], s3 += x[3] + x[7];
+          for (int i = 0; i < 4; ++i) {
+            const int e = c % 4 * 8 + 2 * i;
+            float2 x = parts(fma2(both(v[c / 4][e], v[c / 4][e + 1]), scale, minus));
+            x.x = ex2(x.x), x.y = ex2(x.y);
+            if (i & 1) s1 = add2(s1, both(x.x, x.y));
+            else s0 = add2(s0, both(x.x, x.y));
+            w[i] = pack2(x.x, x.y, T());
+          }
           const uint32_t at = p_s + place * ATOM_Q + r * 128 + ((c ^ (r & 7)) << 4);
-          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack2(x[0], x[1], T())),
-                       "r"(pack2(x[2], x[3], T())), "r"(pack2(x[4], x[5], T())), "r"(pack2(x[6], x[7], T()))
-                       : "memory");
+          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
         }
-        l += (s0 + s1) + (s2 + s3);
+        const float2 sum = parts(add2(s0, s1));
+        l += sum.x + sum.y;
         fence_proxy_async_smem();
         tc_fence_before();
         mbar_arrive(p_full + 8 * place);
