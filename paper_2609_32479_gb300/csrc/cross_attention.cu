@@ -88,7 +88,7 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
   if (!heads_ok(q_heads) || !heads_ok(kv_heads) || q_heads % kv_heads != 0 || !dim_ok(head_dim))
     return TRACKFIT_ERR_UNSUPPORTED;
   if (n_q_rows > MOST_ROWS / (q_heads / kv_heads) || n_kv_rows > MOST_ROWS) return TRACKFIT_ERR_UNSUPPORTED;
-  if (!isfinite(scale)) return TRACKFIT_ERR_INVALID_ARG;
+  if (!isfinite(scale * LOG2E)) return TRACKFIT_ERR_INVALID_ARG;
   if (n_seq == 0 || n_q_rows == 0) return TRACKFIT_OK;
   const int sz = type_size(dtype);
   if (!q_offsets || !kv_offsets || ((reinterpret_cast<uintptr_t>(q_offsets) | reinterpret_cast<uintptr_t>(kv_offsets)) & 7u))

@@ -50,7 +50,6 @@ struct TcArgs {
   CaArgs a;
   int tiles;
   uint32_t idesc_s, idesc_o;
-  unsigned long long* err;
 };
 
 struct Bars {
@@ -114,8 +113,10 @@ __device__ __forceinline__ int block_at(const Pass& p, int j) {
   return p.lo + ((int64_t)(j + 1) * BLOCK > p.len ? p.len - BLOCK : j * BLOCK);
 }
 
-__device__ __forceinline__ void give_up(Bars* s, unsigned long long* err) {
-  if (atomicExch(&s->abort_flag, 1) == 0) atomicAdd(err, 1ull);
+__device__ unsigned long long g_expired;   // CTAs that gave up, since trackfit_operator_errors last asked
+
+__device__ __forceinline__ void give_up(Bars* s) {
+  if (atomicExch(&s->abort_flag, 1) == 0) atomicAdd(&g_expired, 1ull);
 }
 
 template <class T, int NA>
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
   const int rows = (int)(a.nq * a.G);
   const uint32_t base = smem_u32(smem);
   if (base & 1023u) {                                  // the swizzled tiles' alignment, asked for above
-    if (threadIdx.x == 0) atomicAdd(p.err, 1ull);
+    if (threadIdx.x == 0) atomicAdd(&g_expired, 1ull);
     return;
   }
   const uint32_t q_s = base, p_s = q_s + NA * ATOM_Q, k_s = p_s + 2 * ATOM_Q, v_s = k_s + STAGES * NA * ATOM;
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
           for (int c = 0; c < NA; ++c) tma_load_3d(v_s + (s * NA + c) * ATOM, &tv, vf, 64 * c, hk, row);
         }
       }
-      if (!ok) give_up(bars, p.err);
+      if (!ok) give_up(bars);
       // copies still under way land before the CTA exits (after a failure nobody else waits for them)
       volatile int never = 0;
       for (uint32_t i = n < STAGES ? 0 : n - STAGES; i < n; ++i) {
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
         }
         n += blocks;
       }
-      if (!ok) give_up(bars, p.err);
+      if (!ok) give_up(bars);
       // products still under way end before their memory is given back
       volatile int never = 0;
       umma_commit(smem_u32(&bars->drained));
@@ -385,14 +386,12 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
         }
       }
     }
-    if (!ok) give_up(bars, p.err);
+    if (!ok) give_up(bars);
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 5) tmem_dealloc(tmem, 256);
 }
-
-__device__ unsigned long long g_expired;   // waits that ran out, of all operators
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
@@ -419,22 +418,6 @@ bool make_map(CUtensorMap* m, const void* p, int64_t rows, int64_t stride, int h
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The address of g_expired on the current device.
-cudaError_t expired_address(unsigned long long** out) {
-  static std::atomic<unsigned long long*> known[64];
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  unsigned long long* p = dev < 64 ? known[dev].load() : nullptr;
-  if (!p) {
-    e = cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_expired);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) known[dev].store(p);
-  }
-  *out = p;
-  return cudaSuccess;
-}
-
 template <class T, int NA>
 int launch(const CaArgs& a, bool fp16, cudaStream_t st) {
   TcArgs p;
@@ -442,13 +425,11 @@ int launch(const CaArgs& a, bool fp16, cudaStream_t st) {
   p.tiles = (int)((a.nq * a.G + TILE - 1) / TILE);
   p.idesc_s = idesc_f16(128, BLOCK, fp16 ? 0u : 1u, false, false);
   p.idesc_o = idesc_f16(128, NA * 64, fp16 ? 0u : 1u, false, true);
-  cudaError_t e = expired_address(&p.err);
-  if (e != cudaSuccess) return tf_status_from_cuda(e);
   CUtensorMap tk, tv;
   if (!make_map(&tk, a.k, a.nk, a.ks, a.Hk, a.D, fp16) || !make_map(&tv, a.v, a.nk, a.vs, a.Hk, a.D, fp16))
     return TRACKFIT_ERR_CUDA;
   constexpr auto kern = ca_tc_kernel<T, NA>;
-  e = allow_smem<kern>(smem_bytes<NA>());
+  const cudaError_t e = allow_smem<kern>(smem_bytes<NA>());
   if (e != cudaSuccess) return tf_status_from_cuda(e);
   const int64_t units = (int64_t)p.tiles * a.Hk * a.splits;
   if (units > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
@@ -467,9 +448,9 @@ int seqops::cross_tc(int32_t dtype, const CaArgs& a, cudaStream_t st) {
 extern "C" int trackfit_operator_errors(void* stream) {
   tf_nvtx_range nvtx_range("trackfit_operator_errors");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  unsigned long long* p = nullptr;
+  void* p = nullptr;
   unsigned long long n = 0;
-  cudaError_t e = expired_address(&p);
+  cudaError_t e = cudaGetSymbolAddress(&p, g_expired);
   if (e == cudaSuccess) e = cudaMemcpyAsync(&n, p, sizeof(n), cudaMemcpyDeviceToHost, st);
   if (e == cudaSuccess) e = cudaMemsetAsync(p, 0, sizeof(n), st);
   if (e == cudaSuccess) e = cudaStreamSynchronize(st);

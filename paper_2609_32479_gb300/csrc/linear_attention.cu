@@ -17,18 +17,25 @@ using namespace seqops;
 // k are the same for all columns and come from shared memory as broadcasts, 8 rows at a time
 // through a ring that the warp fills by asynchronous copies.  Several columns a lane share what a
 // row costs whatever its columns (loads, exponential, addresses: 90 of 116 instructions with one).
-constexpr int CH = 8, NST = 3;
+constexpr int CH = 8, NST = 2;
 
 template <int DK, int CPL>
 struct __align__(16) SimtSlot {
   float q[CH][DK], k[CH][DK], v[CH][16 * CPL];
   float g[CH];
   int row, seq, flags, pad;      // the chunk, its first row in the direction of the recurrence
+  // behind it, where sequences begin with a state: the state's columns of a piece's first chunk,
+  // [K][16 CPL] (loaded when the chunk came up, they kept the warps waiting half of the time)
+  __device__ float* state() { return reinterpret_cast<float*>(this + 1); }
 };
+template <int DK, int CPL>
+inline int simt_slot_bytes(const LaArgs& a) {
+  return (int)sizeof(SimtSlot<DK, CPL>) + (a.state_in || a.bounds > 1 ? a.K * 16 * CPL * 4 : 0);
+}
 enum { LEN = 0xff, FIRST = 0x100, LAST = 0x200, GOES_ON = 0x400, ENDS = 0x800, NONE = 0x1000 };
 
 template <int DK, int CPL, bool STATE_ONLY>
-__global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaArgs a) {
+__global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaArgs a, int slot_bytes) {
   extern __shared__ __align__(16) unsigned char smem[];
   using Slot = SimtSlot<DK, CPL>;
   constexpr int COLS = 16 * CPL;
@@ -36,13 +43,13 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   const unsigned unit = blockIdx.x;
   const int sl = (int)(unit % a.slices), h = (int)(unit / a.slices % a.H);
   const int64_t tile = unit / a.slices / a.H;
-  Slot* slots = reinterpret_cast<Slot*>(smem);
+  auto slot = [&](int s) -> Slot& { return *reinterpret_cast<Slot*>(smem + s * slot_bytes); };
   const int c0 = sl * COLS, width = a.V - c0 < COLS ? a.V - c0 : COLS;
   const int dir = a.u.reverse ? -1 : 1;
   constexpr int HALF = DK / 2;
   const int col = lane & 15, part = lane >> 4, i0 = part * HALF;   // this lane's columns: col + 16 j; first key channel
   // channels beyond K and V are zeros from here on: the copies leave them alone
-  for (uint32_t* p = reinterpret_cast<uint32_t*>(slots) + lane; p < reinterpret_cast<uint32_t*>(slots + NST); p += 32) *p = 0;
+  for (int i = lane * 4; i < NST * slot_bytes; i += 128) *reinterpret_cast<uint32_t*>(smem + i) = 0;
   __syncwarp();
 
   const int64_t base = STATE_ONLY ? (tile + 1) * a.u.lseg : tile * a.u.seg;
@@ -61,6 +68,10 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
     more = pieces.next(p);
   }
   int done = 0;
+  const int64_t KV = (int64_t)a.K * a.V;
+  auto beginning = [&](bool goes_on, bool ends, int seq, int row) {
+    return piece_begins_with(a, base, row, seq, h, goes_on, ends, STATE_ONLY);
+  };
 
   auto issue = [&](Slot& w) {
     if (more) {
@@ -86,6 +97,14 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
         if (e < width) copy16(smem_addr(&w.v[r][e]), v + (int64_t)(row + dir * r) * a.vs + e, r < len);
       }
       if (lane < CH) copy4(smem_addr(&w.g[lane]), gr + (int64_t)(row + dir * lane) * a.gs, lane < len);
+      if (done == 0) {
+        if (const float* src = beginning(p.goes_on, p.ends, p.seq, row)) {
+          for (int i = lane; i < a.K * (COLS / 4); i += 32) {
+            const int r = i / (COLS / 4), e = i % (COLS / 4) * 4;
+            if (e < width) copy16(smem_addr(w.state() + 4 * i), src + r * a.V + c0 + e, true);
+          }
+        }
+      }
       done += len;
       if (left <= CH) {
         done = 0;
@@ -97,32 +116,39 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
     copy_commit();
   };
 
-  for (int s = 0; s < NST; ++s) issue(slots[s]);
+  for (int s = 0; s < NST; ++s) issue(slot(s));
   uint64_t S[CPL][HALF / 2];
 #pragma unroll
   for (int j = 0; j < CPL; ++j)
 #pragma unroll
     for (int i = 0; i < HALF / 2; ++i) S[j][i] = 0;
+  auto put_state = [&](float* st) {
+#pragma unroll
+    for (int j = 0; j < CPL; ++j)
+#pragma unroll
+      for (int i = 0; i < HALF; i += 2)
+        if (col + 16 * j < width && i0 + i < a.K) {
+          const float2 s2 = parts(S[j][i / 2]);
+          float* d = st + (i0 + i) * a.V + c0 + col + 16 * j;
+          d[0] = s2.x, d[a.V] = s2.y;
+        }
+  };
   float total = 0.0f;
-  const int64_t KV = (int64_t)a.K * a.V;
   for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
-    Slot& w = slots[s];
+    Slot& w = slot(s);
     copy_wait<NST - 1>();
     __syncwarp();
     const int flags = w.flags, row = w.row, seq = w.seq, len = flags & LEN;
     if (flags & NONE) break;
     if (flags & FIRST) {
-      const float* st = nullptr;
-      if (flags & GOES_ON)
-        st = STATE_ONLY ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
-      else if (a.state_in)
-        st = a.state_in + ((int64_t)seq * a.H + h) * KV;
-      if (st) st += i0 * a.V + c0 + col;
+      const bool st = beginning(flags & GOES_ON, flags & ENDS, seq, row) != nullptr;
+      const float* src = w.state() + i0 * COLS + col;
 #pragma unroll
       for (int j = 0; j < CPL; ++j)
 #pragma unroll
         for (int i = 0; i < HALF; i += 2)
-          S[j][i / 2] = st && col + 16 * j < width && i0 + i < a.K ? both(st[i * a.V + 16 * j], st[(i + 1) * a.V + 16 * j]) : 0;
+          S[j][i / 2] = st && i0 + i < a.K ? both(src[i * COLS + 16 * j], src[(i + 1) * COLS + 16 * j]) : 0;
+      if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) put_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);
     }
     for (int r = 0; r < len; ++r) {
       const float e = expf(w.g[r]);
@@ -161,16 +187,7 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
       }
     }
     if ((flags & LAST) && (STATE_ONLY || ((flags & ENDS) && a.state_out))) {
-      float* st = STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV;
-#pragma unroll
-      for (int j = 0; j < CPL; ++j)
-#pragma unroll
-        for (int i = 0; i < HALF; i += 2)
-          if (col + 16 * j < width && i0 + i < a.K) {
-            const float2 s2 = parts(S[j][i / 2]);
-            float* d = st + (i0 + i) * a.V + c0 + col + 16 * j;
-            d[0] = s2.x, d[a.V] = s2.y;
-          }
+      put_state(STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV);
       if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
     }
     __syncwarp();
@@ -300,15 +317,14 @@ size_t workspace_bytes(int64_t n_rows, int64_t n_seq, int H, int K, int V) {
   const int l = rows_a_boundary(n_rows, H, V);
   const size_t bounds = (size_t)((n_rows + l - 1) / l);
   const size_t flags = (bounds * 4 + 15) / 16 * 16, decay = (bounds * H * 4 + 15) / 16 * 16;
-  return flags + decay + bounds * H * (size_t)K * V * 4;
+  return flags + decay + 2 * bounds * H * (size_t)K * V * 4;   // (the second: states in place)
 }
 
 template <int DK, int CPL, bool STATE_ONLY>
 int launch_simt(const LaArgs& a, cudaStream_t st) {
-  const size_t sm = sizeof(SimtSlot<DK, CPL>) * NST;
-  auto kern = la_simt_kernel<DK, CPL, STATE_ONLY>;
-  static_assert(sizeof(SimtSlot<DK, CPL>) * NST <= 48 * 1024, "needs no leave");
-  kern<<<linear_grid(a, STATE_ONLY), 32, sm, st>>>(a);
+  const int bytes = simt_slot_bytes<DK, CPL>(a);
+  static_assert((sizeof(SimtSlot<DK, CPL>) + DK * 16 * CPL * 4) * NST <= 48 * 1024, "needs no leave");
+  la_simt_kernel<DK, CPL, STATE_ONLY><<<linear_grid(a, STATE_ONLY), 32, NST * bytes, st>>>(a, bytes);
   return launched();
 }
 // Columns a lane, at most 64 registers of state, the slices alike.
@@ -387,6 +403,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
   if (n_rows / n_seq >= LONGEST) a.u.seg = a.u.lseg;
   a.u.tiles = n_rows > 0 ? (n_rows + a.u.seg - 1) / a.u.seg : 1;
   a.bounds = 1;
+  a.ws_begin = nullptr;
   if (a.u.tiles > (int64_t)0x7fffffff / (n_heads * a.slices)) return TRACKFIT_ERR_UNSUPPORTED;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (need > 0) {
@@ -397,6 +414,7 @@ extern "C" int trackfit_linear_attention(int32_t dtype, const void* q, int64_t q
     a.ws_decay = reinterpret_cast<float*>(w);
     w += (a.bounds * n_heads * 4 + 15) / 16 * 16;
     a.ws_state = reinterpret_cast<float*>(w);
+    if (state_in && state_in == state_out) a.ws_begin = a.ws_state + a.bounds * n_heads * key_dim * value_dim;
     if (a.bounds > 1) {
       int rc = run<true>(dtype, a, st);
       if (rc != TRACKFIT_OK) return rc;

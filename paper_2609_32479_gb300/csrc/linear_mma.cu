@@ -291,13 +291,10 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
     x *= LOG2E;
     x = x < -150.0f ? -150.0f : x;
     if (flags & FIRST) {
-      const float* src = nullptr;
-      if (flags & GOES_ON)
-        src = STATE_ONLY ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
-      else if (a.state_in)
-        src = a.state_in + ((int64_t)ch.seq * a.H + h) * KV;
+      const float* src = piece_begins_with(a, base, row, ch.seq, h, flags & GOES_ON, flags & ENDS, STATE_ONLY);
       zero = src == nullptr;
       if (!zero) load_state(src);
+      if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) store_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);
     }
     if (STATE_ONLY) total += x;                        // summed over lanes at the end
     float P = x;

@@ -131,6 +131,10 @@ struct LaArgs {
   const float* state_in;
   float* state_out;
   float* ws_state;               // [boundaries][H][K][V]
+  // states in place only, else null: [boundaries][H][K][V], the state that the cut sequence whose
+  // first piece ends at the boundary begins with (its last piece may be done first, and put the
+  // state after the sequence in its place)
+  float* ws_begin;
   float* ws_decay;               // [boundaries][H], sums of g
   int32_t* ws_flag;              // [boundaries]: 0 no cut sequence, 1 its first piece, 2 a later one
   int64_t bounds;                // boundaries 1 .. bounds - 1
@@ -143,6 +147,16 @@ struct LaArgs {
 // are given out by the warp.
 inline unsigned linear_grid(const LaArgs& a, bool state_only) {
   return (unsigned)((state_only ? a.bounds - 1 : a.u.tiles) * a.H * a.slices);
+}
+
+// Where the state that a piece begins with stands, null for zeros.  `row`: its first row in the
+// direction of the recurrence, from `base`.
+__device__ __forceinline__ const float* piece_begins_with(const LaArgs& a, int64_t base, int row, int seq, int h, bool goes_on,
+                                                          bool ends, bool state_only) {
+  const int64_t KV = (int64_t)a.K * a.V;
+  if (goes_on) return state_only ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
+  if (a.ws_begin && !ends && !state_only) return a.ws_begin + (((base + row) / a.u.lseg + 1 - a.u.reverse) * a.H + h) * KV;
+  return a.state_in ? a.state_in + ((int64_t)seq * a.H + h) * KV : nullptr;
 }
 
 // linear_mma.cu: the 16-bit types on the tensor cores.  Channels of v that a warp takes:

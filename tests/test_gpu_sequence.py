@@ -251,6 +251,25 @@ def test_linear_states_in_place_and_in_parts(T, t):
     hold(s2, s, ts)
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rev", [False, True])
+def test_linear_states_in_place_of_long_sequences(T, t, rev):
+    """The parts of a long sequence run in any order: its first part still begins with the state
+    before the call, though the last part may put the state after it in the same place.  (More
+    parts than the GPU holds at a time, the first in the recurrence's direction last.)"""
+    H, K, n = 8, 64, 200000 if t != "float32" else 60000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn((n, H, K), generator=g, device="cuda").to(getattr(torch, t)) for _ in range(3))
+    d = -0.02 * torch.rand((n, H), generator=g, device="cuda")
+    off = dev([0, 600, n - 700, n], "int64")
+    s0 = 10 * torch.randn((3, H, K, K), generator=g, device="cuda")
+    s1, s2 = torch.empty_like(s0), s0.clone()
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    T.linear_attention(q, k, v, d, off, a, reverse=rev, state_in=s0, state_out=s1)
+    T.linear_attention(q, k, v, d, off, b, reverse=rev, state_in=s2, state_out=s2)
+    assert torch.equal(s1, s2) and torch.equal(a, b)
+
+
 def test_linear_is_the_same_wherever_a_sequence_stands(T):
     """Bit for bit: the other sequences of a batch, their order and number do not matter."""
     r = np.random.default_rng(7)
