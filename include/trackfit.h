@@ -406,7 +406,9 @@ int trackfit_forward_noalloc(const trackfit_config_t* cfg, const float* weights,
  * vectors 4-byte, int64 ones 8-byte aligned.  Widths of heads are multiples of 8 up to
  * 128, heads at most 256.  Outputs may not overlap inputs unless a function says so;
  * rows that belong to no sequence are neither read nor written.  Offsets that break the
- * rule leave the outputs undefined, but no access leaves the arrays.
+ * rule leave the outputs undefined, but no access leaves the arrays.  What is not finite
+ * in a row stays in its sequence (and in linear attention out of the rows before it);
+ * infinities may come out as NaN.
  * Asynchronous on `stream`, whose device is the current one and holds the arrays; no
  * allocation, no host synchronisation; capturable.  Calls that may run at the same time
  * need workspaces of their own (as two graphs that are replayed side by side do).
@@ -435,7 +437,8 @@ int trackfit_qk_norm(int32_t dtype, const void* q, int64_t q_stride, int32_t q_h
  * with S of key_dim x value_dim: the gated recurrence of Eq. 2 with a matrix for a state.
  *   q, k        [n_rows][n_heads][key_dim]; v, out [n_rows][n_heads][value_dim].
  *   log_decay   device fp32 [n_rows][decay_stride], the first n_heads of a row used: g,
- *               meant to be <= 0; -inf forgets all that was before.
+ *               at most 0 (fp16 rows scaled up by a larger one may leave their range);
+ *               -inf forgets all that was before.
  *   reverse     0: from a sequence's first row to its last; 1: from its last to its first.
  *   state_in    fp32 [n_seq][n_heads][key_dim][value_dim] to begin with, or NULL (zeros).
  *   state_out   the same shape, the state after each sequence, or NULL; may be state_in.
