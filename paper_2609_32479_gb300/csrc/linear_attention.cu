@@ -12,8 +12,8 @@ namespace {
 using namespace seqops;
 
 // ---------------------------------------------------------------- fp32, on the CUDA cores
-// A lane holds halves of CPL columns of S, K / 2 values each in registers, two to a 64-bit word for
-// the packed fp32 instructions; the lanes l and l + 16 have a column's halves.  The rows of q and
+// A lane holds halves of CPL columns of S, K / 2 values each in registers; the lanes l and l + 16
+// have a column's halves.  The rows of q and
 // k are the same for all columns and come from shared memory as broadcasts, 8 rows at a time
 // through a ring that the warp fills by asynchronous copies.  Several columns a lane share what a
 // row costs whatever its columns (loads, exponential, addresses: 90 of 116 instructions with one).
@@ -117,21 +117,29 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   };
 
   for (int s = 0; s < NST; ++s) issue(slot(s));
-  uint64_t S[CPL][HALF / 2];
+  float S[CPL][HALF];
 #pragma unroll
   for (int j = 0; j < CPL; ++j)
 #pragma unroll
-    for (int i = 0; i < HALF / 2; ++i) S[j][i] = 0;
+    for (int i = 0; i < HALF; ++i) S[j][i] = 0.0f;
+  // the state is exp(G) S: a row's decay goes into G, and its values are taken by exp(-G), which
+  // leaves two multiply-adds a value of the state and row; beyond e^FOLD the factor goes into S
+  float G = 0.0f;
+  constexpr float FOLD = 14.0f;
+  auto fold = [&] {
+    const float f = expf(G);
+    G = 0.0f;
+#pragma unroll
+    for (int j = 0; j < CPL; ++j)
+#pragma unroll
+      for (int i = 0; i < HALF; ++i) S[j][i] *= f;
+  };
   auto put_state = [&](float* st) {
 #pragma unroll
     for (int j = 0; j < CPL; ++j)
 #pragma unroll
-      for (int i = 0; i < HALF; i += 2)
-        if (col + 16 * j < width && i0 + i < a.K) {
-          const float2 s2 = parts(S[j][i / 2]);
-          float* d = st + (i0 + i) * a.V + c0 + col + 16 * j;
-          d[0] = s2.x, d[a.V] = s2.y;
-        }
+      for (int i = 0; i < HALF; ++i)
+        if (col + 16 * j < width && i0 + i < a.K) st[(i0 + i) * a.V + c0 + col + 16 * j] = S[j][i];
   };
   float total = 0.0f;
   for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
@@ -143,50 +151,49 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
     if (flags & FIRST) {
       const bool st = beginning(flags & GOES_ON, flags & ENDS, seq, row) != nullptr;
       const float* src = w.state() + i0 * COLS + col;
+      G = 0.0f;
 #pragma unroll
       for (int j = 0; j < CPL; ++j)
 #pragma unroll
-        for (int i = 0; i < HALF; i += 2)
-          S[j][i / 2] = st && i0 + i < a.K ? both(src[i * COLS + 16 * j], src[(i + 1) * COLS + 16 * j]) : 0;
+        for (int i = 0; i < HALF; ++i) S[j][i] = st && i0 + i < a.K ? src[i * COLS + 16 * j] : 0.0f;
       if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) put_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);
     }
     for (int r = 0; r < len; ++r) {
-      const float e = expf(w.g[r]);
-      const uint64_t ee = both(e, e);
-      uint64_t x[CPL], acc[CPL][2];
-#pragma unroll
-      for (int j = 0; j < CPL; ++j) {
-        x[j] = both(w.v[r][col + 16 * j], w.v[r][col + 16 * j]);
-        acc[j][0] = acc[j][1] = 0;
-      }
+      G += w.g[r];
       if (STATE_ONLY) total += w.g[r];
+      if (!(fabsf(G) <= FOLD)) fold();
+      const float in = expf(-G);
+      float x[CPL], acc[CPL][2];
+#pragma unroll
+      for (int j = 0; j < CPL; ++j) x[j] = in * w.v[r][col + 16 * j], acc[j][0] = acc[j][1] = 0.0f;
 #pragma unroll
       for (int i = 0; i < HALF; i += 4) {
-        const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(&w.k[r][i0 + i]);
-        ulonglong2 qq;
-        if (!STATE_ONLY) qq = *reinterpret_cast<const ulonglong2*>(&w.q[r][i0 + i]);
+        const float4 k4 = *reinterpret_cast<const float4*>(&w.k[r][i0 + i]);
+        const float kk[4] = {k4.x, k4.y, k4.z, k4.w};
+        float4 q4;
+        if (!STATE_ONLY) q4 = *reinterpret_cast<const float4*>(&w.q[r][i0 + i]);
+        const float qq[4] = {q4.x, q4.y, q4.z, q4.w};
 #pragma unroll
-        for (int j = 0; j < CPL; ++j) {
-          S[j][i / 2] = fma2(kk.x, x[j], mul2(ee, S[j][i / 2]));
-          S[j][i / 2 + 1] = fma2(kk.y, x[j], mul2(ee, S[j][i / 2 + 1]));
-          if (!STATE_ONLY) {
-            acc[j][0] = fma2(qq.x, S[j][i / 2], acc[j][0]);
-            acc[j][1] = fma2(qq.y, S[j][i / 2 + 1], acc[j][1]);
+        for (int j = 0; j < CPL; ++j)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            S[j][i + n] = fmaf(kk[n], x[j], S[j][i + n]);
+            if (!STATE_ONLY) acc[j][n & 1] = fmaf(qq[n], S[j][i + n], acc[j][n & 1]);
           }
-        }
       }
       if (!STATE_ONLY) {
         float* o = out + (int64_t)(row + dir * r) * a.os;
+        const float f = a.scale * expf(G);
 #pragma unroll
         for (int j = 0; j < CPL; ++j) {
-          const float2 o0 = parts(acc[j][0]), o1 = parts(acc[j][1]);
-          float y = (o0.x + o0.y) + (o1.x + o1.y);
+          float y = acc[j][0] + acc[j][1];
           y += __shfl_xor_sync(FULL, y, 16);
-          if (part == 0 && col + 16 * j < width) o[16 * j] = a.scale * y;
+          if (part == 0 && col + 16 * j < width) o[16 * j] = f * y;
         }
       }
     }
     if ((flags & LAST) && (STATE_ONLY || ((flags & ENDS) && a.state_out))) {
+      fold();
       put_state(STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV);
       if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
     }
