@@ -494,6 +494,13 @@ int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, con
  * OK. */
 int trackfit_operator_errors(void* stream);
 
+/* Test hook for the bounded waits of the operators' kernels (trackfit_cross_attention, 16-bit
+ * rows, many queries to many states), for the calls of the whole process from here on:
+ * limit_ns in (0, 2 s] replaces the 2 s limit (0 restores it); hold = 1 makes the first CTA's
+ * loader hold its first block back for twice the limit, or until a wait has given up, so that
+ * the waits for it expire (0: no hold).  Host side only; launches nothing. */
+int trackfit_debug_operator_wait(int64_t limit_ns, int32_t hold);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,9 +10,10 @@
 // Operands as in linear_mma.cu: 16 bytes a lane, channels 8t .. 8t+7 of each 32, rows g, g + 8,
 // ..., through a queue of each lane's own words in shared memory; movmatrix turns V.
 //
-// What bounds it: memory, for tracks and for single queries (a state's K and V are read once
-// for the G heads that share them; the products of 16 rows, most of them empty for a single
-// query, take a seventh of the time).  P is rounded to 16 bits once, as the operand of P V: an
+// What bounds it: for tracks the instructions (131,072 tracks of five queries, 4 heads of 32, bf16:
+// 317 us, 4.0 TB/s of the 6.8 that a copy moves), for single queries memory (a state's K and V are
+// read once for the G heads that share them: 61 queries over 1-16,384 states, 4 heads of 128: 184
+// us, 4.9 TB/s, with four warps an SM).  P is rounded to 16 bits once, as the operand of P V: an
 // error of the output's own rounding's size.
 #include "cross_units.cuh"
 #include "mma_sync.cuh"

@@ -29,7 +29,8 @@ EXPORTS = ("trackfit_weight_count", "trackfit_create", "trackfit_forward", "trac
            "trackfit_debug_schedule", "trackfit_debug_wait_limit", "trackfit_debug_alloc", "trackfit_seed",
            "trackfit_decode", "trackfit_forward_packed", "trackfit_last_error", "trackfit_qk_norm",
            "trackfit_linear_attention", "trackfit_linear_attention_workspace", "trackfit_linear_attention_step",
-           "trackfit_cross_attention", "trackfit_cross_attention_workspace", "trackfit_operator_errors")
+           "trackfit_cross_attention", "trackfit_cross_attention_workspace", "trackfit_operator_errors",
+           "trackfit_debug_operator_wait")
 
 
 class Config(ctypes.Structure):
@@ -128,6 +129,8 @@ def load() -> ctypes.CDLL:
     lib.trackfit_cross_attention.restype = ctypes.c_int
     lib.trackfit_operator_errors.argtypes = [vp]
     lib.trackfit_operator_errors.restype = ctypes.c_int
+    lib.trackfit_debug_operator_wait.argtypes = [i64, i32]
+    lib.trackfit_debug_operator_wait.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -569,3 +572,10 @@ def operator_errors(stream=None) -> int:
     """OK, or ERR_TIMEOUT when a bounded wait of an operator's kernel on the current device has
     expired since the last call (synchronises)."""
     return load().trackfit_operator_errors(_stream_handle(stream))
+
+
+def debug_operator_wait(limit_ns: int = 0, hold: bool = False) -> None:
+    """Test hook: the limit of the operators' bounded waits, and a first block held back."""
+    st = load().trackfit_debug_operator_wait(int(limit_ns), int(bool(hold)))
+    if st != OK:
+        raise TrackfitError(st, "trackfit_debug_operator_wait")

@@ -466,6 +466,26 @@ def test_cross_of_many_keeps_what_is_not_finite_to_its_sequence(T, t):
     assert not ok[100:190, 1, 3].any() and ok[100:190, 1, :3].all()
 
 
+def test_an_expired_wait_is_reported_and_the_next_call_is_right(T):
+    """A loader that holds its first block back: the waits for it give up after 20 ms, the call
+    returns, the error is reported once, and the same call afterwards is right."""
+    torch.cuda.synchronize()
+    assert T.operator_errors() == T.OK
+    x = torch.randn((700, 1, 64), device="cuda").to(torch.bfloat16)
+    off = dev([0, 700], "int64")
+    want, out = torch.empty_like(x), torch.empty_like(x)
+    T.cross_attention(x, x, x, off, off, want)
+    T.debug_operator_wait(20_000_000, True)
+    try:
+        T.cross_attention(x, x, x, off, off, out)
+        assert T.operator_errors() == T.ERR_TIMEOUT
+        assert T.operator_errors() == T.OK
+    finally:
+        T.debug_operator_wait()
+    T.cross_attention(x, x, x, off, off, out)
+    assert T.operator_errors() == T.OK and torch.equal(out, want)
+
+
 def test_no_wait_has_expired(T):
     torch.cuda.synchronize()
     assert T.operator_errors() == T.OK

@@ -108,6 +108,12 @@ def test_cross_refusals(lib, kw, want):
     assert call(lib.trackfit_cross_attention, CROSS, **kw) == want
 
 
+def test_wait_hook_refusals(lib):
+    for bad in ((-1, 0), (2_000_000_001, 0), (0, 2), (0, -1)):
+        assert lib.trackfit_debug_operator_wait(*bad) == INVALID
+    assert lib.trackfit_debug_operator_wait(0, 0) == OK
+
+
 def test_the_binding_refuses_tensors_on_the_host(lib):
     torch = pytest.importorskip("torch")
     x, off = torch.zeros((4, 2, 16)), torch.tensor([0, 4])
