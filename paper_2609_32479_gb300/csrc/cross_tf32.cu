@@ -28,7 +28,7 @@ template <int NG>
 constexpr __host__ __device__ int slot_bytes() { return NG * 2 * 512 + KC * pitch<NG>() * 4; }
 
 template <int NG>
-__global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __grid_constant__ CaArgs a) {
+__global__ void __launch_bounds__(32, NG == 2 ? 16 : NG == 4 ? 12 : 8) ca_tf32_kernel(const __grid_constant__ CaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NST = queue<NG>(), SLOT = slot_bytes<NG>(), PV = pitch<NG>();
   const int lane = threadIdx.x, g = lane >> 2, t = lane & 3;
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
   const int rows = (int)a.nq * a.G;
   const uint32_t base = smem_addr(smem), mine = base + lane * 16, mine_q = mine + NST * SLOT;
   if (a.D < NG * 16) {                                 // channels beyond D stay zero: the copies leave them alone
-    for (int i = lane * 4; i < NST * SLOT + NG * 2 * 512; i += 128)
+    for (int i = lane * 4; i < NST * SLOT + NG * 4 * 512; i += 128)
       asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + i), "r"(0) : "memory");
     __syncwarp();
   }
@@ -51,7 +51,8 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
   const int row0 = tile * 16 + g, row1 = row0 + 8;
   const int end = __reduce_max_sync(FULL, hi0 > hi1 ? hi0 : hi1);
 
-  // the queries wait in shared memory: their parts would take 16 registers a group
+  // the queries' parts wait in shared memory (they would take 16 registers a group): the upper
+  // ones [group][8 rows], then the lower
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const bool on = e ? in1 : in0;
@@ -61,8 +62,15 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
     for (int i = 0; i < NG; ++i) {
       uint4 u = make_uint4(0, 0, 0, 0);
       if (on && 16 * i + 4 * t < a.D) u = *reinterpret_cast<const uint4*>(p + 16 * i);
-      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(mine_q + (2 * i + e) * 512), "r"((u.x & a.q_and) ^ a.q_xor),
-                   "r"((u.y & a.q_and) ^ a.q_xor), "r"((u.z & a.q_and) ^ a.q_xor), "r"((u.w & a.q_and) ^ a.q_xor)
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      Parts x[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) x[n] = tf32_parts(__uint_as_float((w[n] & a.q_and) ^ a.q_xor));
+      const uint32_t to = mine_q + (2 * i + e) * 512;
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(x[0].hi), "r"(x[1].hi), "r"(x[2].hi), "r"(x[3].hi)
+                   : "memory");
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + NG * 2 * 512), "r"(x[0].lo), "r"(x[1].lo), "r"(x[2].lo),
+                   "r"(x[3].lo)
                    : "memory");
     }
   }
@@ -114,21 +122,22 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[n][i] = 0.0f;
-#pragma unroll
+#pragma unroll 2
     for (int i = 0; i < NG; ++i) {
-      uint32_t q0[4], q1[4];
-      load_shared(q0, mine_q + (2 * i) * 512);
-      load_shared(q1, mine_q + (2 * i + 1) * 512);
+      uint32_t h0[4], h1[4], g0[4], g1[4];
+      load_shared(h0, mine_q + (2 * i) * 512);
+      load_shared(h1, mine_q + (2 * i + 1) * 512);
+      load_shared(g0, mine_q + (2 * NG + 2 * i) * 512);
+      load_shared(g1, mine_q + (2 * NG + 2 * i + 1) * 512);
+      uint32_t k[2][4];
+      load_shared(k[0], mine + s * SLOT + (2 * i) * 512);
+      load_shared(k[1], mine + s * SLOT + (2 * i + 1) * 512);
 #pragma unroll
       for (int w = 0; w < 4; w += 2) {
-        const Parts qa[4] = {tf32_parts(__uint_as_float(q0[w])), tf32_parts(__uint_as_float(q1[w])),
-                             tf32_parts(__uint_as_float(q0[w + 1])), tf32_parts(__uint_as_float(q1[w + 1]))};
+        const uint32_t ah[4] = {h0[w], h1[w], h0[w + 1], h1[w + 1]}, al[4] = {g0[w], g1[w], g0[w + 1], g1[w + 1]};
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          uint32_t k[2];
-          load_shared(k, mine + s * SLOT + (2 * i + n) * 512 + w * 4);
-          mma8_parts(x[n], qa, tf32_parts(__uint_as_float(k[0])), tf32_parts(__uint_as_float(k[1])));
-        }
+        for (int n = 0; n < 2; ++n)
+          mma8_parts(x[n], ah, al, tf32_bparts(__uint_as_float(k[n][w])), tf32_bparts(__uint_as_float(k[n][w + 1])));
       }
     }
     // states that are not a row's own count nothing
@@ -164,11 +173,14 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
       x[n][2] = ex2(fmaf(x[n][2], a.scale2, -n1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, -n1));
       l0 += x[n][0] + x[n][1], l1 += x[n][2] + x[n][3];
     }
-    Parts p[2][4];                                     // rows g, g + 8 by slots t, t + 4: states 2t, 2t + 1
+    uint32_t ph[2][4], pl[2][4];                       // rows g, g + 8 by slots t, t + 4: states 2t, 2t + 1
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[n][i] = tf32_parts(x[n][(i & 1) * 2 + (i >> 1)]);
+      for (int i = 0; i < 4; ++i) {
+        const Parts p = tf32_parts(x[n][(i & 1) * 2 + (i >> 1)]);
+        ph[n][i] = p.hi, pl[n][i] = p.lo;
+      }
     const float* sv = reinterpret_cast<const float*>(smem + s * SLOT + NG * 2 * 512) + 2 * t * PV + g;
     bool mixed = false;
     if (!whole) {
@@ -187,15 +199,15 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float v0 = sv[8 * e * PV + 8 * n], v1 = sv[(8 * e + 1) * PV + 8 * n];
-        const Parts b0 = tf32_parts(v0), b1 = tf32_parts(v1), none = {0u, 0u, 0u};
+        const BParts b0 = tf32_bparts(v0), b1 = tf32_bparts(v1), none = {0u, 0u, 0u};
         if (!mixed) {
-          mma8_parts(o[n], p[e], b0, b1);
+          mma8_parts(o[n], ph[e], pl[e], b0, b1);
         } else {
           // a value that is not finite stays out of the rows that do not read it: each row by itself
           for (int r = 0; r < 16; ++r) {
             const int j = pos + 8 * e + 2 * t, rl = __shfl_sync(FULL, lo_l, r), rh = __shfl_sync(FULL, hi_l, r);
             float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            mma8_parts(d, p[e], j >= rl && j < rh ? b0 : none, j + 1 >= rl && j + 1 < rh ? b1 : none);
+            mma8_parts(d, ph[e], pl[e], j >= rl && j < rh ? b0 : none, j + 1 >= rl && j + 1 < rh ? b1 : none);
             if (g == r) o[n][0] += d[0], o[n][1] += d[1];
             if (g + 8 == r) o[n][2] += d[2], o[n][3] += d[3];
           }
@@ -230,7 +242,7 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : 8) ca_tf32_kernel(const __g
 template <int NG>
 int launch(const CaArgs& a, cudaStream_t st) {
   constexpr auto kern = ca_tf32_kernel<NG>;
-  const size_t smem = queue<NG>() * slot_bytes<NG>() + NG * 2 * 512;
+  const size_t smem = queue<NG>() * slot_bytes<NG>() + NG * 4 * 512;
   const cudaError_t e = allow_smem<kern>(smem);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
   const int64_t units = (a.nq * a.G + 15) / 16 * a.Hk * a.splits;

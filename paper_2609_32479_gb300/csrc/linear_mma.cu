@@ -159,6 +159,7 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
   const char* g0 = reinterpret_cast<const char*>(a.g + base * a.gs + h);
   char* o0 = reinterpret_cast<char*>((T*)a.out + base * a.os + h * a.V + c0 + VC * t);
   const bool v_on = VC * t < width;
+  const int64_t KV = (int64_t)a.K * a.V;
 
   auto issue = [&](int s) {
     Chunk c;
@@ -190,9 +191,9 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
         copy_v<VC * 2>(mine_v + s * SLOT, v0 + (int64_t)r0 * vs, on0);
         copy_v<VC * 2>(mine_v + s * SLOT + 32 * VC * 2, v0 + (int64_t)r1 * vs, on1);
       }
-      if (done == 0) {                                 // the state that it begins with, on its way to L2
-        if (const float* src = piece_begins_with(a, base, c.row, c.seq, h, p.goes_on, p.ends, STATE_ONLY))
-          for (int i = lane; i < a.K; i += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + i * a.V + c0));
+      if (done == 0 && a.state_in && !p.goes_on) {     // the state that it begins with, on its way to L2
+        const float* src = a.state_in + ((int64_t)c.seq * a.H + h) * KV + c0;
+        for (int i = lane; i < a.K; i += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + i * a.V));
       }
       const int lr = lane & 15;
       copy4(mine_g + s * SLOT, g0 + (int64_t)(dir * c.row + lr) * gs, lr < len);
@@ -209,7 +210,6 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
   float st[MT][KT][4];
   bool zero = true;                                    // the state before the chunk is zero, and st not set
   float total = 0.0f;
-  const int64_t KV = (int64_t)a.K * a.V;
   // st[m][j][i] is key channel 32 (j/4) + 8t + 2 (j%4) + (i&1), value channel
   // VC (g/2) + 2 (2m + i/2) + (g&1) of the slice.  Lanes g and g^1 trade halves, so that each
   // has NV channels side by side
@@ -302,10 +302,13 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
     x *= LOG2E;
     x = x < -150.0f ? -150.0f : x;
     if (flags & FIRST) {
-      const float* src = piece_begins_with(a, base, row, ch.seq, h, flags & GOES_ON, flags & ENDS, STATE_ONLY);
-      zero = src == nullptr;
-      if (!zero) load_state(src);
-      if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) store_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);
+      zero = true;
+      if ((flags & GOES_ON) || a.state_in) {
+        const float* src = piece_begins_with(a, base, row, ch.seq, h, flags & GOES_ON, flags & ENDS, STATE_ONLY);
+        zero = src == nullptr;
+        if (!zero) load_state(src);
+        if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) store_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);
+      }
     }
     if (STATE_ONLY) total += x;                        // summed over lanes at the end
     float P = x;

@@ -60,24 +60,30 @@ __device__ __forceinline__ uint32_t tf32(float x) {   // to nearest, 11 bits
   asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(y) : "f"(x));
   return y;
 }
-// x = hi + lo, 11 bits each: products of three of the four parts keep fp32's 2^-21.  An infinity
-// has no lower part, and is left out (fin) where it would meet another operand's.
+// x = hi + lo, 11 bits each: products of three of the four parts keep fp32's 2^-21.  Of a B
+// operand an infinity has no lower part, and is left out (fin) where it would meet the lower
+// part of A, which may be zero.
 struct Parts {
+  uint32_t hi, lo;
+};
+struct BParts {
   uint32_t hi, lo, fin;
 };
 __device__ __forceinline__ Parts tf32_parts(float x) {
-  Parts p;
-  p.hi = tf32(x);
+  const uint32_t hi = tf32(x);
+  return {hi, tf32(x - __uint_as_float(hi))};
+}
+__device__ __forceinline__ BParts tf32_bparts(float x) {
+  const uint32_t hi = tf32(x);
   const bool inf = fabsf(x) == INFINITY;
-  p.lo = inf ? 0u : tf32(x - __uint_as_float(p.hi));
-  p.fin = inf ? 0u : p.hi;
-  return p;
+  return {hi, inf ? 0u : tf32(x - __uint_as_float(hi)), inf ? 0u : hi};
 }
 // d += a b without the product of the lower parts
-__device__ __forceinline__ void mma8_parts(float (&d)[4], const Parts (&a)[4], const Parts& b0, const Parts& b1) {
-  mma8(d, a[0].lo, a[1].lo, a[2].lo, a[3].lo, b0.fin, b1.fin);
-  mma8(d, a[0].fin, a[1].fin, a[2].fin, a[3].fin, b0.lo, b1.lo);
-  mma8(d, a[0].hi, a[1].hi, a[2].hi, a[3].hi, b0.hi, b1.hi);
+__device__ __forceinline__ void mma8_parts(float (&d)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const BParts& b0,
+                                           const BParts& b1) {
+  mma8(d, al[0], al[1], al[2], al[3], b0.fin, b1.fin);
+  mma8(d, ah[0], ah[1], ah[2], ah[3], b0.lo, b1.lo);
+  mma8(d, ah[0], ah[1], ah[2], ah[3], b0.hi, b1.hi);
 }
 __device__ __forceinline__ float2 halves(uint32_t u, __nv_bfloat16) {
   return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
