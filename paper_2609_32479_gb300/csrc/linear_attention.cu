@@ -71,8 +71,9 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   }
   int done = 0;
   const int64_t KV = (int64_t)a.K * a.V;
-  auto beginning = [&](bool goes_on, bool ends, int seq, int row) {
-    return piece_begins_with(a, base, row, seq, h, goes_on, ends, STATE_ONLY);
+  const int block = STATE_ONLY ? 0 : block_of(a.u, tile);
+  auto beginning = [&](bool goes_on, bool ends, int seq) {
+    return STATE_ONLY ? boundary_begins_with(a, seq, h, goes_on) : piece_begins_with(a, block, seq, h, goes_on, ends);
   };
 
   auto issue = [&](Slot& w) {
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
       }
       if (lane < CH) copy4(smem_addr(&w.g[lane]), gr + (int64_t)(row + dir * lane) * a.gs, lane < len);
       if (done == 0) {
-        if (const float* src = beginning(p.goes_on, p.ends, p.seq, row)) {
+        if (const float* src = beginning(p.goes_on, p.ends, p.seq)) {
           for (int i = lane; i < a.K * (COLS / 4); i += 32) {
             const int r = i / (COLS / 4), e = i % (COLS / 4) * 4;
             if (e < width) copy16(smem_addr(w.state() + 4 * i), src + r * a.V + c0 + e, true);
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
     const int flags = w.flags, row = w.row, seq = w.seq, len = flags & LEN;
     if (flags & NONE) break;
     if (flags & FIRST) {
-      const bool st = beginning(flags & GOES_ON, flags & ENDS, seq, row) != nullptr;
+      const bool st = beginning(flags & GOES_ON, flags & ENDS, seq) != nullptr;
       const float* src = w.state() + i0 * COLS + col;
       G = 0.0f;
 #pragma unroll

@@ -159,6 +159,7 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
   const char* g0 = reinterpret_cast<const char*>(a.g + base * a.gs + h);
   char* o0 = reinterpret_cast<char*>((T*)a.out + base * a.os + h * a.V + c0 + VC * t);
   const bool v_on = VC * t < width;
+  const int block = STATE_ONLY ? 0 : block_of(a.u, tile);
   const int64_t KV = (int64_t)a.K * a.V;
 
   auto issue = [&](int s) {
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
         copy_v<VC * 2>(mine_v + s * SLOT, v0 + (int64_t)r0 * vs, on0);
         copy_v<VC * 2>(mine_v + s * SLOT + 32 * VC * 2, v0 + (int64_t)r1 * vs, on1);
       }
-      if (done == 0 && a.state_in && !p.goes_on) {     // the state that it begins with, on its way to L2
+      if (EXACT && done == 0 && a.state_in && !p.goes_on) {   // the state that it begins with, on its way to L2
         const float* src = a.state_in + ((int64_t)c.seq * a.H + h) * KV + c0;
         for (int i = lane; i < a.K; i += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + i * a.V));
       }
@@ -304,7 +305,8 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
     if (flags & FIRST) {
       zero = true;
       if ((flags & GOES_ON) || a.state_in) {
-        const float* src = piece_begins_with(a, base, row, ch.seq, h, flags & GOES_ON, flags & ENDS, STATE_ONLY);
+        const float* src = STATE_ONLY ? boundary_begins_with(a, ch.seq, h, flags & GOES_ON)
+                                      : piece_begins_with(a, block, ch.seq, h, flags & GOES_ON, flags & ENDS);
         zero = src == nullptr;
         if (!zero) load_state(src);
         if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) store_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);

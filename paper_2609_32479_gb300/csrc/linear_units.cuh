@@ -149,14 +149,20 @@ inline unsigned linear_grid(const LaArgs& a, bool state_only) {
   return (unsigned)((state_only ? a.bounds - 1 : a.u.tiles) * a.H * a.slices);
 }
 
-// Where the state that a piece begins with stands, null for zeros.  `row`: its first row in the
-// direction of the recurrence, from `base`.
-__device__ __forceinline__ const float* piece_begins_with(const LaArgs& a, int64_t base, int row, int seq, int h, bool goes_on,
-                                                          bool ends, bool state_only) {
+// The lseg rows that a tile lies in: all of its pieces but a whole sequence end at their bounds,
+// boundary `block` before them and `block` + 1 behind.
+__device__ __forceinline__ int block_of(const Units& u, int64_t tile) { return (int)((unsigned)tile / (unsigned)(u.lseg / u.seg)); }
+
+// Where the state that a piece of a tile begins with stands, null for zeros.
+__device__ __forceinline__ const float* piece_begins_with(const LaArgs& a, int block, int seq, int h, bool goes_on, bool ends) {
   const int64_t KV = (int64_t)a.K * a.V;
-  if (goes_on) return state_only ? nullptr : a.ws_state + ((base + row + a.u.reverse) / a.u.lseg * a.H + h) * KV;
-  if (a.ws_begin && !ends && !state_only) return a.ws_begin + (((base + row) / a.u.lseg + 1 - a.u.reverse) * a.H + h) * KV;
+  if (goes_on) return a.ws_state + ((int64_t)(block + a.u.reverse) * a.H + h) * KV;
+  if (a.ws_begin && !ends) return a.ws_begin + ((int64_t)(block + 1 - a.u.reverse) * a.H + h) * KV;
   return a.state_in ? a.state_in + ((int64_t)seq * a.H + h) * KV : nullptr;
+}
+// The same of a boundary's piece: where it goes on, zeros (what comes from before is added later).
+__device__ __forceinline__ const float* boundary_begins_with(const LaArgs& a, int seq, int h, bool goes_on) {
+  return a.state_in && !goes_on ? a.state_in + ((int64_t)seq * a.H + h) * a.K * a.V : nullptr;
 }
 
 // linear_mma.cu: the 16-bit types on the tensor cores.  Channels of v that a warp takes:

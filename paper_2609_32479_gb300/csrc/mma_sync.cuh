@@ -69,14 +69,17 @@ struct Parts {
 struct BParts {
   uint32_t hi, lo, fin;
 };
+// The upper part is rounded by integer arithmetic (the conversion takes several times the
+// instructions); of the lower one the product itself takes the 11 bits.  A NaN whose upper part
+// the carry turns into a number is still one in the lower part.
 __device__ __forceinline__ Parts tf32_parts(float x) {
-  const uint32_t hi = tf32(x);
-  return {hi, tf32(x - __uint_as_float(hi))};
+  const uint32_t hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+  return {hi, __float_as_uint(x - __uint_as_float(hi))};
 }
 __device__ __forceinline__ BParts tf32_bparts(float x) {
-  const uint32_t hi = tf32(x);
+  const Parts p = tf32_parts(x);
   const bool inf = fabsf(x) == INFINITY;
-  return {hi, inf ? 0u : tf32(x - __uint_as_float(hi)), inf ? 0u : hi};
+  return {p.hi, inf ? 0u : p.lo, inf ? 0u : p.hi};
 }
 // d += a b without the product of the lower parts
 __device__ __forceinline__ void mma8_parts(float (&d)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const BParts& b0,
