@@ -55,18 +55,29 @@ __global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant_
 bool wide_tiles(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int G) {
   return dtype != TRACKFIT_FP32 && nq * G >= 64 * n_seq && nk >= 512 * n_seq;
 }
-// Parts of each row's range: as many as give every warp of the GPU something to do (152 x 12 of
-// the 16-row kernels, 152 x 2 CTAs of the 128-row one, 152 for wide heads), not under 256 states
-// each (512) on average, and at most the 32 that the joining warp has lanes for.
-int splits_of(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk, int D) {
-  if (nq <= 0 || n_seq <= 0) return 1;
-  const int G = Hq / Hk;
-  const bool wide = wide_tiles(dtype, nq, nk, n_seq, G);
-  const int64_t units = (nq * G + (wide ? 127 : 15)) / (wide ? 128 : 16) * Hk;
-  const int64_t most = nk / n_seq / (wide ? 512 : 256);
-  int64_t s = (wide ? (D <= 64 ? 304 : 152) : 152 * 12) / units;
-  if (s > most) s = most;
-  return s < 1 ? 1 : s > 32 ? 32 : (int)s;
+// How a call is cut.  Parts of each row's range: as many as give every warp of the GPU something
+// to do (152 x 12 of the 16-row kernels, 152 x 2 CTAs of the 128-row one, 152 for wide heads), not
+// under 256 states each (512) on average, and at most the 32 that the joining warp has lanes
+// for.  Where that leaves less than half of the warps busy, tiles of fewer rows, down to a
+// sequence's (20 sequences of 1-2 queries, 4 heads: two tiles of 16 rows a head, each through ten
+// sequences' states).
+struct Cut {
+  bool wide;
+  int splits, tr;
+};
+Cut cut_of(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk, int D) {
+  Cut c = {false, 1, 16};
+  if (nq <= 0 || n_seq <= 0) return c;
+  const int64_t G = Hq / Hk, rows = nq * G;
+  c.wide = wide_tiles(dtype, nq, nk, n_seq, (int)G);
+  const int64_t target = c.wide ? (D <= 64 ? 304 : 152) : 152 * 12, most = nk / n_seq / (c.wide ? 512 : 256);
+  for (;; c.tr /= 2) {
+    const int64_t units = (c.wide ? (rows + 127) / 128 : (rows + c.tr - 1) / c.tr) * Hk;
+    int64_t s = target / units;
+    if (s > most) s = most;
+    c.splits = s < 1 ? 1 : s > 32 ? 32 : (int)s;
+    if (c.wide || c.tr == 1 || units * c.splits * 2 >= target || c.tr / 2 < (rows + n_seq - 1) / n_seq) return c;
+  }
 }
 
 }  // namespace
@@ -76,7 +87,7 @@ extern "C" size_t trackfit_cross_attention_workspace(int32_t dtype, int64_t n_q_
   if (!type_ok(dtype) || n_q_rows < 0 || n_kv_rows < 0 || n_seq < 0 || !heads_ok(q_heads) || !heads_ok(kv_heads) ||
       q_heads % kv_heads != 0 || !dim_ok(head_dim) || n_q_rows > MOST_ROWS / (q_heads / kv_heads) || n_kv_rows > MOST_ROWS)
     return 0;
-  const int s = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads, head_dim);
+  const int s = cut_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads, head_dim).splits;
   return s > 1 ? (size_t)s * n_q_rows * q_heads * (head_dim + 2) * 4 : 0;
 }
 
@@ -111,7 +122,8 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
   a.Hq = q_heads, a.Hk = kv_heads, a.G = q_heads / kv_heads, a.D = head_dim;
   a.scale2 = scale == 0.0f ? 1.0f : fabsf(scale) * LOG2E;
   a.q_and = scale == 0.0f ? 0u : ~0u, a.q_xor = scale < 0.0f ? (dtype == TRACKFIT_FP32 ? 0x80000000u : 0x80008000u) : 0u;
-  a.splits = splits_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads, head_dim);
+  const Cut cut = cut_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads, head_dim);
+  a.splits = cut.splits, a.tr = cut.tr;
   // all heads of a tile by one warp where that leaves ten tiles for each of the 152 x 16 warps
   // (131,072 tracks of five queries: 319 us, with a warp a head 451)
   a.each = (n_q_rows * a.G + 15) / 16 >= 10 * 152 * 16 ? kv_heads : 1;
@@ -119,7 +131,7 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (need > 0 ? (int64_t)a.splits * n_q_rows * q_heads * head_dim : 0));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   a.tc_from = 0;
-  if (wide_tiles(dtype, n_q_rows, n_kv_rows, n_seq, a.G)) {
+  if (cut.wide) {
     // the 16-row kernel after it takes the sequences of few states, if there are any
     a.tc_from = CROSS_TC_FROM;
     const int rc = cross_tc(dtype, a, st);

@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : NG == 4 ? 12 : 8) ca_tf32_k
   const int lo0 = __shfl_sync(FULL, lo_l, g), hi0 = __shfl_sync(FULL, hi_l, g);
   const int lo1 = __shfl_sync(FULL, lo_l, g + 8), hi1 = __shfl_sync(FULL, hi_l, g + 8);
   const bool in0 = __shfl_sync(FULL, (int)in, g), in1 = __shfl_sync(FULL, (int)in, g + 8);
-  const int row0 = tile * 16 + g, row1 = row0 + 8;
+  const int row0 = tile * a.tr + g, row1 = row0 + 8;
   const int end = __reduce_max_sync(FULL, hi0 > hi1 ? hi0 : hi1);
 
   // the queries' parts wait in shared memory (they would take 16 registers a group): the upper
@@ -245,7 +245,7 @@ int launch(const CaArgs& a, cudaStream_t st) {
   const size_t smem = queue<NG>() * slot_bytes<NG>() + NG * 4 * 512;
   const cudaError_t e = allow_smem<kern>(smem);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  const int64_t units = (a.nq * a.G + 15) / 16 * a.Hk * a.splits;
+  const int64_t units = (a.nq * a.G + a.tr - 1) / a.tr * a.Hk * a.splits;
   if (units > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
   kern<<<(unsigned)units, 32, smem, st>>>(a);
   return launched();

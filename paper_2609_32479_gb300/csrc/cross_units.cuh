@@ -1,8 +1,8 @@
 // Attention of packed queries to packed states: arguments and how the work is cut.
 //
 // The G = q_heads / kv_heads heads of a query that share a head of the states are rows of the
-// same products: row i G + j stands for query i, head (kv head) G + j.  A tile is 16 (or, many
-// queries to many states, 128) of these rows, counted from row 0 whatever the sequences; each
+// same products: row i G + j stands for query i, head (kv head) G + j.  A tile is 16 (fewer where
+// tiles are few, 128 for many queries to many states) of these rows, counted from row 0 whatever the sequences; each
 // row has the range of states of its own sequence.  Where tiles are few, each row's range is
 // cut into `splits` parts, and the parts' sums are joined by a second kernel.
 #pragma once
@@ -21,6 +21,7 @@ struct CaArgs {
   float scale2;                  // |scale| * log2(e), or 1 with a scale of 0
   uint32_t q_and, q_xor;         // on queries (two of 16 bits): zeroed with a scale of 0, negated below it
   int splits;
+  int tr;                        // rows of a tile of the 16-row kernels, 1 to 16
   int tc_from;                   // sequences of at least so many states are cross_tc.cu's (0: none)
   int each;                      // heads of the states that a warp takes one after the other
   float* ws_o;                   // [splits][rows][Hk][D], sums not yet divided
@@ -32,11 +33,11 @@ constexpr int FARTHEST = 0x7fffffff;
 // The states that row (lane & 15) of a tile reads, [lo, hi), and whether it is a query of a
 // sequence at all.
 __device__ __forceinline__ void find_rows(const CaArgs& a, int tile, int split, int lane, bool& in, int& lo, int& hi) {
-  const int row = tile * 16 + (lane & 15);
-  const bool there = row < (int)(a.nq * a.G);
-  const int64_t q = there ? row / a.G : a.nq - 1;
-  int64_t b = first_at_least(a.qo, a.n_seq, (int64_t)(tile * 16) / a.G + 1, lane) - 1;   // the last that begins at
-  if (b < 0) b = 0;                                                                      // or before the first row
+  const int first = tile * a.tr, row = first + (lane & 15);
+  const bool there = (lane & 15) < a.tr && row < (int)(a.nq * a.G);
+  const int64_t q = (there ? row : first) / a.G;
+  int64_t b = first_at_least(a.qo, a.n_seq, (int64_t)first / a.G + 1, lane) - 1;   // the last that begins at or
+  if (b < 0) b = 0;                                                                // before the first row
   // the offsets that follow, 32 at a time: how many are at or before the row's query
   for (int64_t at = b + 1;; at += 32) {
     const int64_t o = at + lane < a.n_seq ? a.qo[at + lane] : INT64_MAX;

@@ -392,6 +392,16 @@ def test_cross_long(T, t, nq, nk):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("nq,nk", [([1, 2] * 10, [700] * 20), ([2, 0, 3, 1], [3000, 10, 1, 5000]),
+                                   ([1] * 70, list(range(200, 1600, 20))), ([7, 7, 7], [900, 1000, 0])])
+def test_cross_of_few_queries(T, t, nq, nk):
+    """Few tiles: split ranges, and tiles of fewer rows."""
+    check_cross(T, nq, nk, 4, 4, 64, t)
+    check_cross(T, nq, nk, 6, 2, 32, t, lead=1, tail=3, seed=4)
+    check_cross(T, nq, nk, 3, 1, 128, t, seed=5)
+
+
+@pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("D", [64, 8, 40, 72, 128])
 @pytest.mark.parametrize("nq,nk", [([128], [512]), ([300, 40, 0, 500], [3000, 100, 50, 128]),
                                    ([1, 129, 127, 700], [1, 2047, 127, 4097]), ([64] * 9, [513] * 9)])
