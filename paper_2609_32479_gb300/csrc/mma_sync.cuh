@@ -1,5 +1,5 @@
-// Warp-level matrix products (mma.sync) and their operands from shared memory, for the
-// operators whose pieces of work are a few rows long.  Lane l holds, with g = l / 4 and
+// Warp-level matrix products (mma.sync) and their operands, for the operators whose pieces of
+// work are a few rows long.  Lane l holds, with g = l / 4 and
 // t = l % 4, of an accumulator 16 x 8: (g, 2t), (g, 2t+1), (g+8, 2t), (g+8, 2t+1).
 #pragma once
 
@@ -7,18 +7,6 @@
 
 namespace seqops {
 
-__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
-__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr)
-               : "memory");
-}
 // d += a b, 16 x 8 x 16
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
   asm volatile(

@@ -12,7 +12,9 @@ definition of |q|, |k|, |v|):
           n rows, of the absolute sums; the 16-bit types round the state, or its parts, to 16
           bits as operands, 2 e of the absolute sums.  States: fp32 throughout, (6 n + 16) u.
   cross   a score's error, (D + 8) u of its absolute sum, is the relative error of its weight;
-          the sums over n states, (n + 16) u; 16-bit types round the weights once, e."""
+          the sums over n states, (n + 16) u; 16-bit types round the weights once, e.  fp32
+          operands are two parts of 11 bits, which loses 8 u more of each product: 2 (D + 8) u
+          holds both."""
 import numpy as np
 import pytest
 
