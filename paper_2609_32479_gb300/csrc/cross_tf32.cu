@@ -5,7 +5,8 @@
 // of operands the three largest are taken (m16n8k8): what is left out is 2^-22 of a product, of
 // the order of fp32's own rounding.  Three products of half the rate each leave 100 TFLOP/s of
 // mma.sync's 604, against the 75 of the CUDA cores, whose operands would come from shared
-// memory value by value.
+// memory value by value.  Measured: 2,000 queries over 16,000 states, 4 heads of 64: 1607 us, 20
+// TFLOP/s; the instructions that form the parts bound it, each warp for its own 16 rows.
 //
 // Lane (g, t) reads 16 bytes, channels 4t .. 4t+3 of each 16, of rows g and g + 8: with the k
 // index permuted alike on both sides these are operands of Q K^T as they stand (slots t and

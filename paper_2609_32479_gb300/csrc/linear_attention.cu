@@ -17,7 +17,7 @@ using namespace seqops;
 // memory as broadcasts, 8 rows at a time through a ring that the warp fills by asynchronous
 // copies.  Several columns a lane share what a row costs whatever its columns (loads,
 // exponentials, addresses: 90 of 116 instructions with one).  Measured: 20,011 tracks and parts
-// of tracks, 4 heads of 32 x 48, states in and out: 759 us, 3.5 TB/s; one column a lane 1136,
+// of tracks, 4 heads of 32 x 48, states in and out: 776 us, 3.4 TB/s; one column a lane 1136,
 // a third multiply-add a value for the decay 814.
 constexpr int CH = 8, NST = 2;
 
@@ -320,7 +320,7 @@ constexpr int LONGEST = 512;   // longer sequences are cut
 
 // Whether any may be: not where there are few rows of sequences that are short on average.  The
 // two launches would cost a small call more than a warp's time for the longest sequence that
-// could be among them, 16,384 rows, is likely to (an event of 211 tracks: 13 us instead of 7).
+// could be among them, 16,384 rows, is likely to (an event of 211 tracks: 13 us instead of 6).
 bool cuts(int64_t n_rows, int64_t n_seq) { return n_rows > LONGEST && (n_rows > 16384 || n_rows > 64 * n_seq); }
 
 size_t workspace_bytes(int64_t n_rows, int64_t n_seq, int H, int K, int V) {

@@ -34,10 +34,10 @@
 // bits but not the range for Q K^T and S: these go through tf32 products (11 bits, fp32's
 // range); the decayed V, no larger than V with g <= 0, is split in two.
 //
-// Measured: 131,072 tracks, 4 heads of 32, bf16: 388 us, 4.9 TB/s of the 6.8 that a copy moves;
-// issued instructions bound it (55 % of the slots with 16 warps an SM, the rest waits for
+// Measured: 131,072 tracks, 4 heads of 32, bf16: 381 us, 5.0 TB/s of the 6.8 that a copy moves;
+// issued instructions bound it (two thirds of the slots with 16 warps an SM, the rest waits for
 // their results).  Four sequences of 20,000-40,000 rows, 8 heads of 64, states in and out:
-// 105 us for the parts' own states, 14 for what they pass on, 190 for the outputs, against 84
+// 118 us for the parts' own states, 14 for what they pass on, 192 for the outputs, against 84
 // for one reading of everything; latency with 8 warps an SM bounds it.
 #include "linear_units.cuh"
 #include "mma_sync.cuh"
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
   constexpr bool BF = !__is_same(T, __half);
   constexpr int MT = NV / 2, KT = NG * 4;             // tiles of the state: MT x 16 by KT x 8
   // With 128 registers a thread (16 warps an SM) q and k are read where they are used; with 255
-  // (8 warps) early, and their place filled again: 221 instead of 305 us at K = 64
+  // (8 warps) early, and their place filled again: 221 instead of 305 us at K = 64, when both were tried
   constexpr bool EARLY = NG == 2;
   constexpr int VC = NV * 2;                           // channels of V a lane
   constexpr int SLOT = slot_bytes(NG, NV);
