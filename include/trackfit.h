@@ -413,8 +413,9 @@ int trackfit_forward_noalloc(const trackfit_config_t* cfg, const float* weights,
  * allocation, no host synchronisation; capturable.  Calls that may run at the same time
  * need workspaces of their own (as two graphs that are replayed side by side do).
  * n_rows = 0, n_q_rows = 0 and n_seq = 0 are valid.  Errors: INVALID_ARG (NULL,
- * misalignment, negative counts, a stride below the row's width, a workspace too small,
- * values that are not finite), UNSUPPORTED (widths, heads), CUDA. */
+ * misalignment, negative counts, a stride below the row's width or over 2^28, a workspace
+ * too small, values that are not finite), UNSUPPORTED (widths, heads, more rows or units of
+ * work than 32 bits count), CUDA.  Make the first call of a kind outside of a capture. */
 
 /* Norms of queries and keys for each head, with the position rotation in the same pass.
  *   y = x / sqrt(mean(x^2) + eps) * gain over a head's channels, then, for
