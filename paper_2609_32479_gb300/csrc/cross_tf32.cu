@@ -5,7 +5,7 @@
 // of operands the three largest are taken (m16n8k8): what is left out is 2^-22 of a product, of
 // the order of fp32's own rounding.  Three products of half the rate each leave 100 TFLOP/s of
 // mma.sync's 604, against the 75 of the CUDA cores, whose operands would come from shared
-// memory value by value.  Measured: 2,000 queries over 16,000 states, 4 heads of 64: 1607 us, 20
+// memory value by value.  Measured: 2,000 queries over 16,000 states, 4 heads of 64: 1561 us, 21
 // TFLOP/s; the instructions that form the parts bound it, each warp for its own 16 rows.
 //
 // Lane (g, t) reads 16 bytes, channels 4t .. 4t+3 of each 16, of rows g and g + 8: with the k
@@ -29,7 +29,7 @@ template <int NG>
 constexpr __host__ __device__ int slot_bytes() { return NG * 2 * 512 + KC * pitch<NG>() * 4; }
 
 template <int NG>
-__global__ void __launch_bounds__(32, NG == 2 ? 16 : NG == 4 ? 12 : 8) ca_tf32_kernel(const __grid_constant__ CaArgs a) {
+__global__ void __launch_bounds__(32, NG <= 4 ? 12 : 8) ca_tf32_kernel(const __grid_constant__ CaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NST = queue<NG>(), SLOT = slot_bytes<NG>(), PV = pitch<NG>();
   const int lane = threadIdx.x, g = lane >> 2, t = lane & 3;
@@ -161,19 +161,16 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : NG == 4 ? 12 : 8) ca_tf32_k
     }
     t0 = fmaxf(m0, t0 * a.scale2), t1 = fmaxf(m1, t1 * a.scale2);
     const float n0 = t0 == -INFINITY ? 0.0f : t0, n1 = t1 == -INFINITY ? 0.0f : t1;
-    if (__any_sync(FULL, t0 != m0 || t1 != m1)) {
-      const float f0 = ex2(m0 - n0), f1 = ex2(m1 - n1);
-      l0 *= f0, l1 *= f1;
-#pragma unroll
-      for (int n = 0; n < NG * 2; ++n) o[n][0] *= f0, o[n][1] *= f0, o[n][2] *= f1, o[n][3] *= f1;
-      m0 = t0, m1 = t1;
-    }
+    const float f0 = ex2(m0 - n0), f1 = ex2(m1 - n1);
+    m0 = t0, m1 = t1;
+    float c0 = 0.0f, c1 = 0.0f;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       x[n][0] = ex2(fmaf(x[n][0], a.scale2, -n0)), x[n][1] = ex2(fmaf(x[n][1], a.scale2, -n0));
       x[n][2] = ex2(fmaf(x[n][2], a.scale2, -n1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, -n1));
-      l0 += x[n][0] + x[n][1], l1 += x[n][2] + x[n][3];
+      c0 += x[n][0] + x[n][1], c1 += x[n][2] + x[n][3];
     }
+    l0 = fmaf(l0, f0, c0), l1 = fmaf(l1, f1, c1);
     uint32_t ph[2][4], pl[2][4];                       // rows g, g + 8 by slots t, t + 4: states 2t, 2t + 1
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -195,25 +192,31 @@ __global__ void __launch_bounds__(32, NG == 2 ? 16 : NG == 4 ? 12 : 8) ca_tf32_k
         }
       mixed = __any_sync(FULL, !(sum == 0.0f));
     }
+    // a chunk's own sum first, added to O outside the products: their accumulation cuts bits off, and
+    // over a long range would draw sums of one sign towards zero (16,000 states: 5e-6, 60,000: 2e-5)
 #pragma unroll
-    for (int n = 0; n < NG * 2; ++n)
+    for (int n = 0; n < NG * 2; ++n) {
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float v0 = sv[8 * e * PV + 8 * n], v1 = sv[(8 * e + 1) * PV + 8 * n];
         const BParts b0 = tf32_bparts(v0), b1 = tf32_bparts(v1), none = {0u, 0u, 0u};
         if (!mixed) {
-          mma8_parts(o[n], ph[e], pl[e], b0, b1);
+          mma8_parts(sum, ph[e], pl[e], b0, b1);
         } else {
           // a value that is not finite stays out of the rows that do not read it: each row by itself
           for (int r = 0; r < 16; ++r) {
             const int j = pos + 8 * e + 2 * t, rl = __shfl_sync(FULL, lo_l, r), rh = __shfl_sync(FULL, hi_l, r);
             float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             mma8_parts(d, ph[e], pl[e], j >= rl && j < rh ? b0 : none, j + 1 >= rl && j + 1 < rh ? b1 : none);
-            if (g == r) o[n][0] += d[0], o[n][1] += d[1];
-            if (g + 8 == r) o[n][2] += d[2], o[n][3] += d[3];
+            if (g == r) sum[0] += d[0], sum[1] += d[1];
+            if (g + 8 == r) sum[2] += d[2], sum[3] += d[3];
           }
         }
       }
+      o[n][0] = fmaf(o[n][0], f0, sum[0]), o[n][1] = fmaf(o[n][1], f0, sum[1]);
+      o[n][2] = fmaf(o[n][2], f1, sum[2]), o[n][3] = fmaf(o[n][3], f1, sum[3]);
+    }
     __syncwarp();                                      // read: the place is free
     at[NST - 1] = issue(s);
   }

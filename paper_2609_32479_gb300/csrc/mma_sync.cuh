@@ -48,7 +48,7 @@ __device__ __forceinline__ uint32_t tf32(float x) {   // to nearest, 11 bits
   asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(y) : "f"(x));
   return y;
 }
-// x = hi + lo, 11 bits each: products of three of the four parts keep fp32's 2^-21.  Of a B
+// x = hi + lo, 11 bits each, both to nearest: products of three of the four parts keep fp32's 2^-21.  Of a B
 // operand an infinity has no lower part, and is left out (fin) where it would meet the lower
 // part of A, which may be zero.
 struct Parts {
@@ -57,12 +57,13 @@ struct Parts {
 struct BParts {
   uint32_t hi, lo, fin;
 };
-// The upper part is rounded by integer arithmetic (the conversion takes several times the
-// instructions); of the lower one the product itself takes the 11 bits.  A NaN whose upper part
-// the carry turns into a number is still one in the lower part.
+// Rounded by integer arithmetic (the conversion takes several times the instructions); the 13
+// bits that a product passes over are cut off only where the part is a number of its own.  Cut
+// instead of rounded, the lower part would draw long sums of one sign towards zero.  A NaN whose
+// upper part the carry turns into a number is still one in the lower part.
 __device__ __forceinline__ Parts tf32_parts(float x) {
   const uint32_t hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
-  return {hi, __float_as_uint(x - __uint_as_float(hi))};
+  return {hi, __float_as_uint(x - __uint_as_float(hi)) + 0x1000u};
 }
 __device__ __forceinline__ BParts tf32_bparts(float x) {
   const Parts p = tf32_parts(x);
