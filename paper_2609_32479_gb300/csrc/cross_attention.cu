@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant_
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int s = 0; s < a.splits; ++s) {
-    const float fs = __shfl_sync(FULL, f, s) * inv;
+    const float fs = __shfl_sync(FULL, f, s);
     const float* p = a.ws_o + (s * all + unit) * a.D;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant_
   T* out = (T*)a.out + q * a.os + (hk * a.G + row % a.G) * a.D;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
-    if (lane + 32 * c < a.D) put(out + lane + 32 * c, o[c]);
+    if (lane + 32 * c < a.D) put(out + lane + 32 * c, average(o[c], inv));
 }
 
 // Whether the 128-row kernel runs: 16-bit types, sequences of at least 64 rows and 512 states on

@@ -46,12 +46,13 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
   }
 
   bool in;
-  int lo_l, hi_l;
-  find_rows(a, tile, split, lane, in, lo_l, hi_l);
+  int lo_l, hi_l, most;
+  find_rows(a, tile, split, lane, in, lo_l, hi_l, most);
   const int lo0 = __shfl_sync(FULL, lo_l, g), hi0 = __shfl_sync(FULL, hi_l, g);
   const int lo1 = __shfl_sync(FULL, lo_l, g + 8), hi1 = __shfl_sync(FULL, hi_l, g + 8);
   const bool in0 = __shfl_sync(FULL, (int)in, g), in1 = __shfl_sync(FULL, (int)in, g + 8);
   const int row0 = tile * a.tr + g, row1 = row0 + 8;
+  const float up = weight_up<T>(most);
   const int end = __reduce_max_sync(FULL, hi0 > hi1 ? hi0 : hi1);
   auto wanted = [&](int pos) { return first_wanted(pos, lo0, hi0, lo1, hi1); };
 
@@ -162,10 +163,11 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
         for (int n = 0; n < NG * 4; ++n) o[n][0] *= f0, o[n][1] *= f0, o[n][2] *= f1, o[n][3] *= f1;
         m0 = t0, m1 = t1;
       }
+      const float b0 = up - n0, b1 = up - n1;
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        x[n][0] = ex2(fmaf(x[n][0], a.scale2, -n0)), x[n][1] = ex2(fmaf(x[n][1], a.scale2, -n0));
-        x[n][2] = ex2(fmaf(x[n][2], a.scale2, -n1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, -n1));
+        x[n][0] = ex2(fmaf(x[n][0], a.scale2, b0)), x[n][1] = ex2(fmaf(x[n][1], a.scale2, b0));
+        x[n][2] = ex2(fmaf(x[n][2], a.scale2, b1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, b1));
         l0 += x[n][0] + x[n][1], l1 += x[n][2] + x[n][3];
       }
       uint32_t pa[2][4];

@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     bool ok = true;
     while (ok && passes.next(ps)) {
       float m = -INFINITY, l = 0.0f;                   // m: score * scale2 that the weights are taken against
+      const float up = __is_same(T, __half) ? 0.0f : weight_up<T>(ps.len) - LAG;
       for (int j = ps.j0; j < ps.j1; ++j, ++n) {
         const uint32_t place = n & 1, phase = n >> 1 & 1;
         ok = __all_sync(FULL, mbar_wait(s_full + 8 * place, phase, abort, p.limit_ns));
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
           ok = __all_sync(FULL, mbar_wait(p_free + 8 * place, phase ^ 1, abort, p.limit_ns));
           if (!ok) break;
         }
-        const uint64_t scale = both(a.scale2, a.scale2), minus = both(-mm, -mm);
+        const uint64_t scale = both(a.scale2, a.scale2), minus = both(up - mm, up - mm);
         uint64_t s0 = 0, s1 = 0;
 #pragma unroll
         for (int c = 0; c < 8; ++c) {

@@ -5,7 +5,7 @@
 // of operands the three largest are taken (m16n8k8): what is left out is 2^-22 of a product, of
 // the order of fp32's own rounding.  Three products of half the rate each leave 100 TFLOP/s of
 // mma.sync's 604, against the 75 of the CUDA cores, whose operands would come from shared
-// memory value by value.  Measured: 2,000 queries over 16,000 states, 4 heads of 64: 1561 us, 21
+// memory value by value.  Measured: 2,000 queries over 16,000 states, 4 heads of 64: 1590 us, 21
 // TFLOP/s; the instructions that form the parts bound it, each warp for its own 16 rows.
 //
 // Lane (g, t) reads 16 bytes, channels 4t .. 4t+3 of each 16, of rows g and g + 8: with the k
@@ -44,12 +44,13 @@ __global__ void __launch_bounds__(32, NG <= 4 ? 12 : 8) ca_tf32_kernel(const __g
     __syncwarp();
   }
   bool in;
-  int lo_l, hi_l;
-  find_rows(a, tile, split, lane, in, lo_l, hi_l);
+  int lo_l, hi_l, most;
+  find_rows(a, tile, split, lane, in, lo_l, hi_l, most);
   const int lo0 = __shfl_sync(FULL, lo_l, g), hi0 = __shfl_sync(FULL, hi_l, g);
   const int lo1 = __shfl_sync(FULL, lo_l, g + 8), hi1 = __shfl_sync(FULL, hi_l, g + 8);
   const bool in0 = __shfl_sync(FULL, (int)in, g), in1 = __shfl_sync(FULL, (int)in, g + 8);
   const int row0 = tile * a.tr + g, row1 = row0 + 8;
+  const float up = exp2f(weight_up<float>(most));
   const int end = __reduce_max_sync(FULL, hi0 > hi1 ? hi0 : hi1);
 
   // the queries' parts wait in shared memory (they would take 16 registers a group): the upper
@@ -166,8 +167,9 @@ __global__ void __launch_bounds__(32, NG <= 4 ? 12 : 8) ca_tf32_kernel(const __g
     float c0 = 0.0f, c1 = 0.0f;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      x[n][0] = ex2(fmaf(x[n][0], a.scale2, -n0)), x[n][1] = ex2(fmaf(x[n][1], a.scale2, -n0));
-      x[n][2] = ex2(fmaf(x[n][2], a.scale2, -n1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, -n1));
+      // (the factor in the exponent would cost the argument five bits)
+      x[n][0] = up * ex2(fmaf(x[n][0], a.scale2, -n0)), x[n][1] = up * ex2(fmaf(x[n][1], a.scale2, -n0));
+      x[n][2] = up * ex2(fmaf(x[n][2], a.scale2, -n1)), x[n][3] = up * ex2(fmaf(x[n][3], a.scale2, -n1));
       c0 += x[n][0] + x[n][1], c1 += x[n][2] + x[n][3];
     }
     l0 = fmaf(l0, f0, c0), l1 = fmaf(l1, f1, c1);
@@ -200,7 +202,7 @@ __global__ void __launch_bounds__(32, NG <= 4 ? 12 : 8) ca_tf32_kernel(const __g
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float v0 = sv[8 * e * PV + 8 * n], v1 = sv[(8 * e + 1) * PV + 8 * n];
-        const BParts b0 = tf32_bparts(v0), b1 = tf32_bparts(v1), none = {0u, 0u, 0u};
+        const BParts b0 = tf32_bparts_of_weighted(v0), b1 = tf32_bparts_of_weighted(v1), none = {0u, 0u, 0u};
         if (!mixed) {
           mma8_parts(sum, ph[e], pl[e], b0, b1);
         } else {
@@ -238,8 +240,8 @@ __global__ void __launch_bounds__(32, NG <= 4 ? 12 : 8) ca_tf32_kernel(const __g
   for (int n = 0; n < NG * 2; ++n) {
     const int c = 8 * n + 2 * t;
     if (c >= a.D) continue;
-    if (in0) *reinterpret_cast<float2*>(p0 + c) = make_float2(o[n][0] * f0, o[n][1] * f0);
-    if (in1) *reinterpret_cast<float2*>(p1 + c) = make_float2(o[n][2] * f1, o[n][3] * f1);
+    if (in0) *reinterpret_cast<float2*>(p0 + c) = make_float2(average(o[n][0], f0), average(o[n][1], f0));
+    if (in1) *reinterpret_cast<float2*>(p1 + c) = make_float2(average(o[n][2], f1), average(o[n][3], f1));
   }
 }
 

@@ -7,6 +7,8 @@
 // cut into `splits` parts, and the parts' sums are joined by a second kernel.
 #pragma once
 
+#include <float.h>
+
 #include "seq_ops.cuh"
 
 namespace seqops {
@@ -30,9 +32,26 @@ struct CaArgs {
 
 constexpr int FARTHEST = 0x7fffffff;
 
-// The states that row (lane & 15) of a tile reads, [lo, hi), and whether it is a query of a
-// sequence at all.
-__device__ __forceinline__ void find_rows(const CaArgs& a, int tile, int split, int lane, bool& in, int& lo, int& hi) {
+// Weights are 2^(score - largest + up), and so are their sums and O, which the division takes out
+// again: with as many weights of one as there are states, values next to the type's largest would
+// leave fp32 in O where their average does not.  (Not further down than these need: values next to
+// the smallest would be lost.  2^31 values of fp16 are far below fp32's largest.)  Alike for all
+// parts of a row.
+template <class T>
+__device__ __forceinline__ float weight_up(int states) {
+  return __is_same(T, __half) ? 0.0f : -(float)(32 - __clz(states));
+}
+
+// o f, an average of finite values where o is finite: held at the largest fp32, which the roundings
+// may pass.
+__device__ __forceinline__ float average(float o, float f) {
+  const float y = o * f;
+  return fabsf(y) == INFINITY && fabsf(o) < INFINITY ? copysignf(FLT_MAX, y) : y;
+}
+
+// The states that row (lane & 15) of a tile reads, [lo, hi) of this part, whether it is a query of a
+// sequence at all, and the most states that a row of the tile reads in all parts.
+__device__ __forceinline__ void find_rows(const CaArgs& a, int tile, int split, int lane, bool& in, int& lo, int& hi, int& most) {
   const int first = tile * a.tr, row = first + (lane & 15);
   const bool there = (lane & 15) < a.tr && row < (int)(a.nq * a.G);
   const int64_t q = (there ? row : first) / a.G;
@@ -48,15 +67,17 @@ __device__ __forceinline__ void find_rows(const CaArgs& a, int tile, int split, 
     if (!__any_sync(FULL, n == 32)) break;
   }
   in = there && a.qo[b] <= q && q < a.qo[b + 1];
-  lo = hi = 0;
+  lo = hi = most = 0;
   if (in) {
     const int64_t l = clamp64(a.ko[b], 0, a.nk), h = clamp64(a.ko[b + 1], l, a.nk);
     if (a.tc_from && h - l >= a.tc_from) {
       in = false;
-      return;
+    } else {
+      lo = (int)(l + (h - l) * split / a.splits), hi = (int)(l + (h - l) * (split + 1) / a.splits);
+      most = (int)(h - l);
     }
-    lo = (int)(l + (h - l) * split / a.splits), hi = (int)(l + (h - l) * (split + 1) / a.splits);
   }
+  most = __reduce_max_sync(FULL, most);
 }
 
 // The first state from `pos` on that a row of the tile reads, by all lanes' two rows.

@@ -48,27 +48,32 @@ __device__ __forceinline__ uint32_t tf32(float x) {   // to nearest, 11 bits
   asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(y) : "f"(x));
   return y;
 }
-// x = hi + lo, 11 bits each, both to nearest: products of three of the four parts keep fp32's 2^-21.  Of a B
-// operand an infinity has no lower part, and is left out (fin) where it would meet the lower
-// part of A, which may be zero.
+// x = hi + lo, 11 bits each: products of three of the four parts keep fp32's 2^-21.  An infinity is
+// all in the lower part; of a B operand it is left out (fin) where it would meet the lower part of
+// A, which may be zero.
 struct Parts {
   uint32_t hi, lo;
 };
 struct BParts {
   uint32_t hi, lo, fin;
 };
-// Rounded by integer arithmetic (the conversion takes several times the instructions); the 13
-// bits that a product passes over are cut off only where the part is a number of its own.  Cut
-// instead of rounded, the lower part would draw long sums of one sign towards zero.  A NaN whose
-// upper part the carry turns into a number is still one in the lower part.
+// The upper part is rounded by integer arithmetic (the conversion takes several times the
+// instructions).  The lower one then has 12 bits, of which the product takes 11: off by 2^-22 x at
+// most, and as often to one side as to the other, for it has either sign.  The upper part stays finite
+// where x is next to the largest; a NaN is all in the lower part.
 __device__ __forceinline__ Parts tf32_parts(float x) {
-  const uint32_t hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
-  return {hi, __float_as_uint(x - __uint_as_float(hi)) + 0x1000u};
+  const uint32_t u = __float_as_uint(x), m = (u + 0x1000u) & 0x7fffe000u;
+  const uint32_t hi = (m < 0x7f7fe000u ? m : 0x7f7fe000u) | (u & 0x80000000u);
+  return {hi, __float_as_uint(x - __uint_as_float(hi))};
 }
 __device__ __forceinline__ BParts tf32_bparts(float x) {
   const Parts p = tf32_parts(x);
-  const bool inf = fabsf(x) == INFINITY;
-  return {p.hi, inf ? 0u : p.lo, inf ? 0u : p.hi};
+  return {p.hi, p.lo, fabsf(x) == INFINITY ? 0u : p.hi};
+}
+// Where A's values are one at most, their lower parts may meet any finite number.
+__device__ __forceinline__ BParts tf32_bparts_of_weighted(float x) {
+  const Parts p = tf32_parts(x);
+  return {p.hi, p.lo, p.hi};
 }
 // d += a b without the product of the lower parts
 __device__ __forceinline__ void mma8_parts(float (&d)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], const BParts& b0,

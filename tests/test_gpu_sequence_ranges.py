@@ -33,3 +33,73 @@ def test_cross_fp32_of_values_of_one_sign(T, nq, nk, D):
     hold(out, ref, ref * (2 * (D + 8) * top + 16 + 8 * np.sqrt(nk / 16)) * U)
     # and they have no sign: their mean is that of the weights' errors, which are common to the channels
     assert abs(np.mean(out / ref - 1)) < 32 * U
+
+
+@pytest.mark.parametrize("bits", [0x7fffffff, 0x7fc00000, 0x7f800001, -1])
+def test_cross_fp32_of_any_nan(T, bits):
+    """Whatever its payload, a NaN stays one."""
+    r = np.random.default_rng(30)
+    for at in range(3):
+        x = [dev(r.normal(size=(40, 1, 16))) for _ in range(3)]
+        x[at][7, 0, 5:6].view(torch.int32).fill_(bits)
+        out = torch.empty_like(x[0])
+        T.cross_attention(*x, dev([0, 20, 40], "int64"), dev([0, 20, 40], "int64"), out)
+        assert bool(torch.isfinite(out[20:]).all())
+        bad = torch.isnan(out[:20, 0]).cpu()
+        assert bool(bad[7].all()) if at == 0 else bool(bad.all()) if at == 1 else bool(bad[:, 5].all())
+        assert int(bad.sum()) == (16, 320, 20)[at]
+
+
+# ---------------------------------------------------------------- attention: values next to the largest
+
+@pytest.mark.parametrize("t", ["float32", "bfloat16"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("nq,nk", [(3, 9), (1, 3000), (100, 700)])
+def test_cross_of_one_state_of_the_largest_values(T, t, sign, nq, nk):
+    """One state of them, whose weight is next to one or next to zero."""
+    r = np.random.default_rng(21)
+    D = 32
+    big = sign * torch.finfo(getattr(torch, t)).max
+    q, k, v = (dev(r.normal(size=(m, 1, D)), t) for m in (nq, nk, nk))
+    v[nk // 2] = big
+    out = torch.empty_like(q)
+    for ahead in (30.0, -8.0):
+        q[..., 0], k[..., 0], k[nk // 2, :, 0] = 1.0, 0.0, ahead
+        T.cross_attention(q, k, v, dev([0, nq], "int64"), dev([0, nk], "int64"), out, scale=1.0)
+        args = host(q), host(k)
+        ref = Q.cross_attention(*args, host(v), [0, nq], [0, nk], 1.0)
+        absv = Q.cross_attention(*args, np.abs(host(v)), [0, nq], [0, nk], 1.0)
+        top = np.linalg.norm(args[0], axis=-1).max() * np.linalg.norm(args[1], axis=-1).max()
+        hold(out, ref, rounding(t, ref) + absv * (2 * (D + 8) * top * U + (nk + 16) * U + (half_step(t) if t != "float32" else 0)))
+
+
+def test_cross_of_keys_next_to_the_largest_fp32(T):
+    """Scores are finite where the queries are small."""
+    D, n = 16, 40
+    top = torch.finfo(torch.float32).max
+    q = torch.full((5, 1, D), 2.0 ** -125, device="cuda")
+    k = torch.zeros((n, 1, D), device="cuda")
+    k[:, 0, 0] = top * torch.linspace(-1, 1, n, device="cuda")
+    k[3, 0, 1] = -top
+    v = dev(np.random.default_rng(22).normal(size=(n, 1, D)))
+    out = torch.empty_like(q)
+    T.cross_attention(q, k, v, dev([0, 5], "int64"), dev([0, n], "int64"), out, scale=1.0)
+    ref = Q.cross_attention(host(q), host(k), host(v), [0, 5], [0, n], 1.0)
+    hold(out, ref, 2 * (D + 8) * 16 * U * np.abs(host(v)).max())
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("nq,nk", [(3, 9), (1, 3000), (100, 700)])
+def test_cross_of_the_largest_values_alone(T, t, sign, nq, nk):
+    """All values are the largest: their average is it, though their sum is none."""
+    r = np.random.default_rng(23)
+    D = 32
+    big = sign * torch.finfo(getattr(torch, t)).max
+    q, k = (dev(r.normal(size=(m, 1, D)), t) for m in (nq, nk))
+    v = torch.full_like(k, big)
+    out = torch.empty_like(q)
+    T.cross_attention(q, k, v, dev([0, nq], "int64"), dev([0, nk], "int64"), out)
+    ref = np.full(out.shape, float(big))
+    # the weights' errors act on both sums
+    hold(out, ref, rounding(t, ref) + np.abs(ref) * (nk + 64) * U + (half_step(t) if t != "float32" else 0) * np.abs(ref))
