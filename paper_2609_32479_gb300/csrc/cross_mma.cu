@@ -164,12 +164,14 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
         m0 = t0, m1 = t1;
       }
       const float b0 = up - n0, b1 = up - n1;
+      float c0 = 0.0f, c1 = 0.0f;
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         x[n][0] = ex2(fmaf(x[n][0], a.scale2, b0)), x[n][1] = ex2(fmaf(x[n][1], a.scale2, b0));
         x[n][2] = ex2(fmaf(x[n][2], a.scale2, b1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, b1));
-        l0 += x[n][0] + x[n][1], l1 += x[n][2] + x[n][3];
+        c0 += x[n][0] + x[n][1], c1 += x[n][2] + x[n][3];
       }
+      l0 += c0, l1 += c1;
       uint32_t pa[2][4];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {

@@ -17,8 +17,8 @@
 // product, weights and product left the tensor cores idle most of the time: 448 us for 4,099
 // queries and 30,011 states of 8 heads of 64.)  A thread holds a block's 64 scores in registers:
 // one read of the tensor memory.
-// The maximum that the weights are taken against moves only when a row's grows by more than 2^8:
-// the weights then stay below 256, and O is hardly ever read back and scaled.
+// The maximum that the weights are taken against moves only when a row's grows by more than 2^LAG:
+// O is hardly ever read back and scaled.
 // With heads up to 64 channels two CTAs share an SM (112 KB and 256 columns each), one's products
 // beside the other's exponentials.
 //
@@ -47,7 +47,10 @@ constexpr uint32_t ATOM = BLOCK * 128;       // 64 states of 64 channels
 constexpr uint64_t LIMIT_NS = 2000000000ull;   // of a wait; a test hook shortens it
 constexpr int STAGES = 4;
 static_assert(BLOCK == 64, "a block's weights are one swizzled row of 128 bytes");
-constexpr float LAG = 8.0f;                  // the maximum may be 2^8 behind
+// The maximum that the weights are taken against may be 2^LAG behind.  Not further in fp16: the
+// weights lie as much lower in the type's range (2^-38 of the largest is what one may be off).
+template <class T>
+constexpr float LAG = __is_same(T, __half) ? 2.0f : 8.0f;
 
 struct TcArgs {
   CaArgs a;
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     bool ok = true;
     while (ok && passes.next(ps)) {
       float m = -INFINITY, l = 0.0f;                   // m: score * scale2 that the weights are taken against
-      const float up = __is_same(T, __half) ? 0.0f : weight_up<T>(ps.len) - LAG;
+      const float up = weight_up<T>(ps.len) - LAG<T>;
       for (int j = ps.j0; j < ps.j1; ++j, ++n) {
         const uint32_t place = n & 1, phase = n >> 1 & 1;
         ok = __all_sync(FULL, mbar_wait(s_full + 8 * place, phase, abort, p.limit_ns));
@@ -311,23 +314,23 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
         if (j == ps.j0) {
           m = top;
         } else {
-          const bool move = top > m + LAG;
-          if (__any_sync(FULL, move)) {
+          if (__any_sync(FULL, top > m + LAG<T>)) {
             // the product before this block adds to O until then
             ok = __all_sync(FULL, mbar_wait(p_free + 8 * (place ^ 1), (n - 1) >> 1 & 1, abort, p.limit_ns));
             if (!ok) break;
             tc_fence_after();
+            const bool move = top > m;                 // (with one row of the warp all that have grown)
             const float f = move ? ex2(m - top) : 1.0f;
             if (move) m = top;
             l *= f;
 #pragma unroll 1
-            for (int c = 0; c < NA * 4; ++c) {
-              float o[16];
-              tmem_ld16(tmem_o + lanes + 16 * c, o);
+            for (int c = 0; c < NA * 2; ++c) {
+              float o[32];
+              tmem_ld32(tmem_o + lanes + 32 * c, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] *= f;
-              tmem_st16(tmem_o + lanes + 16 * c, o);
+              for (int i = 0; i < 32; ++i) o[i] *= f;
+              tmem_st32(tmem_o + lanes + 32 * c, o);
             }
             tmem_st_wait();
           }

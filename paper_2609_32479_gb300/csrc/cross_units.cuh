@@ -33,13 +33,17 @@ struct CaArgs {
 constexpr int FARTHEST = 0x7fffffff;
 
 // Weights are 2^(score - largest + up), and so are their sums and O, which the division takes out
-// again: with as many weights of one as there are states, values next to the type's largest would
-// leave fp32 in O where their average does not.  (Not further down than these need: values next to
-// the smallest would be lost.  2^31 values of fp16 are far below fp32's largest.)  Alike for all
-// parts of a row.
+// again.  Alike for all parts of a row.
+// fp32, bf16: with as many weights of one as there are states, values next to the type's largest
+// would leave fp32 in O where their average does not.  (Not further down than these need: values
+// next to the smallest would be lost.)
+// fp16: the weights as operands have its range, 2^-24 to 65504, of which 2^15 for the largest uses
+// all: they keep their bits down to 2^-29 of it, and none is more than 2^-40 of it off.  (Taken
+// against one, they were lost below 2^-25: many states 17 below one of theirs, together as heavy,
+// counted in the sum but not in O.)  2^31 values of fp16 by 2^15 are far below fp32's largest.
 template <class T>
 __device__ __forceinline__ float weight_up(int states) {
-  return __is_same(T, __half) ? 0.0f : -(float)(32 - __clz(states));
+  return __is_same(T, __half) ? 15.0f : -(float)(32 - __clz(states));
 }
 
 // o f, an average of finite values where o is finite: held at the largest fp32, which the roundings

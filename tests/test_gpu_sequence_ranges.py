@@ -52,7 +52,7 @@ def test_cross_fp32_of_any_nan(T, bits):
 
 # ---------------------------------------------------------------- attention: values next to the largest
 
-@pytest.mark.parametrize("t", ["float32", "bfloat16"])
+@pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("sign", [1.0, -1.0])
 @pytest.mark.parametrize("nq,nk", [(3, 9), (1, 3000), (100, 700)])
 def test_cross_of_one_state_of_the_largest_values(T, t, sign, nq, nk):
@@ -103,3 +103,35 @@ def test_cross_of_the_largest_values_alone(T, t, sign, nq, nk):
     ref = np.full(out.shape, float(big))
     # the weights' errors act on both sums
     hold(out, ref, rounding(t, ref) + np.abs(ref) * (nk + 64) * U + (half_step(t) if t != "float32" else 0) * np.abs(ref))
+
+
+# ---------------------------------------------------------------- attention: small weights
+
+def weights_tol(t):
+    """(relative, absolute against a row's largest) error of a weight as an operand.  fp16: two to the
+    13 and up are what the largest weight may be taken as, half of the type's smallest step is 2^-25."""
+    return half_step(t) if t != "float32" else 8 * U, 2.0 ** -38 if t == "float16" else 0.0
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("nq", [1, 100])
+@pytest.mark.parametrize("gap,n,first", [(12.0, 30011, 0.0), (15.0, 30011, 0.0), (18.0, 30011, 0.0), (20.0, 30011, 0.0),
+                                         (17.4, 30011, 1.0), (17.4, 300000, 1.0), (16.0, 600, 0.0)])
+def test_cross_of_one_state_far_ahead(T, t, nq, gap, n, first):
+    """One state whose score is `gap` above all others', which are equal: their weights are e^-gap each."""
+    D = 64
+    q = torch.zeros((nq, 1, D), device="cuda")
+    q[:, :, 0] = 1
+    k = torch.zeros((n, 1, D), device="cuda")
+    k[n // 3, 0, 0] = 1
+    v = torch.ones((n, 1, D), device="cuda")
+    v[n // 3] = first
+    q, k, v = (x.to(getattr(torch, t)) for x in (q, k, v))
+    out = torch.empty_like(q)
+    T.cross_attention(q, k, v, dev([0, nq], "int64"), dev([0, n], "int64"), out, scale=gap)
+    w = (n - 1) * np.exp(-float(np.float32(gap)))
+    y = np.full((nq, 1, D), (first + w) / (1 + w))
+    rel, least = weights_tol(t)
+    # the others' weights: their scores are 0, the first one's is exact; n sums; 64 u for the exponent's product
+    tol = rounding(t, y) + (rel + (np.sqrt(n) + 64) * U) * y + least * n
+    hold(out, y, tol)
