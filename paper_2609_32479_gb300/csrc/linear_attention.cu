@@ -17,8 +17,9 @@ using namespace seqops;
 // memory as broadcasts, 8 rows at a time through a ring that the warp fills by asynchronous
 // copies.  Several columns a lane share what a row costs whatever its columns (loads,
 // exponentials, addresses: 90 of 116 instructions with one).  Measured: 20,011 tracks and parts
-// of tracks, 4 heads of 32 x 48, states in and out: 776 us, 3.4 TB/s; one column a lane 1136,
-// a third multiply-add a value for the decay 814.
+// of tracks, 4 heads of 32 x 48, states in and out: 747 us a call, 3.5 TB/s; one column a lane 1136.
+// Every row decays the state itself: a factor kept beside it, which would save the product, makes
+// values up to that factor larger than the state.
 constexpr int CH = 8, NST = 2;
 
 template <int DK, int CPL>
@@ -120,29 +121,20 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
   };
 
   for (int s = 0; s < NST; ++s) issue(slot(s));
-  float S[CPL][HALF];
+  uint64_t S[CPL][HALF / 2];     // pairs of key channels, an instruction for two
 #pragma unroll
   for (int j = 0; j < CPL; ++j)
 #pragma unroll
-    for (int i = 0; i < HALF; ++i) S[j][i] = 0.0f;
-  // the state is exp(G) S: a row's decay goes into G, and its values are taken by exp(-G), which
-  // leaves two multiply-adds a value of the state and row; beyond e^FOLD the factor goes into S
-  float G = 0.0f;
-  constexpr float FOLD = 14.0f;
-  auto fold = [&] {
-    const float f = expf(G);
-    G = 0.0f;
-#pragma unroll
-    for (int j = 0; j < CPL; ++j)
-#pragma unroll
-      for (int i = 0; i < HALF; ++i) S[j][i] *= f;
-  };
+    for (int i = 0; i < HALF / 2; ++i) S[j][i] = 0;
   auto put_state = [&](float* st) {
 #pragma unroll
     for (int j = 0; j < CPL; ++j)
 #pragma unroll
-      for (int i = 0; i < HALF; ++i)
-        if (col + 16 * j < width && i0 + i < a.K) st[(i0 + i) * a.V + c0 + col + 16 * j] = S[j][i];
+      for (int i = 0; i < HALF; i += 2)
+        if (col + 16 * j < width && i0 + i < a.K) {
+          const float2 x = parts(S[j][i / 2]);
+          st[(i0 + i) * a.V + c0 + col + 16 * j] = x.x, st[(i0 + i + 1) * a.V + c0 + col + 16 * j] = x.y;
+        }
   };
   float total = 0.0f;
   for (int s = 0;; s = s + 1 == NST ? 0 : s + 1) {
@@ -154,49 +146,46 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
     if (flags & FIRST) {
       const bool st = beginning(flags & GOES_ON, flags & ENDS, seq) != nullptr;
       const float* src = w.state() + i0 * COLS + col;
-      G = 0.0f;
 #pragma unroll
       for (int j = 0; j < CPL; ++j)
 #pragma unroll
-        for (int i = 0; i < HALF; ++i) S[j][i] = st && i0 + i < a.K ? src[i * COLS + 16 * j] : 0.0f;
+        for (int i = 0; i < HALF; i += 2)
+          S[j][i / 2] = st && i0 + i < a.K ? both(src[i * COLS + 16 * j], src[(i + 1) * COLS + 16 * j]) : 0;
       if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) put_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);
     }
+    float sum = 0.0f;
     for (int r = 0; r < len; ++r) {
-      G += w.g[r];
-      if (STATE_ONLY) total += w.g[r];
-      if (!(fabsf(G) <= FOLD)) fold();
-      const float in = expf(-G);
-      float x[CPL], acc[CPL][2];
+      const float e = expf(w.g[r]);
+      if (STATE_ONLY) sum += w.g[r];
+      const uint64_t decay = both(e, e);
+      uint64_t x[CPL], acc[CPL];
 #pragma unroll
-      for (int j = 0; j < CPL; ++j) x[j] = in * w.v[r][col + 16 * j], acc[j][0] = acc[j][1] = 0.0f;
+      for (int j = 0; j < CPL; ++j) x[j] = both(w.v[r][col + 16 * j], w.v[r][col + 16 * j]), acc[j] = 0;
 #pragma unroll
       for (int i = 0; i < HALF; i += 4) {
-        const float4 k4 = *reinterpret_cast<const float4*>(&w.k[r][i0 + i]);
-        const float kk[4] = {k4.x, k4.y, k4.z, k4.w};
-        float4 q4;
-        if (!STATE_ONLY) q4 = *reinterpret_cast<const float4*>(&w.q[r][i0 + i]);
-        const float qq[4] = {q4.x, q4.y, q4.z, q4.w};
+        const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(&w.k[r][i0 + i]);
+        ulonglong2 q4;
+        if (!STATE_ONLY) q4 = *reinterpret_cast<const ulonglong2*>(&w.q[r][i0 + i]);
 #pragma unroll
-        for (int j = 0; j < CPL; ++j)
-#pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            S[j][i + n] = fmaf(kk[n], x[j], S[j][i + n]);
-            if (!STATE_ONLY) acc[j][n & 1] = fmaf(qq[n], S[j][i + n], acc[j][n & 1]);
-          }
+        for (int j = 0; j < CPL; ++j) {
+          uint64_t(&s)[2] = *reinterpret_cast<uint64_t(*)[2]>(&S[j][i / 2]);
+          s[0] = fma2(k4.x, x[j], mul2(s[0], decay)), s[1] = fma2(k4.y, x[j], mul2(s[1], decay));
+          if (!STATE_ONLY) acc[j] = fma2(q4.y, s[1], fma2(q4.x, s[0], acc[j]));
+        }
       }
       if (!STATE_ONLY) {
         float* o = out + (int64_t)(row + dir * r) * a.os;
-        const float f = a.scale * expf(G);
 #pragma unroll
         for (int j = 0; j < CPL; ++j) {
-          float y = acc[j][0] + acc[j][1];
+          const float2 p = parts(acc[j]);
+          float y = p.x + p.y;
           y += __shfl_xor_sync(FULL, y, 16);
-          if (part == 0 && col + 16 * j < width) o[16 * j] = f * y;
+          if (part == 0 && col + 16 * j < width) o[16 * j] = a.scale * y;
         }
       }
     }
+    total += sum;
     if ((flags & LAST) && (STATE_ONLY || ((flags & ENDS) && a.state_out))) {
-      fold();
       put_state(STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV);
       if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
     }

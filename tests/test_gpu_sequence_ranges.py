@@ -135,3 +135,51 @@ def test_cross_of_one_state_far_ahead(T, t, nq, gap, n, first):
     # the others' weights: their scores are 0, the first one's is exact; n sums; 64 u for the exponent's product
     tol = rounding(t, y) + (rel + (np.sqrt(n) + 64) * U) * y + least * n
     hold(out, y, tol)
+
+
+# ---------------------------------------------------------------- linear attention: the whole range, long decays
+
+@pytest.mark.parametrize("t", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [1e33, 1e-33])
+@pytest.mark.parametrize("length", [40, 1300])
+def test_linear_of_values_at_the_ends_of_fp32(T, t, size, length):
+    """Sums of 1e33 are finite, and those of 1e-33 keep their bits."""
+    r = np.random.default_rng(20)
+    H, K, V = 2, 32, 32
+    n = length + 25
+    q, k, v = slab(r, [(n, H, K), (n, H, K), (n, H, V)], t)
+    k, v = (0.1 * k.abs()).contiguous(), (v.abs() * size).contiguous()
+    q = (0.1 * q).contiguous()
+    g = dev(-0.9 * np.ones((n, H)))
+    off = np.array([0, 25, n])
+    out, s1 = torch.empty_like(v), torch.empty((2, H, K, V), device="cuda")
+    T.linear_attention(q, k, v, g, dev(off, "int64"), out, state_out=s1)
+    args = host(q), host(k), host(v), host(g), off, 1.0, False, None
+    o, s = Q.linear_attention(*args)
+    to, ts = linear_tol(*args, t, o, s)
+    hold(out, o, to, "out")
+    hold(s1, s, ts, "state")
+
+
+@pytest.mark.parametrize("t", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rate,length,others", [(0.001, 16000, 383), (0.003, 2048, 100), (0.0005, 40000, 1)])
+def test_linear_of_a_constant_decay_over_a_long_sequence(T, t, rate, length, others):
+    """One rate for all rows: the errors of its exponentials are all alike and add up.  (Uncut among
+    many sequences of one row; cut with few.)"""
+    H, K, V = 1, 8, 16
+    n = length + others
+    off = np.concatenate([[0], length + np.arange(others + 1)]).astype(np.int64)
+    x = torch.ones((n, H, K), device="cuda").to(getattr(torch, t))
+    v = torch.ones((n, H, V), device="cuda").to(x.dtype)
+    g = torch.full((n, H), -rate, device="cuda")
+    out, s1 = torch.empty_like(v), torch.empty((others + 1, H, K, V), device="cuda")
+    T.linear_attention(x, x, v, g, dev(off, "int64"), out, scale=0.125, state_out=s1)
+    gd = float(np.float32(-rate))
+    s = np.ones(others + 1)
+    s[0] = np.expm1(gd * length) / np.expm1(gd)
+    # a row: its exponential (an ulp, u below 1), a product, a sum, over what is left of all rows
+    tol = 3 * U * s[0] + 16 * U
+    hold(s1, np.broadcast_to(s[:, None, None, None], s1.shape), tol * s[:, None, None, None])
+    y = np.expm1(gd * np.arange(1, length + 1)) / np.expm1(gd)
+    y = np.broadcast_to(y[:, None, None], (length, H, V))
+    hold(out[:length], y, rounding(t, y) + (3 * U * s[0] + 32 * U + (2 * half_step(t) if t != "float32" else 0)) * y)
