@@ -32,7 +32,7 @@ struct Piece {
   bool goes_on;            // it does not hold the sequence's beginning
   bool ends;               // it holds the sequence's end
 };
-constexpr int FAR = 1 << 30;
+constexpr int FAR = 1 << 29;      // (the distance of two ends, too, fits 32 bits)
 
 // The sequences' offsets from the base row, a warp reading 32 at a time.
 class Offsets {

@@ -183,3 +183,24 @@ def test_linear_of_a_constant_decay_over_a_long_sequence(T, t, rate, length, oth
     y = np.expm1(gd * np.arange(1, length + 1)) / np.expm1(gd)
     y = np.broadcast_to(y[:, None, None], (length, H, V))
     hold(out[:length], y, rounding(t, y) + (3 * U * s[0] + 32 * U + (2 * half_step(t) if t != "float32" else 0)) * y)
+
+
+@pytest.mark.parametrize("rev", [False, True])
+def test_linear_of_a_sequence_longer_than_31_bits_count(T, rev):
+    """All rows are ones and a row forgets half: the outputs stand at 16 from the tenth row on."""
+    n = 2 ** 31 + 5000
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 100 GB")
+    x = torch.ones((n, 1, 8), dtype=torch.bfloat16, device="cuda")
+    g = torch.full((n, 1), -float(np.log(2.0)), device="cuda")
+    out = torch.zeros_like(x)
+    s1 = torch.zeros((1, 1, 8, 8), device="cuda")
+    work = torch.empty(T.linear_attention_workspace(n, 1, 1, 8, 8), dtype=torch.uint8, device="cuda")
+    T.linear_attention(x, x, x, g, dev([0, n], "int64"), out, reverse=rev, state_out=s1, workspace=work)
+    flat = out.view(-1)
+    step = 1 << 28
+    bad = sum(int((flat[at:at + step] != 16).sum()) for at in range(0, flat.numel(), step))
+    del x, g, out, flat, work
+    torch.cuda.empty_cache()
+    # the first rows, by how much a bf16 can tell 16 from: 16 (1 - 2^-i) rounds to it from i = 9 on
+    assert bad <= 9 * 8 and bool(torch.isclose(s1, torch.full_like(s1, 2.0), rtol=1e-5).all())
