@@ -491,8 +491,11 @@ int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, con
 
 /* The counterpart of trackfit_device_errors for the operators: synchronises `stream` and
  * returns TRACKFIT_ERR_TIMEOUT if a bounded wait of an operator's kernel on the current
- * device has expired since the last call (outputs written since then are not valid), else
- * OK. */
+ * device has expired, whatever its stream, since the calling thread last asked with this
+ * stream (with a pair of thread and stream that has not asked before, or not among the
+ * thread's last 64: since the program began), else OK.  Outputs of the device's operators
+ * written since then are not valid; of their streams, only the one given is waited for.
+ * Nothing is taken from what other threads, or calls with other streams, are told. */
 int trackfit_operator_errors(void* stream);
 
 /* Test hook for the bounded waits of the operators' kernels (trackfit_cross_attention, 16-bit

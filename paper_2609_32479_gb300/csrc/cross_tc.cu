@@ -121,7 +121,7 @@ __device__ __forceinline__ int block_at(const Pass& p, int j) {
   return p.lo + ((int64_t)(j + 1) * BLOCK > p.len ? p.len - BLOCK : j * BLOCK);
 }
 
-__device__ unsigned long long g_expired;   // CTAs that gave up, since trackfit_operator_errors last asked
+__device__ unsigned long long g_expired;   // CTAs that gave up; it only grows
 
 __device__ __forceinline__ void give_up(Bars* s) {
   if (atomicExch(&s->abort_flag, 1) == 0) atomicAdd(&g_expired, 1ull);
@@ -471,15 +471,39 @@ extern "C" int trackfit_debug_operator_wait(int64_t limit_ns, int32_t hold) {
   return TRACKFIT_OK;
 }
 
+namespace {
+// What a thread was told of last, for each stream that it asked with: one that asks takes nothing
+// away from another.  A pair that finds no place any more, or had to give it up, is told of all.
+struct Told {
+  int dev;
+  void* stream;
+  unsigned long long n;
+};
+constexpr int TOLD = 64;
+thread_local Told t_told[TOLD];
+thread_local int t_pairs = 0;      // ever, of which the last TOLD have a place
+}  // namespace
+
 extern "C" int trackfit_operator_errors(void* stream) {
   tf_nvtx_range nvtx_range("trackfit_operator_errors");
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   void* p = nullptr;
   unsigned long long n = 0;
-  cudaError_t e = cudaGetSymbolAddress(&p, g_expired);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaGetSymbolAddress(&p, g_expired);
   if (e == cudaSuccess) e = cudaMemcpyAsync(&n, p, sizeof(n), cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaMemsetAsync(p, 0, sizeof(n), st);
   if (e == cudaSuccess) e = cudaStreamSynchronize(st);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  return n > 0 ? TRACKFIT_ERR_TIMEOUT : TRACKFIT_OK;
+  Told* told = nullptr;
+  for (int i = 0; i < t_pairs && i < TOLD && !told; ++i)
+    if (t_told[i].dev == dev && t_told[i].stream == stream) told = &t_told[i];
+  if (!told) {
+    told = &t_told[t_pairs % TOLD];
+    t_pairs = t_pairs + 1 < 2 * TOLD ? t_pairs + 1 : TOLD;
+    *told = {dev, stream, 0};
+  }
+  const bool more = n > told->n;
+  told->n = n;
+  return more ? TRACKFIT_ERR_TIMEOUT : TRACKFIT_OK;
 }

@@ -570,7 +570,7 @@ def cross_attention(q, k, v, q_offsets, kv_offsets, out, scale: Optional[float] 
 
 def operator_errors(stream=None) -> int:
     """OK, or ERR_TIMEOUT when a bounded wait of an operator's kernel on the current device has
-    expired since the last call (synchronises)."""
+    expired since this thread last asked with this stream (synchronises it)."""
     return load().trackfit_operator_errors(_stream_handle(stream))
 
 

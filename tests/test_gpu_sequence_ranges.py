@@ -204,3 +204,44 @@ def test_linear_of_a_sequence_longer_than_31_bits_count(T, rev):
     torch.cuda.empty_cache()
     # the first rows, by how much a bf16 can tell 16 from: 16 (1 - 2^-i) rounds to it from i = 9 on
     assert bad <= 9 * 8 and bool(torch.isclose(s1, torch.full_like(s1, 2.0), rtol=1e-5).all())
+
+
+# ---------------------------------------------------------------- expired waits, asked for by several
+
+def test_an_expired_wait_is_reported_to_every_thread_and_stream_that_asks(T):
+    import threading
+    torch.cuda.synchronize()
+    device = torch.cuda.current_device()
+    streams = [torch.cuda.current_stream(), torch.cuda.Stream()]
+    x = torch.randn((700, 1, 64), device="cuda").to(torch.bfloat16)
+    off, out = dev([0, 700], "int64"), torch.empty_like(x)
+    go, asked, seen = threading.Event(), threading.Event(), []
+
+    def other():
+        torch.cuda.set_device(device)
+        for s in streams:                  # what expired before this test is told to whoever first asks
+            T.operator_errors(s)
+        seen.append([T.operator_errors(s) for s in streams])
+        asked.set()
+        go.wait(60)
+        seen.append([T.operator_errors(s) for s in streams])
+        seen.append([T.operator_errors(s) for s in streams])
+
+    thread = threading.Thread(target=other)
+    thread.start()
+    assert asked.wait(60) and seen[0] == [T.OK] * 2
+    for s in streams:
+        T.operator_errors(s)
+    assert [T.operator_errors(s) for s in streams] == [T.OK, T.OK]
+    T.debug_operator_wait(20_000_000, True)
+    try:
+        T.cross_attention(x, x, x, off, off, out, stream=streams[0])
+        torch.cuda.synchronize()
+    finally:
+        T.debug_operator_wait()
+    go.set()
+    thread.join(60)
+    assert seen[1:] == [[T.ERR_TIMEOUT] * 2, [T.OK] * 2]
+    # what the other thread was told is still told here, for each stream once
+    assert [T.operator_errors(s) for s in reversed(streams)] == [T.ERR_TIMEOUT] * 2
+    assert [T.operator_errors(s) for s in streams] == [T.OK] * 2
