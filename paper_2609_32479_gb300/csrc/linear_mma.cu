@@ -29,10 +29,10 @@
 //
 // Roundings: the products' operands are 16 bits.  Q K^T o L is split into two bf16 parts, the
 // decayed V into two, or three where the state is asked for (bf16: 8, 16, 24 bits; its chunks'
-// sums are then added outside the products too), so that the states keep fp32.  The state's
-// operand of Q S is rounded once, an error of the output's own rounding's size.  fp16 has the
-// bits but not the range for Q K^T and S: these go through tf32 products (11 bits, fp32's
-// range); the decayed V, no larger than V with g <= 0, is split in two.
+// sums are then added outside the products too): states asked for keep fp32.  The state's operand of Q S is
+// rounded once, an error of the output's own rounding's size.  fp16 has the bits but not the range
+// for Q K^T, S and the decayed V (whose lower parts would fall below its smallest step, as V itself
+// may lie next to that): these go through tf32 products (11 bits, fp32's range), V in two parts.
 //
 // Measured: 131,072 tracks, 4 heads of 32, bf16: 381 us, 5.0 TB/s of the 6.8 that a copy moves;
 // issued instructions bound it (two thirds of the slots with 16 warps an SM, the rest waits for
@@ -115,6 +115,10 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
   // With 128 registers a thread (16 warps an SM) q and k are read where they are used; with 255
   // (8 warps) early, and their place filled again: 221 instead of 305 us at K = 64, when both were tried
   constexpr bool EARLY = NG == 2;
+  // A chunk's own sum first, added to the state outside the products: their accumulation cuts bits
+  // off, and on the state itself that would shrink it a little with every chunk (2^-24: nothing that
+  // bf16 outputs show)
+  constexpr bool APART = EXACT || !BF;
   constexpr int VC = NV * 2;                           // channels of V a lane
   constexpr int SLOT = slot_bytes(NG, NV);
   const int lane = threadIdx.x;
@@ -431,7 +435,7 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
           for (int j = 0; j < KT; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st[m][j][i] = 0.0f;
-      } else if (!EXACT) {
+      } else if (!APART) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -450,7 +454,8 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
       Z = ex2(Z);
       const float w0 = __shfl_sync(FULL, Z, 2 * t), w1 = __shfl_sync(FULL, Z, 2 * t + 1);
       const float w8 = __shfl_sync(FULL, Z, 2 * t + 8), w9 = __shfl_sync(FULL, Z, 2 * t + 9);
-      constexpr int TERMS = BF && EXACT ? 3 : 2;
+      // the decayed values in parts; fp16 has the bits but not the range for lower parts: tf32
+      constexpr int TERMS = BF ? (EXACT ? 3 : 2) : 4;  // (fp16: of both parts the even and the odd rows)
       uint32_t va[TERMS][MT][4];
 #pragma unroll
       for (int n = 0; n < NV; ++n)
@@ -458,14 +463,20 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
         for (int i = 0; i < 2; ++i) {
           float2 y = halves(vb[n][i], T());
           y.x *= i ? w8 : w0, y.y *= i ? w9 : w1;
+          if (BF) {
 #pragma unroll
-          for (int e = 0; e < TERMS; ++e) {
-            const uint32_t u = pack2(y.x, y.y, T());
-            va[e][n / 2][2 * i + (n & 1)] = u;
-            if (e + 1 < TERMS) {
-              const float2 z = halves(u, T());
-              y.x -= z.x, y.y -= z.y;
+            for (int e = 0; e < TERMS; ++e) {
+              const uint32_t u = pack2(y.x, y.y, T());
+              va[e][n / 2][2 * i + (n & 1)] = u;
+              if (e + 1 < TERMS) {
+                const float2 z = halves(u, T());
+                y.x -= z.x, y.y -= z.y;
+              }
             }
+          } else {
+            const Parts px = tf32_split(y.x), py = tf32_split(y.y);
+            va[0][n / 2][2 * i + (n & 1)] = px.hi, va[1][n / 2][2 * i + (n & 1)] = py.hi;
+            va[2][n / 2][2 * i + (n & 1)] = px.lo, va[3][n / 2][2 * i + (n & 1)] = py.lo;
           }
         }
 #pragma unroll
@@ -476,21 +487,29 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
           load_shared(k[i0][1], slot + (2 * NG + 2 * i0 + 1) * 512);
         }
         const uint32_t b0 = turned(k[i0][0][j % 4]), b1 = turned(k[i0][1][j % 4]);
+        const float2 k0 = halves(b0, T()), k1 = halves(b1, T());
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          if (EXACT) {
-            // a chunk's own sum first: the products' accumulation cuts bits off, and on the state
-            // itself that would shrink it a little with every chunk
-            float d[4];
+          float d[4];
+          if (!APART) {
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) mma16(st[m][j], va[e][m], b0, b1, T());
+            continue;
+          }
+          if (BF) {
             mma16_new(d, va[0][m], b0, b1, T());
 #pragma unroll
             for (int e = 1; e < TERMS; ++e) mma16(d, va[e][m], b0, b1, T());
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st[m][j][i] = fmaf(st[m][j][i], f, d[i]);
           } else {
+            d[0] = d[1] = d[2] = d[3] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < TERMS; ++e) mma16(st[m][j], va[e][m], b0, b1, T());
+            for (int e = TERMS - 2; e >= 0; e -= 2) {
+              mma8(d, va[e][m][0], va[e][m][1], va[e + 1][m][0], va[e + 1][m][1], __float_as_uint(k0.x), __float_as_uint(k0.y));
+              mma8(d, va[e][m][2], va[e][m][3], va[e + 1][m][2], va[e + 1][m][3], __float_as_uint(k1.x), __float_as_uint(k1.y));
+            }
           }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st[m][j][i] = fmaf(st[m][j][i], f, d[i]);
         }
       }
       if ((flags & LAST) && (STATE_ONLY || (flags & ENDS))) {

@@ -54,6 +54,11 @@ __device__ __forceinline__ uint32_t tf32(float x) {   // to nearest, 11 bits
 struct Parts {
   uint32_t hi, lo;
 };
+// The parts of a number that is not next to the largest, 11 bits each of 24: off by 2^-22 at most.
+__device__ __forceinline__ Parts tf32_split(float x) {
+  const uint32_t hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+  return {hi, __float_as_uint(x - __uint_as_float(hi))};
+}
 struct BParts {
   uint32_t hi, lo, fin;
 };

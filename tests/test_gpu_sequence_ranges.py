@@ -245,3 +245,31 @@ def test_an_expired_wait_is_reported_to_every_thread_and_stream_that_asks(T):
     # what the other thread was told is still told here, for each stream once
     assert [T.operator_errors(s) for s in reversed(streams)] == [T.ERR_TIMEOUT] * 2
     assert [T.operator_errors(s) for s in streams] == [T.OK] * 2
+
+
+# ---------------------------------------------------------------- linear attention: fp16 values of any size
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("K,V", [(16, 16), (32, 48), (64, 64), (128, 40)])
+@pytest.mark.parametrize("size", [1e-2, 1e-4, 3e-7, 3e4])
+def test_linear_states_of_values_of_any_size(T, t, K, V, size):
+    """States are fp32 sums of decayed rows, however small these are in their own type."""
+    r = np.random.default_rng(26)
+    H = 2
+    lengths = [0, 1, 2, 15, 16, 17, 20, 33, 700]
+    off = np.concatenate([[0], np.cumsum(lengths)])
+    n = int(off[-1])
+    q, k, v = slab(r, [(n, H, K), (n, H, K), (n, H, V)], t)
+    v = (v * size * torch.logspace(-3, 0, V, device="cuda").to(v.dtype)).clamp(-6e4, 6e4)
+    g = dev(-0.3 * r.random((n, H)))
+    out, s1 = torch.empty_like(v), torch.empty((len(lengths), H, K, V), device="cuda")
+    T.linear_attention(q, k, v, g, dev(off, "int64"), out, scale=1e-3 if size > 1 else 1.0, state_out=s1)
+    args = host(q), host(k), host(v), host(g), off, 1e-3 if size > 1 else 1.0, False, None
+    o, s = Q.linear_attention(*args)
+    to, ts = linear_tol(*args, t, o, s)
+    # a row of which less than fp32's smallest, 2^-126, is left counts nothing: as many of them as there are
+    # rows, with |k| of 6, are below 2^-113
+    hold(s1, s, ts + 2.0 ** -113, "state")
+    hold(out, o, to, "out")
+    T.linear_attention(q, k, v, g, dev(off, "int64"), out, scale=args[5])
+    hold(out, o, to, "out without states")
