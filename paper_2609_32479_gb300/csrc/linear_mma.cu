@@ -27,12 +27,14 @@
 //
 // Rows beyond a chunk's are zeros, so that nothing of another sequence enters a product.
 //
-// Roundings: the products' operands are 16 bits.  Q K^T o L is split into two bf16 parts, the
-// decayed V into two, or three where the state is asked for (bf16: 8, 16, 24 bits; its chunks'
-// sums are then added outside the products too): states asked for keep fp32.  The state's operand of Q S is
-// rounded once, an error of the output's own rounding's size.  fp16 has the bits but not the range
-// for Q K^T, S and the decayed V (whose lower parts would fall below its smallest step, as V itself
-// may lie next to that): these go through tf32 products (11 bits, fp32's range), V in two parts.
+// Roundings: the products' operands are 16 bits, and what is not a row as it came is split.
+// bf16: Q K^T o L, the state as the operand of Q S, and the decayed V into two parts (16 bits), V
+// into three where the state is asked for (24 bits; its chunks' sums are then added outside the
+// products too).  fp16 has the bits but not the range for any of them (a lower part of V would fall
+// below its smallest step, as V itself may lie next to that): all go through tf32 products (fp32's
+// range) in two parts of 11 bits.  Outputs are off by their own rounding and by 2^-16 (bf16) or
+// 2^-22 of what is added up; states asked for keep fp32.  With one part each for S and the fp16
+// weights it was 2^-8 and 2^-11 of it, for 7 % (tracks, bf16) to 20 % (fp16) less time.
 //
 // Measured: 131,072 tracks, 4 heads of 32, bf16: 381 us, 5.0 TB/s of the 6.8 that a copy moves;
 // issued instructions bound it (two thirds of the slots with 16 warps an SM, the rest waits for
@@ -351,24 +353,30 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
           mma16(s0, qa, k[i0][0][w], k[i0][0][w + 1], T());
           mma16(s1, qa, k[i0][1][w], k[i0][1][w + 1], T());
         }
-        if (!zero) {
+        if (!zero) {                                   // S in two parts
           if (BF) {
 #pragma unroll
             for (int n = 0; n < NV; ++n) {
               const float(&u0)[4] = st[n / 2][2 * kk], (&u1)[4] = st[n / 2][2 * kk + 1];
               const int i = (n & 1) * 2;
-              mma16(o[n], qa, pack2(u0[i], u0[i + 1], T()), pack2(u1[i], u1[i + 1], T()), T());
+              const uint32_t b0 = pack2(u0[i], u0[i + 1], T()), b1 = pack2(u1[i], u1[i + 1], T());
+              const float2 h0 = halves(b0, T()), h1 = halves(b1, T());
+              mma16(o[n], qa, pack2(u0[i] - h0.x, u0[i + 1] - h0.y, T()), pack2(u1[i] - h1.x, u1[i + 1] - h1.y, T()), T());
+              mma16(o[n], qa, b0, b1, T());
             }
           } else {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {              // 8 channels of the key a time
               const float2 x0 = halves(qa[2 * e], T()), x1 = halves(qa[2 * e + 1], T());
+              const uint32_t a0 = __float_as_uint(x0.x), a1 = __float_as_uint(x1.x);
+              const uint32_t a2 = __float_as_uint(x0.y), a3 = __float_as_uint(x1.y);
 #pragma unroll
               for (int n = 0; n < NV; ++n) {
                 const float(&u)[4] = st[n / 2][2 * kk + e];
                 const int i = (n & 1) * 2;
-                mma8(o[n], __float_as_uint(x0.x), __float_as_uint(x1.x), __float_as_uint(x0.y), __float_as_uint(x1.y),
-                     tf32(u[i]), tf32(u[i + 1]));
+                const Parts b0 = tf32_split(u[i]), b1 = tf32_split(u[i + 1]);
+                mma8(o[n], a0, a1, a2, a3, b0.lo, b1.lo);
+                mma8(o[n], a0, a1, a2, a3, b0.hi, b1.hi);
               }
             }
           }
@@ -404,15 +412,19 @@ __global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kerne
             },
             zero, o, vb, len, g, t);
       } else {
-        const uint32_t f0 = tf32(s0[0]), f1 = tf32(s0[1]), f2 = tf32(s0[2]), f3 = tf32(s0[3]);
-        const uint32_t f6 = tf32(s1[2]), f7 = tf32(s1[3]);
+        const Parts f0 = tf32_split(s0[0]), f1 = tf32_split(s0[1]), f2 = tf32_split(s0[2]), f3 = tf32_split(s0[3]);
+        const Parts f6 = tf32_split(s1[2]), f7 = tf32_split(s1[3]);
         add_rows(
             T(),
             [&](float(&d)[4], uint32_t b0, uint32_t b1, bool anew) {
               if (anew) d[0] = d[1] = d[2] = d[3] = 0.0f;
               const float2 v0 = halves(b0, T()), v1 = halves(b1, T());
-              mma8(d, f0, f2, f1, f3, __float_as_uint(v0.x), __float_as_uint(v0.y));
-              mma8(d, 0u, f6, 0u, f7, __float_as_uint(v1.x), __float_as_uint(v1.y));
+              const uint32_t x0 = __float_as_uint(v0.x), y0 = __float_as_uint(v0.y);
+              const uint32_t x1 = __float_as_uint(v1.x), y1 = __float_as_uint(v1.y);
+              mma8(d, f0.lo, f2.lo, f1.lo, f3.lo, x0, y0);
+              mma8(d, 0u, f6.lo, 0u, f7.lo, x1, y1);
+              mma8(d, f0.hi, f2.hi, f1.hi, f3.hi, x0, y0);
+              mma8(d, 0u, f6.hi, 0u, f7.hi, x1, y1);
             },
             zero, o, vb, len, g, t);
       }

@@ -43,11 +43,6 @@ __device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, ui
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t tf32(float x) {   // to nearest, 11 bits
-  uint32_t y;
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(y) : "f"(x));
-  return y;
-}
 // x = hi + lo, 11 bits each: products of three of the four parts keep fp32's 2^-21.  An infinity is
 // all in the lower part; of a B operand it is left out (fin) where it would meet the lower part of
 // A, which may be zero.

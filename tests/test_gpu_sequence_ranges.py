@@ -273,3 +273,31 @@ def test_linear_states_of_values_of_any_size(T, t, K, V, size):
     hold(out, o, to, "out")
     T.linear_attention(q, k, v, g, dev(off, "int64"), out, scale=args[5])
     hold(out, o, to, "out without states")
+
+
+# ---------------------------------------------------------------- operands of 16 bits: two parts
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("K,V", [(16, 16), (32, 32), (32, 48), (64, 64), (128, 40)])
+@pytest.mark.parametrize("states", [False, True])
+def test_linear_holds_its_state_and_weights_in_two_parts(T, t, rev, K, V, states):
+    """Outputs are off by their own rounding and by e^2 of what is added up, not by e of it."""
+    r = np.random.default_rng(27)
+    H = 2
+    lengths = [1, 15, 16, 17, 20, 33, 64, 900]
+    off = np.concatenate([[0], np.cumsum(lengths)])
+    n = int(off[-1])
+    q, k, v = slab(r, [(n, H, K), (n, H, K), (n, H, V)], t)
+    g = dev(-0.5 * r.random((n, H)))
+    s0 = dev(r.normal(size=(len(lengths), H, K, V))) if states else None
+    out = torch.empty_like(v, memory_format=torch.contiguous_format)
+    s1 = torch.empty_like(s0) if states else None
+    T.linear_attention(q, k, v, g, dev(off, "int64"), out, scale=0.2, reverse=rev, state_in=s0, state_out=s1)
+    args = host(q), host(k), host(v), host(g), off, 0.2, rev, None if s0 is None else host(s0)
+    o, s = Q.linear_attention(*args)
+    oa, _ = Q.linear_attention(*(np.abs(x) for x in args[:3]), args[3], off, 0.2, rev, None if s0 is None else np.abs(args[7]))
+    e, steps = half_step(t), 17 / 0.25 + 64
+    # (6 n + K + 16) u as in linear_tol, n the rows that count at a mean decay of 0.25; the state's parts
+    # and the weights' each leave e^2
+    hold(out, o, rounding(t, o) + ((6 * steps + K + 16) * U + 2 * e * e) * oa, "out")
