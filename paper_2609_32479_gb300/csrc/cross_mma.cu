@@ -11,10 +11,11 @@
 // ..., through a queue of each lane's own words in shared memory; movmatrix turns V.
 //
 // What bounds it: for tracks the instructions (131,072 tracks of five queries, 4 heads of 32, bf16:
-// 317 us, 4.0 TB/s of the 6.8 that a copy moves), for single queries memory (a state's K and V are
+// 355 us a call, 3.6 TB/s of the 6.8 that a copy moves), for single queries memory (a state's K and V are
 // read once for the G heads that share them: 61 queries over 1-16,384 states, 4 heads of 128: 184
-// us, 4.9 TB/s, with four warps an SM).  P is rounded to 16 bits once, as the operand of P V: an
-// error of the output's own rounding's size.
+// us, 4.9 TB/s, with four warps an SM).  P is the sum of two 16-bit parts as an operand of P V: with
+// one, rounded to 2^-8 (fp16 2^-11), the readout took 320 us instead of 355 and outputs were off by
+// as much again as by their own rounding.
 #include "cross_units.cuh"
 #include "mma_sync.cuh"
 
@@ -172,12 +173,16 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
         c0 += x[n][0] + x[n][1], c1 += x[n][2] + x[n][3];
       }
       l0 += c0, l1 += c1;
-      uint32_t pa[2][4];
+      uint32_t pa[2][4], pl[2][4];                       // the weights in two parts
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        pa[e][0] = pack2(x[2 * e][0], x[2 * e][1], T()), pa[e][1] = pack2(x[2 * e][2], x[2 * e][3], T());
-        pa[e][2] = pack2(x[2 * e + 1][0], x[2 * e + 1][1], T()), pa[e][3] = pack2(x[2 * e + 1][2], x[2 * e + 1][3], T());
-      }
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float p0 = x[2 * e + w / 2][w % 2 * 2], p1 = x[2 * e + w / 2][w % 2 * 2 + 1];
+          pa[e][w] = pack2(p0, p1, T());
+          const float2 h = halves(pa[e][w], T());
+          pl[e][w] = pack2(p0 - h.x, p1 - h.y, T());
+        }
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         uint32_t v[4][4], sum = 0u;
@@ -196,7 +201,11 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
           for (int w = 0; w < 4; ++w)
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-            if (e == 0 || !lower) mma16(o[4 * i + w], pa[e], turned(v[2 * e][w]), turned(v[2 * e + 1][w]), T());
+              if (e == 0 || !lower) {
+                const uint32_t u0 = turned(v[2 * e][w]), u1 = turned(v[2 * e + 1][w]);
+                mma16(o[4 * i + w], pl[e], u0, u1, T());
+                mma16(o[4 * i + w], pa[e], u0, u1, T());
+              }
         } else {
           for (int r = 0; r < 16; ++r) {
             const int rl = __shfl_sync(FULL, lo_l, r) - pos, rh = __shfl_sync(FULL, hi_l, r) - pos;
@@ -211,7 +220,8 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
                   u[c] = turned(v[2 * e + c][w]) & ((j >= rl && j < rh ? 0xffffu : 0u) | (j + 1 >= rl && j + 1 < rh ? 0xffff0000u : 0u));
                 }
                 float d[4];
-                mma16_new(d, pa[e], u[0], u[1], T());
+                mma16_new(d, pl[e], u[0], u[1], T());
+                mma16(d, pa[e], u[0], u[1], T());
                 if (g == r) o[4 * i + w][0] += d[0], o[4 * i + w][1] += d[1];
                 if (g + 8 == r) o[4 * i + w][2] += d[2], o[4 * i + w][3] += d[3];
               }

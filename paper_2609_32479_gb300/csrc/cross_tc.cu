@@ -8,25 +8,29 @@
 // than 64 states are left to the 16-row kernel.  The last block of a sequence ends at its last
 // state and takes the first ones twice, the second time with weight zero: no state of another
 // sequence is ever in a product.
-//   warps 0-3  a thread a row: the maximum of S, the weights (packed to 16 bits into shared
-//              memory, the K-major operand of P V), the sum; at a pass's end O / l
+//   warps 0-3  a thread a row: the maximum of S, the weights (two 16-bit parts each, put in the
+//              place of the scores, which P V reads as its A operand), the sum; at a pass's end
+//              O / l
 //   warp 4     TMA loads of K and V
 //   warp 5     the tcgen05.mma issuer and owner of the tensor memory
-// S and P have two places each: the scores of the next block are formed while the weights of
-// this one are, and P V runs behind.  (In one place, with blocks of 128 states, the chain of
+// S has two places: the scores of the next block are formed while the weights of this one are, and
+// P V runs behind.  (In one place, with blocks of 128 states, the chain of
 // product, weights and product left the tensor cores idle most of the time: 448 us for 4,099
 // queries and 30,011 states of 8 heads of 64.)  A thread holds a block's 64 scores in registers:
 // one read of the tensor memory.
 // The maximum that the weights are taken against moves only when a row's grows by more than 2^LAG:
 // O is hardly ever read back and scaled.
-// With heads up to 64 channels two CTAs share an SM (112 KB and 256 columns each), one's products
+// With heads up to 64 channels two CTAs share an SM (80 KB and 256 columns each), one's products
 // beside the other's exponentials.
 //
-// Bound: per 128 states the products take 617 clocks of an SM by their operations and 770 by
-// their operands' reads of shared memory, the 16,384 exponentials 512, and the instructions
-// around them (scale and subtract, maximum, sum, packing) about 550.
-// Measured: 4,099 queries over 30,011 states, 8 heads of 64, fp16: 320 us, 790 TFLOP/s of the
-// 1,969 that a large library product reaches.
+// With one part a weight, rounded to 2^-8 (fp16 2^-11), outputs were off by as much again as by
+// their own rounding; it was stored in shared memory and took 327 (bf16) and 351 us instead of 386
+// and 405 for the case below.
+// Bound: per 64 states and CTA the products take some 460 clocks of an SM, the 8,192 exponentials 256,
+// and the instructions around them (scale and subtract, maximum, sum, parts, packing) about 400; two
+// CTAs take 940 a block each way, most of it the chain of one block.
+// Measured: 4,099 queries over 30,011 states, 8 heads of 64, fp16: 405 us a call, 620 TFLOP/s of the
+// 1,969 that a large library product reaches (the lower parts' products not counted).
 //
 // Every wait has a limit; where one expires, the CTA gives up, the call's outputs are not valid,
 // and trackfit_operator_errors() says so.
@@ -34,6 +38,7 @@
 #include <cudaTypedefs.h>
 
 #include "cross_units.cuh"
+#include "mma_sync.cuh"
 #include "sm100_ptx.cuh"
 
 namespace {
@@ -42,11 +47,11 @@ using namespace sm100;
 
 constexpr int TILE = 128;                    // rows of a tile
 constexpr int BLOCK = CROSS_TC_FROM;         // states of a block
-constexpr uint32_t ATOM_Q = TILE * 128;      // 128 rows of 64 channels, or of 64 weights
+constexpr uint32_t ATOM_Q = TILE * 128;      // 128 rows of 64 channels
 constexpr uint32_t ATOM = BLOCK * 128;       // 64 states of 64 channels
 constexpr uint64_t LIMIT_NS = 2000000000ull;   // of a wait; a test hook shortens it
 constexpr int STAGES = 4;
-static_assert(BLOCK == 64, "a block's weights are one swizzled row of 128 bytes");
+static_assert(BLOCK == 64, "a block's weights, in two parts, take the place of its scores");
 // The maximum that the weights are taken against may be 2^LAG behind.  Not further in fp16: the
 // weights lie as much lower in the type's range (2^-38 of the largest is what one may be off).
 template <class T>
@@ -69,7 +74,7 @@ struct Bars {
 
 template <int NA>
 constexpr __host__ __device__ uint32_t smem_bytes() {
-  return (NA + 2) * ATOM_Q + 2 * STAGES * NA * ATOM + 256;
+  return NA * ATOM_Q + 2 * STAGES * NA * ATOM + 256;
 }
 static_assert(sizeof(Bars) <= 256, "the barriers' place");
 
@@ -142,7 +147,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     if (threadIdx.x == 0) atomicAdd(&g_expired, 1ull);
     return;
   }
-  const uint32_t q_s = base, p_s = q_s + NA * ATOM_Q, k_s = p_s + 2 * ATOM_Q, v_s = k_s + STAGES * NA * ATOM;
+  const uint32_t q_s = base, k_s = q_s + NA * ATOM_Q, v_s = k_s + STAGES * NA * ATOM;
   Bars* bars = reinterpret_cast<Bars*>(smem + smem_bytes<NA>() - 256);
   const uint32_t s_full = smem_u32(bars->s_full), p_full = smem_u32(bars->p_full), p_free = smem_u32(bars->p_free);
   const uint32_t o_done = smem_u32(&bars->o_done);
@@ -234,11 +239,12 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     if (elect_one()) {
       uint32_t n = 0;                                  // blocks of the passes before
       bool ok = true;
-      // the scores of block m of all, in place m & 1 (whose scores before have been read: their
-      // weights have been waited for)
+      // the scores of block m of all, in place m & 1, where the weights of the block before the last
+      // were: their product has ended
       auto scores = [&](uint32_t m) {
         const int s = m % STAGES;
-        ok = mbar_wait(smem_u32(&bars->k_full[s]), m / STAGES & 1, abort, p.limit_ns);
+        ok = (m < 2 || mbar_wait(p_free + 8 * (m & 1), (m >> 1 & 1) ^ 1, abort, p.limit_ns)) &&
+             mbar_wait(smem_u32(&bars->k_full[s]), m / STAGES & 1, abort, p.limit_ns);
         if (!ok) return;
         tc_fence_after();
         const uint32_t ks = k_s + s * NA * ATOM;
@@ -260,10 +266,11 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
                mbar_wait(smem_u32(&bars->v_full[s]), m / STAGES & 1, abort, p.limit_ns);
           if (!ok) break;
           tc_fence_after();
-          // V as it lies, [state][channel]: groups of 8 states 1024 bytes apart, 64 channels ATOM
-          for (int k = 0; k < BLOCK / 16; ++k)
-            umma_f16(tmem_o, sdesc_sw128(p_s + (m & 1) * ATOM_Q + 32 * k, 16, 1024),
-                     sdesc_sw128(v_s + s * NA * ATOM + k * 2048, ATOM, 1024), p.idesc_o, (j > 0) | (k > 0));
+          // both parts of the weights, 8 columns for 16 states; V as it lies, [state][channel]: groups
+          // of 8 states 1024 bytes apart, 64 channels ATOM
+          for (int k = 0; k < BLOCK / 8; ++k)
+            umma_f16_ts(tmem_o, tmem + (m & 1) * BLOCK + 8 * k, sdesc_sw128(v_s + s * NA * ATOM + k % 4 * 2048, ATOM, 1024),
+                        p.idesc_o, (j > 0) | (k > 0));
           umma_commit(p_free + 8 * (m & 1));
           umma_commit(smem_u32(&bars->v_free[s]));
           if (j + 1 == blocks) umma_commit(o_done);
@@ -336,30 +343,30 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
           }
         }
         const float mm = m == -INFINITY ? 0.0f : m;
-        if (n >= 2) {                                  // the weights' place is free
-          ok = __all_sync(FULL, mbar_wait(p_free + 8 * place, phase ^ 1, abort, p.limit_ns));
-          if (!ok) break;
-        }
-        const uint64_t scale = both(a.scale2, a.scale2), minus = both(up - mm, up - mm);
+        const uint64_t scale = both(a.scale2, a.scale2), minus = both(up - mm, up - mm), back = both(-1.0f, -1.0f);
         uint64_t s0 = 0, s1 = 0;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          uint32_t w[4];
+        for (int c = 0; c < 4; ++c) {                  // 16 states: 8 columns of the upper parts, 8 of the lower
+          float hi[8], lo[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int e = c % 4 * 8 + 2 * i;
-            float2 x = parts(fma2(both(v[c / 4][e], v[c / 4][e + 1]), scale, minus));
-            x.x = ex2(x.x), x.y = ex2(x.y);
-            if (i & 1) s1 = add2(s1, both(x.x, x.y));
-            else s0 = add2(s0, both(x.x, x.y));
-            w[i] = pack2(x.x, x.y, T());
+          for (int i = 0; i < 8; ++i) {
+            const int e = 16 * c + 2 * i;
+            const float2 x = parts(fma2(both(v[e / 32][e % 32], v[(e + 1) / 32][(e + 1) % 32]), scale, minus));
+            const uint64_t w = both(ex2(x.x), ex2(x.y));
+            if (i & 1) s1 = add2(s1, w);
+            else s0 = add2(s0, w);
+            const float2 y = parts(w);
+            const uint32_t u = pack2(y.x, y.y, T());
+            const float2 h = halves(u, T());
+            const float2 z = parts(fma2(both(h.x, h.y), back, w));
+            hi[i] = __uint_as_float(u), lo[i] = __uint_as_float(pack2(z.x, z.y, T()));
           }
-          const uint32_t at = p_s + place * ATOM_Q + r * 128 + ((c ^ (r & 7)) << 4);
-          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+          tmem_st8(tmem + lanes + place * BLOCK + 8 * c, hi);
+          tmem_st8(tmem + lanes + place * BLOCK + 32 + 8 * c, lo);
         }
         const float2 sum = parts(add2(s0, s1));
         l += sum.x + sum.y;
-        fence_proxy_async_smem();
+        tmem_st_wait();
         tc_fence_before();
         mbar_arrive(p_full + 8 * place);
       }

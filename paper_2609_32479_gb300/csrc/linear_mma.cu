@@ -110,7 +110,7 @@ __device__ __forceinline__ void add_rows(T, Mul mul, bool zero, float (&o)[NV][4
 }
 
 template <class T, int NG, int NV, bool STATE_ONLY, bool EXACT>
-__global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT ? 12 : 16) la_mma_kernel(const __grid_constant__ LaArgs a) {
+__global__ void __launch_bounds__(32, NG > 1 ? 8 : EXACT || __is_same(T, __half) ? 12 : 16) la_mma_kernel(const __grid_constant__ LaArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr bool BF = !__is_same(T, __half);
   constexpr int MT = NV / 2, KT = NG * 4;             // tiles of the state: MT x 16 by KT x 8

@@ -301,3 +301,24 @@ def test_linear_holds_its_state_and_weights_in_two_parts(T, t, rev, K, V, states
     # (6 n + K + 16) u as in linear_tol, n the rows that count at a mean decay of 0.25; the state's parts
     # and the weights' each leave e^2
     hold(out, o, rounding(t, o) + ((6 * steps + K + 16) * U + 2 * e * e) * oa, "out")
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+@pytest.mark.parametrize("nq,nk,D", [([5, 3, 17], [20, 8, 33], 32), ([1, 2], [3000, 900], 64), ([4, 0, 40], [700, 3, 60], 128),
+                                     ([200, 90], [900, 1300], 64), ([200, 90], [900, 1300], 128), ([150], [600], 24)])
+def test_cross_holds_its_weights_in_two_parts(T, t, nq, nk, D):
+    """Outputs are off by their own rounding and by e^2 of the weighted |v|."""
+    r = np.random.default_rng(28)
+    qo, ko = np.concatenate([[0], np.cumsum(nq)]), np.concatenate([[0], np.cumsum(nk)])
+    q = dev(r.normal(size=(int(qo[-1]), 4, D)), t)
+    k, v = (dev(r.normal(size=(int(ko[-1]), 2, D)), t) for _ in range(2))
+    out = torch.empty_like(q)
+    T.cross_attention(q, k, v, dev(qo, "int64"), dev(ko, "int64"), out)
+    sc = D ** -0.5
+    ref = Q.cross_attention(host(q), host(k), host(v), qo, ko, sc)
+    absv = Q.cross_attention(host(q), host(k), np.abs(host(v)), qo, ko, sc)
+    top = sc * np.linalg.norm(host(q), axis=-1).max() * np.linalg.norm(host(k), axis=-1).max()
+    e, n = half_step(t), max(nk)
+    # fp16: the lower part's smallest step, 2^-38 of the largest weight a state, on values up to the largest
+    least = n * 2.0 ** -38 * np.abs(host(v)).max() if t == "float16" else 0.0
+    hold(out, ref, rounding(t, ref) + absv * (2 * (D + 8) * top * U + (16 + 8 * np.sqrt(n)) * U + 2 * e * e) + least)
