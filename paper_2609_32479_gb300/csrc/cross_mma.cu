@@ -157,13 +157,8 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
       }
       t0 = fmaxf(m0, t0 * a.scale2), t1 = fmaxf(m1, t1 * a.scale2);
       const float n0 = t0 == -INFINITY ? 0.0f : t0, n1 = t1 == -INFINITY ? 0.0f : t1;
-      if (__any_sync(FULL, t0 != m0 || t1 != m1)) {
-        const float f0 = ex2(m0 - n0), f1 = ex2(m1 - n1);
-        l0 *= f0, l1 *= f1;
-#pragma unroll
-        for (int n = 0; n < NG * 4; ++n) o[n][0] *= f0, o[n][1] *= f0, o[n][2] *= f1, o[n][3] *= f1;
-        m0 = t0, m1 = t1;
-      }
+      const float f0 = ex2(m0 - n0), f1 = ex2(m1 - n1);
+      m0 = t0, m1 = t1;
       const float b0 = up - n0, b1 = up - n1;
       float c0 = 0.0f, c1 = 0.0f;
 #pragma unroll
@@ -172,7 +167,7 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
         x[n][2] = ex2(fmaf(x[n][2], a.scale2, b1)), x[n][3] = ex2(fmaf(x[n][3], a.scale2, b1));
         c0 += x[n][0] + x[n][1], c1 += x[n][2] + x[n][3];
       }
-      l0 += c0, l1 += c1;
+      l0 = fmaf(l0, f0, c0), l1 = fmaf(l1, f1, c1);
       uint32_t pa[2][4], pl[2][4];                       // the weights in two parts
 #pragma unroll
       for (int e = 0; e < 2; ++e)
@@ -196,17 +191,27 @@ __global__ void __launch_bounds__(32, NG == 1 ? 16 : 8) ca_mma_kernel(const __gr
             for (int w = 0; w < 4; ++w) sum = zero_if_finite(v[r][w], sum, T());
           mixed = __any_sync(FULL, (sum & 0x7fff7fffu) != 0u);
         }
+        // a chunk's own sum first, added to O outside the products: their accumulation cuts bits off, and
+        // over a long range would draw sums of one sign towards zero
         if (!mixed) {
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
+          for (int w = 0; w < 4; ++w) {
+            float sum[4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (e == 0 || !lower) {
-                const uint32_t u0 = turned(v[2 * e][w]), u1 = turned(v[2 * e + 1][w]);
-                mma16(o[4 * i + w], pl[e], u0, u1, T());
-                mma16(o[4 * i + w], pa[e], u0, u1, T());
-              }
+            for (int e = 0; e < 2; ++e) {
+              if (e == 1 && lower) continue;
+              const uint32_t u0 = turned(v[2 * e][w]), u1 = turned(v[2 * e + 1][w]);
+              if (e == 0) mma16_new(sum, pl[e], u0, u1, T());
+              else mma16(sum, pl[e], u0, u1, T());
+              mma16(sum, pa[e], u0, u1, T());
+            }
+            float(&on)[4] = o[4 * i + w];
+            on[0] = fmaf(on[0], f0, sum[0]), on[1] = fmaf(on[1], f0, sum[1]);
+            on[2] = fmaf(on[2], f1, sum[2]), on[3] = fmaf(on[3], f1, sum[3]);
+          }
         } else {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) o[4 * i + w][0] *= f0, o[4 * i + w][1] *= f0, o[4 * i + w][2] *= f1, o[4 * i + w][3] *= f1;
           for (int r = 0; r < 16; ++r) {
             const int rl = __shfl_sync(FULL, lo_l, r) - pos, rh = __shfl_sync(FULL, hi_l, r) - pos;
 #pragma unroll

@@ -24,12 +24,12 @@
 // beside the other's exponentials.
 //
 // With one part a weight, rounded to 2^-8 (fp16 2^-11), outputs were off by as much again as by
-// their own rounding; it was stored in shared memory and took 327 (bf16) and 351 us instead of 386
-// and 405 for the case below.
+// their own rounding; it was stored in shared memory and took 327 (bf16) and 351 us (fp16) instead of
+// 388 and 421 for the case below.
 // Bound: per 64 states and CTA the products take some 460 clocks of an SM, the 8,192 exponentials 256,
 // and the instructions around them (scale and subtract, maximum, sum, parts, packing) about 400; two
 // CTAs take 940 a block each way, most of it the chain of one block.
-// Measured: 4,099 queries over 30,011 states, 8 heads of 64, fp16: 405 us a call, 620 TFLOP/s of the
+// Measured: 4,099 queries over 30,011 states, 8 heads of 64, fp16: 421 us a call, 600 TFLOP/s of the
 // 1,969 that a large library product reaches (the lower parts' products not counted).
 //
 // Every wait has a limit; where one expires, the CTA gives up, the call's outputs are not valid,
@@ -57,6 +57,12 @@ static_assert(BLOCK == 64, "a block's weights, in two parts, take the place of i
 template <class T>
 constexpr float LAG = __is_same(T, __half) ? 2.0f : 8.0f;
 
+// Blocks whose products are added up in O before the row's thread puts it aside: the accumulation
+// cuts bits off, up to 2^-23 of O a step of 16 states, which draws sums of one sign towards zero
+// (32 blocks: 1.4e-5, a 35th of an fp16 output's rounding, whatever the range; in one sum it would
+// be that rounding for a range of 100,000 states).
+constexpr int ASIDE = 32;
+
 struct TcArgs {
   CaArgs a;
   int tiles;
@@ -75,6 +81,11 @@ struct Bars {
 template <int NA>
 constexpr __host__ __device__ uint32_t smem_bytes() {
   return NA * ATOM_Q + 2 * STAGES * NA * ATOM + 256;
+}
+// Of tensor memory: two places of S, O and what of it is put aside.
+template <int NA>
+constexpr __host__ __device__ uint32_t columns() {
+  return NA == 1 ? 256 : 512;
 }
 static_assert(sizeof(Bars) <= 256, "the barriers' place");
 
@@ -169,7 +180,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     fence_mbar_init();
   }
   if (warp == 5) {
-    tmem_alloc(smem_u32(&bars->tmem), 256);
+    tmem_alloc(smem_u32(&bars->tmem), columns<NA>());
     tmem_relinquish();
   }
   // the tile's queries: rows of 128 bytes, 16-byte pieces swizzled as the K-major operand wants
@@ -187,7 +198,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = bars->tmem, tmem_o = tmem + 2 * BLOCK;   // after the two places of S
+  const uint32_t tmem = bars->tmem, tmem_o = tmem + 2 * BLOCK, tmem_aside = tmem_o + 64 * NA;
   volatile int* abort = &bars->abort_flag;
   Passes passes(a, row0, split, lane);
   Pass ps;
@@ -270,7 +281,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
           // of 8 states 1024 bytes apart, 64 channels ATOM
           for (int k = 0; k < BLOCK / 8; ++k)
             umma_f16_ts(tmem_o, tmem + (m & 1) * BLOCK + 8 * k, sdesc_sw128(v_s + s * NA * ATOM + k % 4 * 2048, ATOM, 1024),
-                        p.idesc_o, (j > 0) | (k > 0));
+                        p.idesc_o, ((j % ASIDE) > 0) | (k > 0));
           umma_commit(p_free + 8 * (m & 1));
           umma_commit(smem_u32(&bars->v_free[s]));
           if (j + 1 == blocks) umma_commit(o_done);
@@ -292,6 +303,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
     bool ok = true;
     while (ok && passes.next(ps)) {
       float m = -INFINITY, l = 0.0f;                   // m: score * scale2 that the weights are taken against
+      float m_aside = -INFINITY;                       // .. that those of what is put aside were
       const float up = weight_up<T>(ps.len) - LAG<T>;
       for (int j = ps.j0; j < ps.j1; ++j, ++n) {
         const uint32_t place = n & 1, phase = n >> 1 & 1;
@@ -318,28 +330,40 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
         }
         t0 = max3(t0, v[1][28], v[1][29]), t1 = max3(t1, v[1][30], v[1][31]);
         const float top = fmaxf(max3(t0, t1, t2), t3) * a.scale2;
-        if (j == ps.j0) {
-          m = top;
-        } else {
-          if (__any_sync(FULL, top > m + LAG<T>)) {
-            // the product before this block adds to O until then
-            ok = __all_sync(FULL, mbar_wait(p_free + 8 * (place ^ 1), (n - 1) >> 1 & 1, abort, p.limit_ns));
-            if (!ok) break;
-            tc_fence_after();
-            const bool move = top > m;                 // (with one row of the warp all that have grown)
-            const float f = move ? ex2(m - top) : 1.0f;
-            if (move) m = top;
-            l *= f;
+        const bool aside = j > ps.j0 && (j - ps.j0) % ASIDE == 0;
+        const bool moves = j > ps.j0 && __any_sync(FULL, top > m + LAG<T>);
+        if (j == ps.j0) m = top;
+        if (aside || moves) {
+          // the product before this block adds to O until then
+          ok = __all_sync(FULL, mbar_wait(p_free + 8 * (place ^ 1), (n - 1) >> 1 & 1, abort, p.limit_ns));
+          if (!ok) break;
+          tc_fence_after();
+          // put aside as it is, or scaled to the new maximum (with one row of the warp all that have grown)
+          const float f = aside ? m_aside == -INFINITY ? 0.0f : ex2(m_aside - m) : top > m ? ex2(m - top) : 1.0f;
+          const bool first = j - ps.j0 == ASIDE;
+          const uint32_t to = lanes + (aside ? tmem_aside : tmem_o);
 #pragma unroll 1
-            for (int c = 0; c < NA * 2; ++c) {
-              float o[32];
-              tmem_ld32(tmem_o + lanes + 32 * c, o);
+          for (int c = 0; c < NA * 4; ++c) {
+            float o[16];
+            tmem_ld16(to + 16 * c, o);
+            if (aside) {
+              float x[16];
+              tmem_ld16(tmem_o + lanes + 16 * c, x);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] *= f;
-              tmem_st32(tmem_o + lanes + 32 * c, o);
+              for (int i = 0; i < 16; ++i) o[i] = first ? x[i] : fmaf(o[i], f, x[i]);
+            } else {
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] *= f;
             }
-            tmem_st_wait();
+            tmem_st16(to + 16 * c, o);
+          }
+          tmem_st_wait();
+          if (aside) m_aside = m;
+          if (moves && top > m) {
+            l *= ex2(m - top);
+            m = top;
           }
         }
         const float mm = m == -INFINITY ? 0.0f : m;
@@ -380,6 +404,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
       const int64_t at = ((int64_t)split * rows + row) * a.Hk + hk;
       const float f = a.splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
       if (a.splits > 1 && mine) a.ws_ml[at] = make_float2(m, l);
+      const float f_aside = m_aside == -INFINITY ? 0.0f : ex2(m_aside - m);
       T* out = mine ? (T*)a.out + (int64_t)(row / a.G) * a.os + (hk * a.G + row % a.G) * a.D : nullptr;
       float* part = mine ? a.ws_o + at * a.D : nullptr;
 #pragma unroll 1
@@ -389,6 +414,13 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
         if (any) {
           tmem_ld32(tmem_o + lanes + 32 * c, v);
           tmem_ld_wait();
+          if (ps.j1 - ps.j0 > ASIDE) {
+            float x[32];
+            tmem_ld32(tmem_aside + lanes + 32 * c, x);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = fmaf(x[i], f_aside, v[i]);
+          }
         } else {
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = 0.0f;
@@ -412,7 +444,7 @@ __global__ void __launch_bounds__(192, NA == 1 ? 2 : 1)
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 5) tmem_dealloc(tmem, 256);
+  if (warp == 5) tmem_dealloc(tmem, columns<NA>());
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {

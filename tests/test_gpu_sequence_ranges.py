@@ -322,3 +322,19 @@ def test_cross_holds_its_weights_in_two_parts(T, t, nq, nk, D):
     # fp16: the lower part's smallest step, 2^-38 of the largest weight a state, on values up to the largest
     least = n * 2.0 ** -38 * np.abs(host(v)).max() if t == "float16" else 0.0
     hold(out, ref, rounding(t, ref) + absv * (2 * (D + 8) * top * U + (16 + 8 * np.sqrt(n)) * U + 2 * e * e) + least)
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+@pytest.mark.parametrize("nq,nk", [(16, 30000), (100, 120000), (2100, 30000), (20000, 30000)])
+def test_cross_16_bits_of_values_of_one_sign(T, t, nq, nk):
+    """No output is further off than its rounding and its weights'.  The mean of all is that of the
+    definition rounded alike (outputs near one gather at few values, so that the rounding by itself
+    has a mean): an output that rounds the other way is 2 e off, to either side, and six deviations
+    of as many as there are hold it.  What the products cut off does not grow with the states: 256
+    steps at most, up to 2^-23 each of a sum that grows as they go."""
+    out, ref, top = one_sign(T, t, nq, nk, 64, 25)
+    e = half_step(t)
+    hold(out, ref, ref * (2 * e + 2 * 72 * top * U + (16 + 8 * np.sqrt(nk / 16)) * U))
+    near = torch.from_numpy(ref).to(getattr(torch, t)).double().numpy()
+    off = np.mean(out / near - 1)
+    assert abs(off) < 12 * e * np.sqrt(np.mean(out != near) / out.size) + 256 * U, off
