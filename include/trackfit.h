@@ -398,7 +398,10 @@ int trackfit_forward_noalloc(const trackfit_config_t* cfg, const float* weights,
  * minGRU; none of these operators is tied to a model.
  *   dtype    type of the row arrays: TRACKFIT_FP32, TRACKFIT_BF16_PROJ (bf16) or
  *            TRACKFIT_FP16_PROJ (fp16).  Sums, softmax statistics, norms and states
- *            are fp32 whatever the type.
+ *            are fp32 whatever the type.  As operands of a matrix product they are two
+ *            parts: beside its own rounding and those of fp32 sums an output is off by
+ *            2^-15 (bf16) or 2^-21 (fp16; fp32 in attention) of the absolute values that
+ *            are added up.
  *   strides  elements from a row to the next; heads stand side by side within a row,
  *            so q, k and v may be column blocks of one projection.
  * Row arrays are device memory, 16-byte aligned, rows too (stride x element size a
@@ -418,14 +421,14 @@ int trackfit_forward_noalloc(const trackfit_config_t* cfg, const float* weights,
  * work than 32 bits count), CUDA.  Make the first call of a kind outside of a capture. */
 
 /* Norms of queries and keys for each head, with the position rotation in the same pass.
- *   y = x / sqrt(mean(x^2) + eps) * gain over a head's channels, then, for
- *   i < rot_dim / 2, (y_i, y_{i + rot_dim/2}) turned by the angle
- *   positions[row] * rot_base^(-2 i / rot_dim).
+ *   y = x / sqrt(mean(x^2) + eps) * gain over a head's channels (zeros where the sum of
+ *   squares leaves fp32's range), then, for i < rot_dim / 2, (y_i, y_{i + rot_dim/2})
+ *   turned by the angle positions[row] * rot_base^(-2 i / rot_dim).
  *   q, q_out   [n_rows][q_heads][head_dim]; q_out may be q itself (same stride).
  *   k, k_out   [n_rows][k_heads][head_dim], likewise; NULL with k_heads = 0.
  *   q_gain, k_gain  device fp32 [head_dim], or NULL (ones).
- *   positions  device int32 [n_rows], any values (angles keep 2^-32 of a turn however far
- *              the position); may be NULL with rot_dim = 0.
+ *   positions  device int32 [n_rows], any values (an angle is off by at most 2^-25 of a turn
+ *              and 2^-51 of the turns that the position makes); may be NULL with rot_dim = 0.
  *   rot_dim    a multiple of 16 in [0, head_dim]; the channels from rot_dim on are
  *              normalised only.  rot_base >= 1, eps > 0. */
 int trackfit_qk_norm(int32_t dtype, const void* q, int64_t q_stride, int32_t q_heads, const void* k,
@@ -476,6 +479,7 @@ int trackfit_linear_attention_step(int32_t dtype, const void* q, int64_t q_strid
  *   q, out      [n_q_rows][q_heads][head_dim], sequences by q_offsets.
  *   k, v        [n_kv_rows][kv_heads][head_dim], sequences by kv_offsets; head h of the
  *               queries reads head h / (q_heads / kv_heads).
+ * fp16: a weight is off by no more than 2^-38 of its row's largest, however small it is.
  * A query whose sequence has no states gets zeros.  Waits inside the kernels are limited
  * (2 s): see trackfit_operator_errors.
  *   workspace   trackfit_cross_attention_workspace() bytes, 16-byte aligned (few queries:

@@ -10,9 +10,11 @@
 // sum over G lanes and a pair's other half is r/2 channels, hence whole lanes, away.
 //
 // The angle in turns is a product modulo 1: position times the frequency as a 64-bit
-// fixed-point fraction of a turn, whose low 64 bits are exactly the fraction, however far
-// the position.  Every angle of a row is formed by one lane and shared through shared
-// memory: all heads of a row turn alike.
+// fixed-point fraction of a turn, whose low 64 bits are exactly the fraction, however far the
+// position.  What is lost: the frequency comes from fp64 operations, 2^-51 of it at most (at
+// position 2^31 2^-22 of a turn), and the fraction's 32 upper bits are rounded to fp32, 2^-26 of a
+// turn.  Every angle of a row is formed by one lane and shared through shared memory: all heads of a
+// row turn alike.
 //
 // Measured: 1,310,003 rows of 4 + 4 heads of 32, bf16: 261 us, 5.2 TB/s of the 6.8 that a copy
 // moves; 404 with two rows' loads under way instead of four and the frequencies read from the
