@@ -48,12 +48,20 @@ __global__ void __launch_bounds__(NW * 32) ca_join_kernel(const __grid_constant_
     if (lane + 32 * c < a.D) put(out + lane + 32 * c, average(o[c], inv));
 }
 
-// Whether the 128-row kernel runs: 16-bit types, sequences of at least 64 rows and 512 states on
-// average.  Measured at 8 heads of 64, fp16, it against the 16-row kernel: 64 sequences of 64 rows
-// and 512 states 31 and 37 us, of 64 and 2,048 67 and 112, of 32 and 2,048 80 and 56; 256 of 100
-// and 512 168 and 200, of 100 and 300 142 and 139; one of 4,099 and 30,011 327 and 1568.
-bool wide_tiles(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int G) {
-  return dtype != TRACKFIT_FP32 && nq * G >= 64 * n_seq && nk >= 512 * n_seq;
+// Whether the 128-row kernel runs: 16-bit types, sequences of at least 512 states and 64 rows of the
+// products (queries by shared heads) on average, 128 where the 16-row kernel's heads are narrowest.
+// Measured, the 16-row kernel against it, us (heads on heads of the states x width; sequences of
+// rows and states):
+//   8 on 8 x 64    64 of 64, 256: 26, 30 fp16 and 26, 27 bf16; 64 of 64, 512: 40, 39 and 40, 34; 64 of
+//                  32, 2,048: 65, 108 and 65, 88; 64 of 64, 2,048: 125, 89 and 125, 74
+//   4 on 4 x 128   64 of 64, 256: 28, 32 and 28, 28; 64 of 64, 512: 44, 42 and 44, 34; 64 of 32, 2,048:
+//                  86, 110 and 85, 85; 256 of 100, 300: 158, 187 and 157, 160; of 100, 512: 236, 234
+//                  and 235, 186
+//   16 on 4 x 128  64 of 64, 512: 44, 42 fp16;  8 on 2 x 64  64 of 64, 512: 24, 32; of 64, 2,048: 55, 49
+//   4 on 4 x 32    64 of 64, 512: 19, 32 and 19, 26; 64 of 64, 2,048: 55, 64 and 55, 55; 64 of 128, 512:
+//                  26, 26 and 26, 24; 64 of 128, 2,048: 78, 51 and 79, 44
+bool wide_tiles(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int G, int D) {
+  return dtype != TRACKFIT_FP32 && nq * G >= (D <= 32 ? 128 : 64) * n_seq && nk >= 512 * n_seq;
 }
 // How a call is cut.  Parts of each row's range: as many as give every warp of the GPU something
 // to do (152 x 12 of the 16-row kernels, 152 x 2 CTAs of the 128-row one, 152 for wide heads), not
@@ -69,7 +77,7 @@ Cut cut_of(int32_t dtype, int64_t nq, int64_t nk, int64_t n_seq, int Hq, int Hk,
   Cut c = {false, 1, 16};
   if (nq <= 0 || n_seq <= 0) return c;
   const int64_t G = Hq / Hk, rows = nq * G;
-  c.wide = wide_tiles(dtype, nq, nk, n_seq, (int)G);
+  c.wide = wide_tiles(dtype, nq, nk, n_seq, (int)G, D);
   const int64_t target = c.wide ? (D <= 64 ? 304 : 152) : 152 * 12, most = nk / n_seq / (c.wide ? 512 : 256);
   for (;; c.tr /= 2) {
     const int64_t units = (c.wide ? (rows + 127) / 128 : (rows + c.tr - 1) / c.tr) * Hk;

@@ -307,9 +307,10 @@ int rows_a_boundary(int64_t n_rows, int H, int V) {
 }
 constexpr int LONGEST = 512;   // longer sequences are cut
 
-// Whether any may be: not where there are few rows of sequences that are short on average.  The
-// two launches would cost a small call more than a warp's time for the longest sequence that
-// could be among them, 16,384 rows, is likely to (an event of 211 tracks: 13 us instead of 6).
+// Whether any may be: not where there are few rows of sequences that are short on average, for which
+// the two launches are the longer part of a call (an event of 211 tracks: 13 us instead of 6 on the
+// device).  What that costs where a long one is among them: 250 tracks of 14 rows and a sequence of
+// 12,000, 4 heads of 32, take 722 us uncut (fp32 2,268); with 200 tracks, cut, 55 (129).
 bool cuts(int64_t n_rows, int64_t n_seq) { return n_rows > LONGEST && (n_rows > 16384 || n_rows > 64 * n_seq); }
 
 size_t workspace_bytes(int64_t n_rows, int64_t n_seq, int H, int K, int V) {
