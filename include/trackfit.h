@@ -441,8 +441,7 @@ int trackfit_qk_norm(int32_t dtype, const void* q, int64_t q_stride, int32_t q_h
  * with S of key_dim x value_dim: the gated recurrence of Eq. 2 with a matrix for a state.
  *   q, k        [n_rows][n_heads][key_dim]; v, out [n_rows][n_heads][value_dim].
  *   log_decay   device fp32 [n_rows][decay_stride], the first n_heads of a row used: g,
- *               at most 0 (fp16 rows scaled up by a larger one may leave their range);
- *               -inf forgets all that was before.
+ *               at most 0; -inf forgets all that was before.
  *   reverse     0: from a sequence's first row to its last; 1: from its last to its first.
  *   state_in    fp32 [n_seq][n_heads][key_dim][value_dim] to begin with, or NULL (zeros).
  *   state_out   the same shape, the state after each sequence, or NULL; may be state_in.
@@ -480,6 +479,8 @@ int trackfit_linear_attention_step(int32_t dtype, const void* q, int64_t q_strid
  *   k, v        [n_kv_rows][kv_heads][head_dim], sequences by kv_offsets; head h of the
  *               queries reads head h / (q_heads / kv_heads).
  * fp16: a weight is off by no more than 2^-38 of its row's largest, however small it is.
+ * fp32, bf16: averages of values up to the type's largest are finite; values below 2^-126
+ * times the number of states may lose bits.
  * A query whose sequence has no states gets zeros.  Waits inside the kernels are limited
  * (2 s): see trackfit_operator_errors.
  *   workspace   trackfit_cross_attention_workspace() bytes, 16-byte aligned (few queries:

@@ -133,7 +133,7 @@ extern "C" int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_
   const Cut cut = cut_of(dtype, n_q_rows, n_kv_rows, n_seq, q_heads, kv_heads, head_dim);
   a.splits = cut.splits, a.tr = cut.tr;
   // all heads of a tile by one warp where that leaves ten tiles for each of the 152 x 16 warps
-  // (131,072 tracks of five queries: 319 us, with a warp a head 451)
+  // (131,072 tracks of five queries, with one part a weight: 319 us, with a warp a head 451)
   a.each = (n_q_rows * a.G + 15) / 16 >= 10 * 152 * 16 ? kv_heads : 1;
   a.ws_o = static_cast<float*>(workspace);
   a.ws_ml = reinterpret_cast<float2*>(a.ws_o + (need > 0 ? (int64_t)a.splits * n_q_rows * q_heads * head_dim : 0));

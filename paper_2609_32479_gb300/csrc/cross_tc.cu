@@ -26,9 +26,10 @@
 // With one part a weight, rounded to 2^-8 (fp16 2^-11), outputs were off by as much again as by
 // their own rounding; it was stored in shared memory and took 327 (bf16) and 351 us (fp16) instead of
 // 388 and 421 for the case below.
-// Bound: per 64 states and CTA the products take some 460 clocks of an SM, the 8,192 exponentials 256,
-// and the instructions around them (scale and subtract, maximum, sum, parts, packing) about 400; two
-// CTAs take 940 a block each way, most of it the chain of one block.
+// Bound: a block takes an SM 985 clocks, of which its twelve products of 128 x 64 x 16 (four for the
+// scores, eight for both parts of the weights) need 384, its 8,192 exponentials 256, and the 504
+// instructions of each of its four warps as many of a scheduler; the rest is the chain of a block,
+// which two CTAs an SM do not hide.
 // Measured: 4,099 queries over 30,011 states, 8 heads of 64, fp16: 421 us a call, 600 TFLOP/s of the
 // 1,969 that a large library product reaches (the lower parts' products not counted).
 //
