@@ -338,3 +338,76 @@ def test_cross_16_bits_of_values_of_one_sign(T, t, nq, nk):
     near = torch.from_numpy(ref).to(getattr(torch, t)).double().numpy()
     off = np.mean(out / near - 1)
     assert abs(off) < 12 * e * np.sqrt(np.mean(out != near) / out.size) + 256 * U, off
+
+
+# ---------------------------------------------------------------- attention: what is put aside
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+@pytest.mark.parametrize("D", [40, 64, 128])
+@pytest.mark.parametrize("growth", [-6.0, 3.0, 14.0])
+def test_cross_of_scores_that_grow_over_a_long_range(T, t, D, growth):
+    """Many heads, so that a range is one part: O is put aside several times, and the maximum that the
+    weights are taken against moves in between, or never again."""
+    r = np.random.default_rng(31)
+    H, nq, nk = 80, 500, [7000, 0, 130, 2048, 2049]
+    ko, qo = np.concatenate([[0], np.cumsum(nk)]), np.array([0, 300, 310, 350, 430, nq])
+    q, k = dev(0.3 * r.normal(size=(nq, H, D)), t), dev(0.3 * r.normal(size=(ko[-1], H, D)), t)
+    v = dev(r.normal(size=(ko[-1], H, D)), t)
+    q[..., 0] = 1.0
+    for a, n in zip(ko, nk):
+        k[a:a + n, :, 0] = torch.linspace(0, growth, max(n, 1), device="cuda")[:n, None].to(k.dtype)
+    out = torch.full_like(q, float("nan"))
+    T.cross_attention(q, k, v, dev(qo, "int64"), dev(ko, "int64"), out, scale=1.0)
+    e = half_step(t)
+    for b, n in enumerate(nk):
+        rows, at = slice(qo[b], qo[b + 1]), slice(ko[b], ko[b + 1])
+        if n == 0:
+            assert bool((out[rows] == 0).all())
+            continue
+        x = torch.softmax(torch.einsum("qhd,khd->hqk", q[rows].double(), k[at].double()), -1)
+        ref = torch.einsum("hqk,khd->qhd", x, v[at].double()).cpu().numpy()
+        absv = torch.einsum("hqk,khd->qhd", x, v[at].double().abs()).cpu().numpy()
+        top = float(q[rows].double().norm(dim=-1).max() * k[at].double().norm(dim=-1).max())
+        # 256 steps of a product's accumulation, up to 2^-23 each of a sum that grows
+        tol = rounding(t, ref) + absv * (2 * (D + 8) * top * U + (256 + 8 * np.sqrt(n)) * U + 2 * e * e)
+        hold(out[rows], ref, tol + (n * 2.0 ** -38 * 6 if t == "float16" else 0.0), f"sequence {b}")
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+def test_cross_of_long_ranges_keeps_what_is_not_finite_to_its_sequence(T, t):
+    r = np.random.default_rng(32)
+    H, D, nq, nk = 160, 64, [100, 90, 66], [2500, 3000, 2600]
+    qo, ko = np.concatenate([[0], np.cumsum(nq)]), np.concatenate([[0], np.cumsum(nk)])
+    q, k, v = (dev(r.normal(size=(m, H, D)), t) for m in (qo[-1], ko[-1], ko[-1]))
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    T.cross_attention(q, k, v, dev(qo, "int64"), dev(ko, "int64"), want)
+    k[2600, 0, 3] = float("nan")
+    v[2700, 1, 3] = float("inf")
+    v[5400, 2, 5] = float("nan")
+    T.cross_attention(q, k, v, dev(qo, "int64"), dev(ko, "int64"), out)
+    same = (out == want).cpu()
+    assert same[:100].all() and same[190:].all() and same[100:190, 3:].all()
+    ok = torch.isfinite(out[100:190]).cpu()
+    assert not ok[:, 0].any() and not ok[:, 1, 3].any() and not ok[:, 2, 5].any()
+    assert ok[:, 1, :3].all() and ok[:, 1, 4:].all() and ok[:, 2, :5].all() and ok[:, 2, 6:].all()
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+def test_cross_of_two_widths_at_once(T, t):
+    """Kernels that take different parts of tensor memory, on two streams, one call after the other."""
+    r = np.random.default_rng(33)
+    calls = []
+    for D, H in ((64, 24), (128, 12), (128, 24), (40, 12)):
+        q, k, v = (dev(r.normal(size=(m, H, D)), t) for m in (900, 4000, 4000))
+        off, ko, out = dev([0, 500, 900], "int64"), dev([0, 2500, 4000], "int64"), torch.empty_like(q)
+        T.cross_attention(q, k, v, off, ko, out)
+        calls.append((q, k, v, off, ko, out, out.clone()))
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for s, (q, k, v, off, ko, out, _) in zip(streams, calls):
+            T.cross_attention(q, k, v, off, ko, out, stream=s)
+    torch.cuda.synchronize()
+    assert T.operator_errors() == T.OK
+    for *_, out, want in calls:
+        assert torch.equal(out, want)
