@@ -5,7 +5,7 @@
 // of operands the three largest are taken (m16n8k8): what is left out is 2^-22 of a product, of
 // the order of fp32's own rounding.  Three products of half the rate each leave 100 TFLOP/s of
 // mma.sync's 604, against the 75 of the CUDA cores, whose operands would come from shared
-// memory value by value.  Measured: 2,000 queries over 16,000 states, 4 heads of 64: 1590 us, 21
+// memory value by value.  Measured: 2,000 queries over 16,000 states, 4 heads of 64: 1603 us, 20
 // TFLOP/s; the instructions that form the parts bound it, each warp for its own 16 rows.
 //
 // Lane (g, t) reads 16 bytes, channels 4t .. 4t+3 of each 16, of rows g and g + 8: with the k
@@ -134,13 +134,22 @@ __global__ void __launch_bounds__(32, NG <= 4 ? 12 : 8) ca_tf32_kernel(const __g
       uint32_t k[2][4];
       load_shared(k[0], mine + s * SLOT + (2 * i) * 512);
       load_shared(k[1], mine + s * SLOT + (2 * i + 1) * 512);
+      float d[2][4];                                   // these channels' sum, added outside the products
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) d[n][c] = 0.0f;
 #pragma unroll
       for (int w = 0; w < 4; w += 2) {
         const uint32_t ah[4] = {h0[w], h1[w], h0[w + 1], h1[w + 1]}, al[4] = {g0[w], g1[w], g0[w + 1], g1[w + 1]};
 #pragma unroll
         for (int n = 0; n < 2; ++n)
-          mma8_parts(x[n], ah, al, tf32_bparts(__uint_as_float(k[n][w])), tf32_bparts(__uint_as_float(k[n][w + 1])));
+          mma8_parts(d[n], ah, al, tf32_bparts(__uint_as_float(k[n][w])), tf32_bparts(__uint_as_float(k[n][w + 1])));
       }
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[n][c] += d[n][c];
     }
     // states that are not a row's own count nothing
     const bool whole = __all_sync(FULL, lo0 <= pos && pos + KC <= hi0 && lo1 <= pos && pos + KC <= hi1);

@@ -411,3 +411,20 @@ def test_cross_of_two_widths_at_once(T, t):
     assert T.operator_errors() == T.OK
     for *_, out, want in calls:
         assert torch.equal(out, want)
+
+
+# ---------------------------------------------------------------- fp32: errors that no sum lessens
+
+@pytest.mark.parametrize("D", [16, 64, 96, 128])
+@pytest.mark.parametrize("nq,nk", [(40, 350), (1, 900), (300, 40)])
+def test_cross_fp32_is_as_near_as_fp32_products(T, D, nq, nk):
+    """Scores of a few, each a sum of groups of 16 channels that are off by 2^-22 of their size: weights
+    are off by a few u, and 12 u holds their average."""
+    r = np.random.default_rng(35)
+    H = 3
+    q, k, v = (dev(r.normal(size=(m, H, D))) for m in (nq, nk, nk))
+    q = 1.5 * q
+    out = torch.empty_like(q)
+    T.cross_attention(q, k, v, dev([0, nq], "int64"), dev([0, nk], "int64"), out)
+    ref = Q.cross_attention(host(q), host(k), host(v), [0, nq], [0, nk], D ** -0.5)
+    assert np.linalg.norm(host(out) - ref) < 12 * U * np.linalg.norm(ref)
