@@ -17,9 +17,11 @@ using namespace seqops;
 // memory as broadcasts, 8 rows at a time through a ring that the warp fills by asynchronous
 // copies.  Several columns a lane share what a row costs whatever its columns (loads,
 // exponentials, addresses: 90 of 116 instructions with one).  Measured: 20,011 tracks and parts
-// of tracks, 4 heads of 32 x 48, states in and out: 747 us a call, 3.5 TB/s; one column a lane 1136.
+// of tracks, 4 heads of 32 x 48, states in and out: 773 us a call, 3.4 TB/s; one column a lane 1136.
 // Every row decays the state itself: a factor kept beside it, which would save the product, makes
-// values up to that factor larger than the state.
+// values up to that factor larger than the state.  A small decay goes in as S + (e^g - 1) S: e^g
+// rounded would be an error that all values of the state have in common, 2^-25 a row, which no sum
+// over them lessens (over 1,000 rows 2e-6 of the output, ten times what is left).
 constexpr int CH = 8, NST = 2;
 
 template <int DK, int CPL>
@@ -153,26 +155,38 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
           S[j][i / 2] = st && i0 + i < a.K ? both(src[i * COLS + 16 * j], src[(i + 1) * COLS + 16 * j]) : 0;
       if (STATE_ONLY && a.ws_begin && !(flags & GOES_ON)) put_state(a.ws_begin + ((tile + 1) * a.H + h) * KV);
     }
-    float sum = 0.0f;
+    // the rows' decays, a lane each: e^g - 1 of a small one, which is not positive, else e^g, which is
+    // (-1 where it is zero)
+    if (lane < len) {
+      const float x = w.g[lane];
+      float e = x > -0.5f && x <= 0.0f ? expm1f(x) : expf(x);
+      if (e == 0.0f && x < 0.0f) e = x > -0.5f ? e : -1.0f;
+      if (STATE_ONLY) total += x;
+      w.g[lane] = e;
+    }
+    __syncwarp();
     for (int r = 0; r < len; ++r) {
-      const float e = expf(w.g[r]);
-      if (STATE_ONLY) sum += w.g[r];
-      const uint64_t decay = both(e, e);
+      const float e = w.g[r];
+      const uint64_t e2 = both(e, e);
       uint64_t x[CPL], acc[CPL];
 #pragma unroll
       for (int j = 0; j < CPL; ++j) x[j] = both(w.v[r][col + 16 * j], w.v[r][col + 16 * j]), acc[j] = 0;
+      auto step = [&](auto decayed) {
 #pragma unroll
-      for (int i = 0; i < HALF; i += 4) {
-        const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(&w.k[r][i0 + i]);
-        ulonglong2 q4;
-        if (!STATE_ONLY) q4 = *reinterpret_cast<const ulonglong2*>(&w.q[r][i0 + i]);
+        for (int i = 0; i < HALF; i += 4) {
+          const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(&w.k[r][i0 + i]);
+          ulonglong2 q4;
+          if (!STATE_ONLY) q4 = *reinterpret_cast<const ulonglong2*>(&w.q[r][i0 + i]);
 #pragma unroll
-        for (int j = 0; j < CPL; ++j) {
-          uint64_t(&s)[2] = *reinterpret_cast<uint64_t(*)[2]>(&S[j][i / 2]);
-          s[0] = fma2(k4.x, x[j], mul2(s[0], decay)), s[1] = fma2(k4.y, x[j], mul2(s[1], decay));
-          if (!STATE_ONLY) acc[j] = fma2(q4.y, s[1], fma2(q4.x, s[0], acc[j]));
+          for (int j = 0; j < CPL; ++j) {
+            uint64_t &s0 = S[j][i / 2], &s1 = S[j][i / 2 + 1];
+            s0 = fma2(k4.x, x[j], decayed(s0)), s1 = fma2(k4.y, x[j], decayed(s1));
+            if (!STATE_ONLY) acc[j] = fma2(q4.y, s1, fma2(q4.x, s0, acc[j]));
+          }
         }
-      }
+      };
+      if (e <= 0.0f) step([e2](uint64_t s) { return fma2(s, e2, s); });
+      else step([e2](uint64_t s) { return mul2(s, e2); });
       if (!STATE_ONLY) {
         float* o = out + (int64_t)(row + dir * r) * a.os;
 #pragma unroll
@@ -184,10 +198,13 @@ __global__ void __launch_bounds__(32) la_simt_kernel(const __grid_constant__ LaA
         }
       }
     }
-    total += sum;
     if ((flags & LAST) && (STATE_ONLY || ((flags & ENDS) && a.state_out))) {
       put_state(STATE_ONLY ? a.ws_state + ((tile + 1) * a.H + h) * KV : a.state_out + ((int64_t)seq * a.H + h) * KV);
-      if (STATE_ONLY && sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
+      if (STATE_ONLY) {
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
+        if (sl == 0 && lane == 0) a.ws_decay[(tile + 1) * a.H + h] = total;
+      }
     }
     __syncwarp();
     issue(w);

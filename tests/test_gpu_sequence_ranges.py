@@ -428,3 +428,17 @@ def test_cross_fp32_is_as_near_as_fp32_products(T, D, nq, nk):
     T.cross_attention(q, k, v, dev([0, nq], "int64"), dev([0, nk], "int64"), out)
     ref = Q.cross_attention(host(q), host(k), host(v), [0, nq], [0, nk], D ** -0.5)
     assert np.linalg.norm(host(out) - ref) < 12 * U * np.linalg.norm(ref)
+
+
+def test_linear_fp32_over_slow_decays(T):
+    """A row's two roundings a value, 0.4 u each as a deviation, over the 700 rows that count, leave 15 u of
+    a state's size and of an output's; an error of the decay, which all values share, would add to it."""
+    r = np.random.default_rng(34)
+    n, H, K = 4000, 3, 32
+    q, k, v = (dev(r.normal(size=(n, H, K))) for _ in range(3))
+    g = dev(-0.001 * (0.5 + r.random((n, H))) * np.array([1.0, 2.0, 0.7]))
+    out, s1 = torch.empty_like(v), torch.empty((1, H, K, K), device="cuda")
+    T.linear_attention(q, k, v, g, dev([0, n], "int64"), out, state_out=s1)
+    o, s = Q.linear_attention(host(q), host(k), host(v), host(g), [0, n])
+    for got, ref in ((out, o), (s1, s)):
+        assert np.linalg.norm(host(got) - ref) < 24 * U * np.linalg.norm(ref)
