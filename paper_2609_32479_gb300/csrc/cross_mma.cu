@@ -12,8 +12,8 @@
 //
 // What bounds it: for tracks the instructions (131,072 tracks of five queries, 4 heads of 32, bf16:
 // 350 us a call, 3.7 TB/s of the 6.8 that a copy moves), for single queries memory (a state's K and V
-// are read once for the G heads that share them: 61 queries over 1-16,384 states, 4 heads of 128: 205
-// us a call, 4.4 TB/s; 173 the kernel, with five warps an SM).  P is the sum of two 16-bit parts as an operand of P V: with
+// are read once for the G heads that share them: 61 queries over 1-16,384 states, 4 heads of 128: 212
+// us a call, 4.3 TB/s; 173 the kernel, with five warps an SM).  P is the sum of two 16-bit parts as an operand of P V: with
 // one, rounded to 2^-8 (fp16 2^-11), the readout took 320 us instead of 355 and outputs were off by
 // as much again as by their own rounding.
 #include "cross_units.cuh"

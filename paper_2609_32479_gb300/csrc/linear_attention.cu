@@ -17,11 +17,11 @@ using namespace seqops;
 // memory as broadcasts, 8 rows at a time through a ring that the warp fills by asynchronous
 // copies.  Several columns a lane share what a row costs whatever its columns (loads,
 // exponentials, addresses: 90 of 116 instructions with one).  Measured: 20,011 tracks and parts
-// of tracks, 4 heads of 32 x 48, states in and out: 773 us a call, 3.4 TB/s; one column a lane 1136.
+// of tracks, 4 heads of 32 x 48, states in and out: 774 us a call, 3.4 TB/s; one column a lane 1136.
 // Every row decays the state itself: a factor kept beside it, which would save the product, makes
 // values up to that factor larger than the state.  A small decay goes in as S + (e^g - 1) S: e^g
 // rounded would be an error that all values of the state have in common, 2^-25 a row, which no sum
-// over them lessens (over 1,000 rows 2e-6 of the output, ten times what is left).
+// over them lessens (over 2,000 rows 2.4e-6 of the output; 4e-7 are left).
 constexpr int CH = 8, NST = 2;
 
 template <int DK, int CPL>

@@ -36,10 +36,10 @@
 // 2^-22 of what is added up; states asked for keep fp32.  With one part each for S and the fp16
 // weights it was 2^-8 and 2^-11 of it, for 7 % (tracks, bf16) to 20 % (fp16) less time.
 //
-// Measured: 131,072 tracks, 4 heads of 32, bf16: 426 us a call, 4.5 TB/s of the 6.8 that a copy
+// Measured: 131,072 tracks, 4 heads of 32, bf16: 425 us a call, 4.5 TB/s of the 6.8 that a copy
 // moves (412 the kernel; the rest two launches that find no sequence to cut); issued instructions
 // bound it (71 % of the slots with 16 warps an SM, the rest waits for their results).  Four sequences
-// of 20,000-40,000 rows, 8 heads of 64, states in and out: 364 us a call, 119 for the parts' own
+// of 20,000-40,000 rows, 8 heads of 64, states in and out: 363 us a call, 119 for the parts' own
 // states, 15 for what they pass on, 232 for the outputs, against 84 for one reading of everything;
 // latency with 8 warps an SM bounds it.
 #include "linear_units.cuh"
