@@ -494,6 +494,102 @@ int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, con
                              int32_t kv_heads, int32_t head_dim, float scale, void* out, int64_t out_stride,
                              void* workspace, size_t workspace_size, void* stream);
 
+/* The gated recurrence of Eq. 2 along each sequence, a state a channel, over any length:
+ *   z_t = sigma(p_t),   h_t = h_{t-1} + z_t (n_t - h_{t-1})
+ *   gate, cand  p and n, [n_rows][channels], column blocks of one projection for instance;
+ *   out         h, [n_rows][channels].  channels: a multiple of 8, at most 65536.
+ *   reverse     0: from a sequence's first row to its last; 1: from its last to its first.
+ *   state_in    fp32 [n_seq][channels] to begin with, or NULL (zeros).
+ *   state_out   the same shape, the state after each sequence (of an empty one: the state
+ *               before it), or NULL; may be state_in.
+ *   saved       trackfit_gated_scan_saved() bytes, 16-byte aligned, for
+ *               trackfit_gated_scan_backward, or NULL.
+ *   workspace   trackfit_gated_scan_workspace() bytes, 16-byte aligned (the parts of the rows
+ *               are joined through it; NULL when that is 0).
+ * z and 1 - z are both off by (2 |p| + 10) 2^-24 of themselves at most, however near to 0. */
+size_t trackfit_gated_scan_saved(int64_t n_rows, int32_t channels);
+size_t trackfit_gated_scan_workspace(int32_t dtype, int64_t n_rows, int64_t n_seq, int32_t channels);
+int trackfit_gated_scan(int32_t dtype, const void* gate, int64_t gate_stride, const void* cand, int64_t cand_stride,
+                        int64_t n_rows, const int64_t* offsets, int64_t n_seq, int32_t channels, int32_t reverse,
+                        const float* state_in, float* state_out, float* saved, void* out, int64_t out_stride,
+                        void* workspace, size_t workspace_size, void* stream);
+
+/* The gradients of trackfit_gated_scan: with g_t that of h_t from d_out and D_t all of it,
+ *   D_t = g_t + (1 - z_{t+1}) D_{t+1},  dn_t = z_t D_t,  dp_t = z_t (1 - z_t) (n_t - h_{t-1}) D_t
+ *   gate, cand, offsets, reverse, state_in   as they were in the forward call (state_in's
+ *               values too: a call whose state_out was state_in keeps a copy for this one).
+ *   saved       what the forward call wrote there (the states at every 128 rows; those in
+ *               between are formed again).
+ *   d_out       g, [n_rows][channels].
+ *   d_state_out fp32 [n_seq][channels], the gradients of state_out, or NULL (zeros).
+ *   d_state_in  the same shape, the gradients of state_in, or NULL; may be d_state_out.
+ *   d_gate, d_cand   dp and dn, [n_rows][channels]; column blocks of one array for instance.
+ *   workspace   as for the forward call, of the same size. */
+int trackfit_gated_scan_backward(int32_t dtype, const void* gate, int64_t gate_stride, const void* cand,
+                                 int64_t cand_stride, int64_t n_rows, const int64_t* offsets, int64_t n_seq,
+                                 int32_t channels, int32_t reverse, const float* state_in, const float* saved,
+                                 const void* d_out, int64_t d_out_stride, const float* d_state_out, float* d_state_in,
+                                 void* d_gate, int64_t d_gate_stride, void* d_cand, int64_t d_cand_stride,
+                                 void* workspace, size_t workspace_size, void* stream);
+
+/* One row more of each of n_seq sequences: the step of trackfit_gated_scan.
+ *   gate, cand, out   as there, row b for sequence b.
+ *   slots, n_slots, state_in, state_out   as for trackfit_linear_attention_step, states of
+ *               [n_slots][channels]. */
+int trackfit_gated_scan_step(int32_t dtype, const void* gate, int64_t gate_stride, const void* cand,
+                             int64_t cand_stride, int64_t n_seq, int32_t channels, const int32_t* slots,
+                             int64_t n_slots, const float* state_in, float* state_out, void* out, int64_t out_stride,
+                             void* stream);
+
+/* Beside trackfit_precision, a type of rows in 8 bits (4 exponent bits, 3 of the fraction, the
+ * largest value 448), each row with an fp32 scale that its values are multiplied with. */
+#define TRACKFIT_E4M3 3
+
+/* Root-mean-square norm of rows, with the addition of a branch's output before it:
+ *   s = x + delta,  y = s / sqrt(mean(s^2) + eps) * gain over a row's channels
+ * (zeros where the sum of squares leaves fp32's range; s is not rounded before the norm).
+ *   x, delta    [n_rows][channels]; delta may be NULL (s = x).  channels: a multiple of 8 (16
+ *               with an output in 8 bits), at most 16384.
+ *   sum_out     s in the rows' type, or NULL; may be x or delta (same stride).
+ *   gain        device fp32 [channels], or NULL (ones).  eps > 0.
+ *   out_type    dtype, or TRACKFIT_E4M3: out holds y / scale to the nearest (halves to even)
+ *               and scales[row], fp32, the scale max |y| / 448, 2^-100 at least.
+ *   out         [n_rows][channels] of out_type; of the rows' type it may be x or delta (same
+ *               stride) where sum_out is not the same array.
+ *   scales      device fp32 [n_rows]; NULL unless out_type is TRACKFIT_E4M3. */
+int trackfit_add_norm(int32_t dtype, const void* x, int64_t x_stride, const void* delta, int64_t delta_stride,
+                      int64_t n_rows, int32_t channels, const float* gain, float eps, void* sum_out,
+                      int64_t sum_stride, int32_t out_type, void* out, int64_t out_stride, float* scales,
+                      void* stream);
+
+/* What a product's sum goes through before the gate. */
+typedef enum {
+  TRACKFIT_ACT_NONE = 0,
+  TRACKFIT_ACT_RELU = 1,
+  TRACKFIT_ACT_SILU = 2,  /* y sigma(y) */
+  TRACKFIT_ACT_GELU = 3   /* y (1 + erf(y / sqrt 2)) / 2 */
+} trackfit_activation;
+
+/* Rows times a weight matrix, with an epilogue:
+ *   out = residual + act(x W^T + bias) * sigma(gate)
+ *   operand_type   dtype, or TRACKFIT_E4M3 for x and W in 8 bits (trackfit_add_norm's output for
+ *               instance): then the sum is multiplied by x_scales[row] * weight_scales[output].
+ *   x           [n_rows][in_dim] of operand_type; weight W [out_dim][in_dim], likewise.  in_dim: a
+ *               multiple of 8 (16 in 8 bits), at most 16384; out_dim: of 8, at most 65536.
+ *   x_scales, weight_scales   device fp32 [n_rows], [out_dim]; NULL unless in 8 bits.
+ *   bias        device fp32 [out_dim], or NULL (zeros).
+ *   gate        [n_rows][out_dim] of dtype, or NULL (no gate).
+ *   residual    [n_rows][out_dim] of dtype, or NULL (none); may be out (same stride).
+ *   out         [n_rows][out_dim] of dtype.
+ * Products are exact and added in fp32 (16 and 8 bits: by the tensor cores, which drop what is
+ * below a sum's last bit: at most 2^-22 of the largest partial sum for 16 channels); fp32 rows are
+ * multiplied and added in fp32.  What is not finite in a row of x stays in that row of out. */
+int trackfit_product(int32_t dtype, int32_t operand_type, const void* x, int64_t x_stride, const float* x_scales,
+                     const void* weight, int64_t weight_stride, const float* weight_scales, int64_t n_rows,
+                     int32_t in_dim, int32_t out_dim, const float* bias, int32_t activation, const void* gate,
+                     int64_t gate_stride, const void* residual, int64_t residual_stride, void* out,
+                     int64_t out_stride, void* stream);
+
 /* The counterpart of trackfit_device_errors for the operators: synchronises `stream` and
  * returns TRACKFIT_ERR_TIMEOUT if a bounded wait of an operator's kernel on the current
  * device has expired, whatever its stream, since the calling thread last asked with this

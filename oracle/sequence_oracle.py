@@ -1,11 +1,14 @@
 """Plain numpy fp64 definitions of the operators on packed sequences: norms of heads with
 the position rotation, linear attention with a decay a head (whole sequences and a single
-row), attention to the states of an encoder.  A row at a time, a sequence at a time;
-nothing is blocked, fused or approximated.
+row), attention to the states of an encoder, the gated recurrence with its gradients, the
+norm with a residual's addition, the product with its epilogue.  A row at a time, a sequence
+at a time; nothing is blocked, fused or approximated.
 
 Rows of all sequences stand back to back; sequence b has the rows offsets[b] ..
 offsets[b + 1] - 1.  Rows of no sequence stay as `out` has them (NaN here)."""
 from __future__ import annotations
+
+import math
 
 import numpy as np
 
@@ -71,3 +74,83 @@ def cross_attention(q, k, v, q_offsets, kv_offsets, scale):
             p = np.exp(s - s.max(axis=1, keepdims=True))
             out[qs, h] = (p / p.sum(axis=1, keepdims=True)) @ v[ks, h // G]
     return out
+
+
+def logistic(x):
+    """1 / (1 + exp(-x)), accurate near 0 too."""
+    x = np.asarray(x, np.float64)
+    e = np.exp(-np.abs(x))
+    return np.where(x >= 0, 1.0, e) / (1.0 + e)
+
+
+def gated_scan(p, n, offsets, reverse=False, state_in=None):
+    """h <- h + sigma(p) (n - h) along each sequence: (out [N, C], states [B, C] after each)."""
+    p, n = np.asarray(p, np.float64), np.asarray(n, np.float64)
+    z = logistic(p)
+    B = len(offsets) - 1
+    out = np.full(n.shape, np.nan)
+    states = np.zeros((B, n.shape[1])) if state_in is None else np.array(state_in, np.float64)
+    for b in range(B):
+        h = states[b]
+        rows = range(int(offsets[b]), int(offsets[b + 1]))
+        for t in (reversed(rows) if reverse else rows):
+            h = h + z[t] * (n[t] - h)
+            out[t] = h
+        states[b] = h
+    return out, states
+
+
+def gated_scan_backward(p, n, offsets, d_out, reverse=False, state_in=None, d_state_out=None):
+    """Gradients of p, n [N, C] and of the first states [B, C]."""
+    p, n, g = (np.asarray(t, np.float64) for t in (p, n, d_out))
+    z, w = logistic(p), logistic(-p)
+    B, C = len(offsets) - 1, n.shape[1]
+    dp, dn = np.full(n.shape, np.nan), np.full(n.shape, np.nan)
+    h, _ = gated_scan(p, n, offsets, reverse, state_in)
+    first = np.zeros((B, C)) if state_in is None else np.asarray(state_in, np.float64)
+    d0 = np.zeros((B, C)) if d_state_out is None else np.array(d_state_out, np.float64)
+    for b in range(B):
+        rows = list(range(int(offsets[b]), int(offsets[b + 1])))
+        if reverse:
+            rows.reverse()
+        d = d0[b]
+        for i in range(len(rows) - 1, -1, -1):
+            t = rows[i]
+            before = h[rows[i - 1]] if i > 0 else first[b]
+            d = d + g[t]
+            dn[t] = z[t] * d
+            dp[t] = z[t] * w[t] * (n[t] - before) * d
+            d = w[t] * d
+        d0[b] = d
+    return dp, dn, d0
+
+
+def e4m3(x):
+    """The nearest values of the 8-bit type (halves to even), for |x| <= 448."""
+    x = np.asarray(x, np.float64)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        step = np.exp2(np.maximum(np.floor(np.log2(np.abs(x))), -6) - 3)
+    return np.where(np.abs(x) > 0, np.round(x / step) * step, x)
+
+
+def add_norm(x, delta, gain, eps):
+    """(s, y): s = x + delta (None: x), y = s over sqrt(mean of squares + eps), times gain."""
+    s = np.asarray(x, np.float64) + (0.0 if delta is None else np.asarray(delta, np.float64))
+    y = s / np.sqrt(np.mean(s * s, axis=-1, keepdims=True) + eps)
+    return s, y if gain is None else y * np.asarray(gain, np.float64)
+
+
+def product(x, weight, bias=None, activation="none", gate=None, residual=None):
+    """residual + act(x W^T + bias) * sigma(gate); None: left out."""
+    y = np.asarray(x, np.float64) @ np.asarray(weight, np.float64).T
+    if bias is not None:
+        y = y + np.asarray(bias, np.float64)
+    if activation == "relu":
+        y = np.maximum(y, 0.0)
+    elif activation == "silu":
+        y = y * logistic(y)
+    elif activation == "gelu":
+        y = y * 0.5 * np.vectorize(math.erfc, otypes=[float])(-y / math.sqrt(2.0))
+    if gate is not None:
+        y = y * logistic(gate)
+    return y if residual is None else y + np.asarray(residual, np.float64)

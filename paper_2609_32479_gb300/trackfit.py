@@ -30,7 +30,11 @@ EXPORTS = ("trackfit_weight_count", "trackfit_create", "trackfit_forward", "trac
            "trackfit_decode", "trackfit_forward_packed", "trackfit_last_error", "trackfit_qk_norm",
            "trackfit_linear_attention", "trackfit_linear_attention_workspace", "trackfit_linear_attention_step",
            "trackfit_cross_attention", "trackfit_cross_attention_workspace", "trackfit_operator_errors",
-           "trackfit_debug_operator_wait")
+           "trackfit_debug_operator_wait", "trackfit_gated_scan", "trackfit_gated_scan_saved",
+           "trackfit_gated_scan_workspace", "trackfit_gated_scan_backward", "trackfit_gated_scan_step",
+           "trackfit_add_norm", "trackfit_product")
+E4M3 = 3
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 
 class Config(ctypes.Structure):
@@ -127,6 +131,22 @@ def load() -> ctypes.CDLL:
     lib.trackfit_cross_attention.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32, f32,
                                              vp, i64, vp, size, vp]
     lib.trackfit_cross_attention.restype = ctypes.c_int
+    lib.trackfit_gated_scan_saved.argtypes = [i64, i32]
+    lib.trackfit_gated_scan_saved.restype = size
+    lib.trackfit_gated_scan_workspace.argtypes = [i32, i64, i64, i32]
+    lib.trackfit_gated_scan_workspace.restype = size
+    lib.trackfit_gated_scan.argtypes = [i32, vp, i64, vp, i64, i64, vp, i64, i32, i32, vp, vp, vp, vp, i64, vp, size, vp]
+    lib.trackfit_gated_scan.restype = ctypes.c_int
+    lib.trackfit_gated_scan_backward.argtypes = [i32, vp, i64, vp, i64, i64, vp, i64, i32, i32, vp, vp, vp, i64, vp, vp,
+                                                 vp, i64, vp, i64, vp, size, vp]
+    lib.trackfit_gated_scan_backward.restype = ctypes.c_int
+    lib.trackfit_gated_scan_step.argtypes = [i32, vp, i64, vp, i64, i64, i32, vp, i64, vp, vp, vp, i64, vp]
+    lib.trackfit_gated_scan_step.restype = ctypes.c_int
+    lib.trackfit_add_norm.argtypes = [i32, vp, i64, vp, i64, i64, i32, vp, f32, vp, i64, i32, vp, i64, vp, vp]
+    lib.trackfit_add_norm.restype = ctypes.c_int
+    lib.trackfit_product.argtypes = [i32, i32, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp, i32, vp, i64, vp, i64, vp,
+                                     i64, vp]
+    lib.trackfit_product.restype = ctypes.c_int
     lib.trackfit_operator_errors.argtypes = [vp]
     lib.trackfit_operator_errors.restype = ctypes.c_int
     lib.trackfit_debug_operator_wait.argtypes = [i64, i32]
@@ -434,6 +454,19 @@ class _OpArgs:
             raise ValueError(f"{self.what}: the heads of a row of {name} must stand side by side, got strides {s}")
         return t.data_ptr(), s[0] if n > 1 else h * d
 
+    def matrix(self, name, t, shape, dtype=None):
+        """(pointer, row stride) of [rows, width], (None, 0) for None."""
+        if t is None:
+            return None, 0
+        dtype = self.dtype if dtype is None else dtype
+        if t.shape != shape or t.dtype != dtype or t.device != self.device:
+            raise ValueError(f"{self.what}: {name} must be {list(shape)} {dtype} on {self.device}, got "
+                             f"{list(t.shape)} {t.dtype} on {t.device}")
+        s = t.stride()
+        if s[1] != 1 and shape[1] > 1 and shape[0] > 0:
+            raise ValueError(f"{self.what}: the values of a row of {name} must stand side by side, got strides {s}")
+        return t.data_ptr(), s[0] if shape[0] > 1 else shape[1]
+
     def vector(self, name, t, dtype, shape):
         """Pointer of a contiguous array, None for None."""
         if t is None:
@@ -442,6 +475,10 @@ class _OpArgs:
             raise ValueError(f"{self.what}: {name} must be contiguous {list(shape)} {dtype} on {self.device}, got "
                              f"{list(t.shape)} {t.dtype} on {t.device}")
         return t.data_ptr()
+
+    def kept(self, name, t, n, c):
+        """Pointer of what a forward pass keeps for the backward pass, None for None."""
+        return None if t is None else self.vector(name, t, self.torch.float32, (gated_scan_saved(n, c),))
 
     def decay(self, t, n, h):
         s = t.stride()
@@ -566,6 +603,121 @@ def cross_attention(q, k, v, q_offsets, kv_offsets, out, scale: Optional[float] 
             a.vector("kv_offsets", kv_offsets, a.torch.int64, (b + 1,)), nk, b, hq, hk, d,
             float(d) ** -0.5 if scale is None else float(scale), op, os_),
            stream, need=lib.trackfit_cross_attention_workspace(t, nq, nk, b, hq, hk, d), workspace=workspace)
+
+
+def gated_scan_saved(n_rows: int, channels: int) -> int:
+    """fp32 values that gated_scan keeps for gated_scan_backward."""
+    return int(load().trackfit_gated_scan_saved(n_rows, channels)) // 4
+
+
+def gated_scan_workspace(dtype, n_rows: int, n_seq: int, channels: int) -> int:
+    """Bytes of workspace of a gated_scan or gated_scan_backward call on rows of a torch type."""
+    import torch
+    code = {torch.float32: W.PRECISION_FP32, torch.bfloat16: W.PRECISION_BF16, torch.float16: W.PRECISION_FP16}[dtype]
+    return int(load().trackfit_gated_scan_workspace(code, n_rows, n_seq, channels))
+
+
+def gated_scan(gate, cand, offsets, out, reverse: bool = False, state_in=None, state_out=None, saved=None,
+               workspace=None, stream=None) -> None:
+    """h <- h + sigma(p) (n - h) along each sequence: gate p, cand n, out h [N, C] (strided
+    rows), offsets [B + 1] i64; states [B, C] f32 before and after, or None.  saved: an array
+    of gated_scan_saved(N, C) f32 values for gated_scan_backward, or None."""
+    n, c = gate.shape
+    b = int(offsets.shape[0]) - 1
+    a = _OpArgs("gated_scan", gate)
+    pp, ps = a.matrix("gate", gate, (n, c))
+    np_, ns = a.matrix("cand", cand, (n, c))
+    op, os_ = a.matrix("out", out, (n, c))
+    lib, f32 = load(), a.torch.float32
+    a.call(lib.trackfit_gated_scan,
+           (a.code, pp, ps, np_, ns, n, a.vector("offsets", offsets, a.torch.int64, (b + 1,)), b, c,
+            int(bool(reverse)), a.vector("state_in", state_in, f32, (b, c)),
+            a.vector("state_out", state_out, f32, (b, c)), a.kept("saved", saved, n, c), op, os_),
+           stream, need=lib.trackfit_gated_scan_workspace(a.code, n, b, c), workspace=workspace)
+
+
+def gated_scan_backward(gate, cand, offsets, saved, d_out, d_gate, d_cand, reverse: bool = False, state_in=None,
+                        d_state_out=None, d_state_in=None, workspace=None, stream=None) -> None:
+    """Gradients of gated_scan, given what it saved: d_out [N, C] and d_state_out [B, C] f32 (or
+    None) -> d_gate, d_cand [N, C] and d_state_in [B, C] f32 (or None)."""
+    n, c = gate.shape
+    b = int(offsets.shape[0]) - 1
+    a = _OpArgs("gated_scan_backward", gate)
+    pp, ps = a.matrix("gate", gate, (n, c))
+    np_, ns = a.matrix("cand", cand, (n, c))
+    gp, gs = a.matrix("d_out", d_out, (n, c))
+    dpp, dps = a.matrix("d_gate", d_gate, (n, c))
+    dnp, dns = a.matrix("d_cand", d_cand, (n, c))
+    lib, f32 = load(), a.torch.float32
+    a.call(lib.trackfit_gated_scan_backward,
+           (a.code, pp, ps, np_, ns, n, a.vector("offsets", offsets, a.torch.int64, (b + 1,)), b, c,
+            int(bool(reverse)), a.vector("state_in", state_in, f32, (b, c)), a.kept("saved", saved, n, c), gp, gs,
+            a.vector("d_state_out", d_state_out, f32, (b, c)), a.vector("d_state_in", d_state_in, f32, (b, c)),
+            dpp, dps, dnp, dns),
+           stream, need=lib.trackfit_gated_scan_workspace(a.code, n, b, c), workspace=workspace)
+
+
+def gated_scan_step(gate, cand, state_in, state_out, out, slots=None, stream=None) -> None:
+    """One row more of each of B sequences: gate, cand, out [B, C]; states [slots, C] f32, taken
+    from and put to slots [B] i32 (None: state b).  A slot outside the states: a NaN row, no
+    state."""
+    b, c = gate.shape
+    a = _OpArgs("gated_scan_step", gate)
+    ns = int(state_in.shape[0])
+    pp, ps = a.matrix("gate", gate, (b, c))
+    np_, nst = a.matrix("cand", cand, (b, c))
+    op, os_ = a.matrix("out", out, (b, c))
+    f32 = a.torch.float32
+    a.call(load().trackfit_gated_scan_step,
+           (a.code, pp, ps, np_, nst, b, c, a.vector("slots", slots, a.torch.int32, (b,)), ns,
+            a.vector("state_in", state_in, f32, (ns, c)), a.vector("state_out", state_out, f32, (ns, c)), op, os_),
+           stream)
+
+
+def add_norm(x, out, delta=None, sum_out=None, gain=None, eps: float = 1e-6, scales=None, stream=None) -> None:
+    """Root-mean-square norm of x + delta [N, C] with gain [C] f32 -> out [N, C], in the rows'
+    type or, torch.float8_e4m3fn, in 8 bits with scales [N] f32; the sum itself -> sum_out [N, C].
+    delta, sum_out and gain may be None."""
+    n, c = x.shape
+    a = _OpArgs("add_norm", x)
+    e8 = a.torch.float8_e4m3fn
+    eight = out.dtype == e8
+    xp, xs = a.matrix("x", x, (n, c))
+    dp, ds = a.matrix("delta", delta, (n, c))
+    sp, ss = a.matrix("sum_out", sum_out, (n, c))
+    op, os_ = a.matrix("out", out, (n, c), e8 if eight else None)
+    if eight != (scales is not None):
+        raise ValueError("add_norm: scales go with an output in 8 bits")
+    f32 = a.torch.float32
+    a.call(load().trackfit_add_norm,
+           (a.code, xp, xs, dp, ds, n, c, a.vector("gain", gain, f32, (c,)), float(eps), sp, ss,
+            E4M3 if eight else a.code, op, os_, a.vector("scales", scales, f32, (n,))), stream)
+
+
+def product(x, weight, out, bias=None, activation: str = "none", gate=None, residual=None, x_scales=None,
+            weight_scales=None, stream=None) -> None:
+    """residual + act(x weight^T + bias) * sigma(gate) -> out [N, M]: x [N, K], weight [M, K] of
+    out's type, or both torch.float8_e4m3fn with x_scales [N] and weight_scales [M] f32; bias [M]
+    f32, gate and residual [N, M] or None; activation "none", "relu", "silu" or "gelu"."""
+    n, k = x.shape
+    m = int(weight.shape[0])
+    a = _OpArgs("product", out)
+    e8 = a.torch.float8_e4m3fn
+    eight = x.dtype == e8
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"product: activation must be one of {', '.join(ACTIVATIONS)}, got {activation!r}")
+    if eight != (x_scales is not None) or eight != (weight_scales is not None):
+        raise ValueError("product: x_scales and weight_scales go with operands in 8 bits")
+    xp, xs = a.matrix("x", x, (n, k), e8 if eight else None)
+    wp, ws = a.matrix("weight", weight, (m, k), e8 if eight else None)
+    op, os_ = a.matrix("out", out, (n, m))
+    gp, gs = a.matrix("gate", gate, (n, m))
+    rp, rs = a.matrix("residual", residual, (n, m))
+    f32 = a.torch.float32
+    a.call(load().trackfit_product,
+           (a.code, E4M3 if eight else a.code, xp, xs, a.vector("x_scales", x_scales, f32, (n,)), wp, ws,
+            a.vector("weight_scales", weight_scales, f32, (m,)), n, k, m, a.vector("bias", bias, f32, (m,)),
+            ACTIVATIONS[activation], gp, gs, rp, rs, op, os_), stream)
 
 
 def operator_errors(stream=None) -> int:
