@@ -504,6 +504,24 @@ int seqops::cross_tc(int32_t dtype, const CaArgs& a, cudaStream_t st) {
   return a.D <= 64 ? launch<__half, 1>(a, true, st) : launch<__half, 2>(a, true, st);
 }
 
+uint64_t seqops::operator_limit_ns() { return g_limit_ns.load(); }
+
+unsigned long long* seqops::operator_expired() {
+  static std::atomic<unsigned long long*> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  unsigned long long* p = dev < 64 ? known[dev].load() : nullptr;
+  if (!p) {
+    const cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(&p), g_expired);
+    if (e != cudaSuccess) {
+      tf_note_cuda(e, "cudaGetSymbolAddress");
+      return nullptr;
+    }
+    if (dev < 64) known[dev].store(p);
+  }
+  return p;
+}
+
 extern "C" int trackfit_debug_operator_wait(int64_t limit_ns, int32_t hold) {
   if (limit_ns < 0 || limit_ns > (int64_t)LIMIT_NS || hold < 0 || hold > 1) return TRACKFIT_ERR_INVALID_ARG;
   g_limit_ns.store(limit_ns > 0 ? (uint64_t)limit_ns : LIMIT_NS);

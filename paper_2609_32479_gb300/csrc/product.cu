@@ -1,76 +1,110 @@
-// A product of rows with a weight matrix and its epilogue:
+// Rows times a weight matrix and the product's epilogue:
 //   out = residual + act(x W^T [* x_scales w_scales] + bias) * sigma(gate)
 //
-// Tiles of 64 x 64 outputs on the CUDA cores, 16 channels at a time through shared memory.
-#include "seq_ops.cuh"
-
-#include <cuda_fp8.h>
+// Up to 16 rows go to product_few.cu, more rows of 16 or 8 bits to product_tc.cu, more rows of fp32
+// to the kernel here: tiles of TM x TN outputs on the CUDA cores, 16 channels at a time through two
+// buffers in shared memory, the next one's loads under way while one is used.  A thread adds up
+// RM x RN outputs, two neighbouring ones in an instruction; each output's products are added in the
+// order of the channels, in fp32.
+#include "product_units.cuh"
 
 namespace {
 using namespace seqops;
 
 constexpr int MAX_INNER = 1 << 14, MAX_OUTER = 1 << 16;
-constexpr int TM = 64, TN = 64, TK = 16;
+constexpr int TK = 16, NT = 256;
 
-struct PrArgs {
-  const void *x, *w, *gate, *res;
-  void* out;
-  int64_t xs, ws, gs, rs, os;
-  const float *x_scales, *w_scales, *bias;
-  int64_t n;
-  int K, M, act;
-};
-
-template <class T>
-__device__ __forceinline__ float operand(T x) { return to_float(x); }
-__device__ __forceinline__ float operand(__nv_fp8_e4m3 x) { return (float)x; }
-__device__ __forceinline__ float sigma(float x) { return 1.0f / (1.0f + expf(-x)); }
-__device__ __forceinline__ float activate(float y, int act) {
-  switch (act) {
-    case TRACKFIT_ACT_RELU: return y < 0.0f ? 0.0f : y;
-    case TRACKFIT_ACT_SILU: return y * sigma(y);
-    case TRACKFIT_ACT_GELU: return 0.5f * y * erfcf(y * -0.70710678118654752f);
-    default: return y;
+template <int RM, int RN>
+__global__ void __launch_bounds__(NT) product_fp32_kernel(const ProductArgs a, int tiles_n) {
+  constexpr int TM = 16 * RM, TN = 16 * RN, LX = TM * 4 / NT, LW = TN * 4 / NT;
+  static_assert(RM % 4 == 0 && RN % 4 == 0, "16 bytes of rows and outputs");
+  __shared__ __align__(16) float xs[2][TK][TM + 4], ws[2][TK][TN + 4];
+  const int64_t r0 = (int64_t)(blockIdx.x / tiles_n) * TM;
+  const int c0 = (int)(blockIdx.x % tiles_n) * TN, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  const int lr = threadIdx.x / 4, lk = threadIdx.x % 4 * 4;       // this thread's row and channels of a load
+  const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float4 u[LX], v[LW];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < LX; ++i) {
+      const int64_t r = r0 + lr + i * (NT / 4);
+      u[i] = r < a.n && k0 + lk < a.K ? __ldg(reinterpret_cast<const float4*>((const float*)a.x + r * a.xs + k0 + lk)) : none;
+    }
+#pragma unroll
+    for (int i = 0; i < LW; ++i) {
+      const int64_t c = c0 + lr + i * (NT / 4);
+      v[i] = c < a.M && k0 + lk < a.K ? __ldg(reinterpret_cast<const float4*>((const float*)a.w + c * a.ws + k0 + lk)) : none;
+    }
+  };
+  auto put_down = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < LX; ++i) {
+      float* d = &xs[b][lk][lr + i * (NT / 4)];
+      d[0] = u[i].x, d[TM + 4] = u[i].y, d[2 * (TM + 4)] = u[i].z, d[3 * (TM + 4)] = u[i].w;
+    }
+#pragma unroll
+    for (int i = 0; i < LW; ++i) {
+      float* d = &ws[b][lk][lr + i * (NT / 4)];
+      d[0] = v[i].x, d[TN + 4] = v[i].y, d[2 * (TN + 4)] = v[i].z, d[3 * (TN + 4)] = v[i].w;
+    }
+  };
+  uint64_t acc[RM][RN / 2];
+#pragma unroll
+  for (int i = 0; i < RM; ++i)
+#pragma unroll
+    for (int j = 0; j < RN / 2; ++j) acc[i][j] = 0;
+  load(0);
+  put_down(0);
+  __syncthreads();
+  for (int k0 = 0, b = 0; k0 < a.K; k0 += TK, b ^= 1) {
+    if (k0 + TK < a.K) load(k0 + TK);
+#pragma unroll
+    for (int k = 0; k < TK; ++k) {
+      float x[RM];
+      uint64_t w[RN / 2];
+#pragma unroll
+      for (int i = 0; i < RM; i += 4) *reinterpret_cast<float4*>(&x[i]) = *reinterpret_cast<const float4*>(&xs[b][k][16 * i + 4 * ty]);
+#pragma unroll
+      for (int j = 0; j < RN; j += 4) {
+        const ulonglong2 t = *reinterpret_cast<const ulonglong2*>(&ws[b][k][16 * j + 4 * tx]);
+        w[j / 2] = t.x, w[j / 2 + 1] = t.y;
+      }
+#pragma unroll
+      for (int i = 0; i < RM; ++i) {
+        const uint64_t xx = both(x[i], x[i]);
+#pragma unroll
+        for (int j = 0; j < RN / 2; ++j) acc[i][j] = fma2(xx, w[j], acc[i][j]);
+      }
+    }
+    if (k0 + TK < a.K) put_down(b ^ 1);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < RM; ++i) {
+    const int64_t r = r0 + 16 * (i / 4 * 4) + 4 * ty + i % 4;
+    if (r >= a.n) continue;
+#pragma unroll
+    for (int j = 0; j < RN; j += 4) {
+      const int c = c0 + 16 * j + 4 * tx;
+      if (c >= a.M) continue;
+      const float2 lo = parts(acc[i][j / 2]), hi = parts(acc[i][j / 2 + 1]);
+      float y[4] = {lo.x, lo.y, hi.x, hi.y};
+      const uint4 z = make_uint4(0, 0, 0, 0);
+      const uint4 gate = a.gate ? *reinterpret_cast<const uint4*>((const float*)a.gate + r * a.gs + c) : z;
+      const uint4 res = a.res ? *reinterpret_cast<const uint4*>((const float*)a.res + r * a.rs + c) : z;
+      finish<float, false>(a, y, 1.0f, c, gate, res);
+      *reinterpret_cast<uint4*>((float*)a.out + r * a.os + c) = pack(y, 0.0f);
+    }
   }
 }
 
-template <class T, class O>
-__global__ void __launch_bounds__(256) product_kernel(const PrArgs a) {
-  __shared__ float xs[TK][TM + 1], ws[TK][TN + 1];
-  const int64_t r0 = (int64_t)blockIdx.x * TM;
-  const int c0 = blockIdx.y * TN, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < a.K; k0 += TK) {
-    for (int i = threadIdx.x; i < TM * TK; i += 256) {
-      const int r = i / TK, k = i % TK;
-      xs[k][r] = r0 + r < a.n && k0 + k < a.K ? operand(((const O*)a.x)[(r0 + r) * a.xs + k0 + k]) : 0.0f;
-      ws[k][r] = c0 + r < a.M && k0 + k < a.K ? operand(((const O*)a.w)[(int64_t)(c0 + r) * a.ws + k0 + k]) : 0.0f;
-    }
-    __syncthreads();
-    for (int k = 0; k < TK; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[k][ty * 4 + i], ws[k][tx * 4 + j], acc[i][j]);
-    __syncthreads();
-  }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t r = r0 + ty * 4 + i;
-      const int c = c0 + tx * 4 + j;
-      if (r >= a.n || c >= a.M) continue;
-      float y = acc[i][j];
-      if (a.x_scales) y *= a.x_scales[r] * a.w_scales[c];
-      if (a.bias) y += a.bias[c];
-      y = activate(y, a.act);
-      if (a.gate) y *= sigma(to_float(((const T*)a.gate)[r * a.gs + c]));
-      if (a.res) y += to_float(((const T*)a.res)[r * a.rs + c]);
-      put((T*)a.out + r * a.os + c, y);
-    }
-}
-
-template <class T>
-void launch(const PrArgs& a, bool eight, dim3 grid, cudaStream_t st) {
-  if (eight) product_kernel<T, __nv_fp8_e4m3><<<grid, 256, 0, st>>>(a);
-  else product_kernel<T, T><<<grid, 256, 0, st>>>(a);
+template <int RM, int RN>
+int launch(const ProductArgs& a, cudaStream_t st) {
+  const int tiles_n = (a.M + 16 * RN - 1) / (16 * RN);
+  const int64_t tiles = (a.n + 16 * RM - 1) / (16 * RM) * tiles_n;
+  if (tiles > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
+  product_fp32_kernel<RM, RN><<<(unsigned)tiles, NT, 0, st>>>(a, tiles_n);
+  return launched();
 }
 
 }  // namespace
@@ -96,18 +130,16 @@ extern "C" int trackfit_product(int32_t dtype, int32_t operand_type, const void*
     return TRACKFIT_ERR_INVALID_ARG;
   if (mis4(bias) || mis4(x_scales) || mis4(weight_scales) || (eight != (x_scales != nullptr)) || (eight != (weight_scales != nullptr)))
     return TRACKFIT_ERR_INVALID_ARG;
-  PrArgs a;
+  if (n_rows > 0x7fffff00) return TRACKFIT_ERR_UNSUPPORTED;   // a tile's coordinates have 32 bits
+  ProductArgs a;
   a.x = x, a.xs = x_stride, a.w = weight, a.ws = weight_stride, a.gate = gate, a.gs = gate_stride;
   a.res = residual, a.rs = residual_stride, a.out = out, a.os = out_stride;
   a.x_scales = x_scales, a.w_scales = weight_scales, a.bias = bias;
   a.n = n_rows, a.K = in_dim, a.M = out_dim, a.act = activation;
-  const int64_t tiles = (n_rows + TM - 1) / TM;
-  const int cols = (out_dim + TN - 1) / TN;
-  if (tiles > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)tiles, (unsigned)cols);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (dtype == TRACKFIT_FP32) launch<float>(a, eight, grid, st);
-  else if (dtype == TRACKFIT_BF16_PROJ) launch<__nv_bfloat16>(a, eight, grid, st);
-  else launch<__half>(a, eight, grid, st);
-  return launched();
+  if (n_rows <= PRODUCT_FEW) return product_few(dtype, a, st);
+  if (eight || dtype != TRACKFIT_FP32) return product_tc(dtype, a, st);
+  // tiles of 128 x 128 while they fill the SMs, else of 64 x 64
+  const bool large = (n_rows + 127) / 128 * ((out_dim + 127) / 128) >= 152;
+  return large ? launch<8, 8>(a, st) : launch<4, 4>(a, st);
 }

@@ -169,6 +169,11 @@ inline cudaError_t allow_smem(size_t bytes) {
   if (e == cudaSuccess) given.fetch_or(bit);
   return e;
 }
+// The operators' bounded waits (cross_tc.cu): the limit in force, and the current device's count of
+// those that have expired (null: no such device memory), for trackfit_operator_errors().
+uint64_t operator_limit_ns();
+unsigned long long* operator_expired();
+
 inline int launched() {
   const cudaError_t e = cudaPeekAtLastError();
   if (e == cudaSuccess) return TRACKFIT_OK;
