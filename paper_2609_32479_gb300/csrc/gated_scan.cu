@@ -65,50 +65,92 @@ struct GsArgs {
   unsigned long long* expired;
 };
 
-// z and w of a gate, each accurate however near to 0: 2^(-|p| log2 e) and 1 over one more than it.
+__device__ __forceinline__ float rcp(float x) {   // (1 ulp; for x in [1, 2])
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// z and w of a gate, each accurate however near to 0: from 2^(-|p| log2 e) and 1 over one more than it.
 __device__ __forceinline__ void gate(float p, float& z, float& w) {
-  const float e = ex2(-LOG2E * fabsf(p)), r = __fdividef(1.0f, 1.0f + e), s = e * r;
+  const float e = ex2(-LOG2E * fabsf(p)), r = rcp(1.0f + e), s = e * r;
   z = p < 0.0f ? s : r, w = p < 0.0f ? r : s;
 }
 
+// A lane's channels of a row: 4 bytes, one or two fp32 values (two in the instructions that take two).
 template <class T>
-struct Lane;                               // a lane's channels of a row: 4 bytes
+struct Lane;
 template <>
 struct Lane<float> {
   static constexpr int V = 1;
-  static __device__ __forceinline__ void get(const void* p, float (&x)[1]) { x[0] = *(const float*)p; }
-  static __device__ __forceinline__ void put(void* p, const float (&x)[1]) { *(float*)p = x[0]; }
+  using P = float;
+  static __device__ __forceinline__ P make(float a, float) { return a; }
+  static __device__ __forceinline__ P get(uint32_t at) {
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+    return x;
+  }
+  static __device__ __forceinline__ void put(void* p, P x) { *(float*)p = x; }
+  static __device__ __forceinline__ P mul(P a, P b) { return a * b; }
+  static __device__ __forceinline__ P add(P a, P b) { return a + b; }
+  static __device__ __forceinline__ P sub(P a, P b) { return a - b; }
+  static __device__ __forceinline__ P fma(P a, P b, P c) { return fmaf(a, b, c); }
+  static __device__ __forceinline__ P pick(bool first, P a, P b) { return first ? a : b; }
+  static __device__ __forceinline__ void gates(P p, P& z, P& w) { gate(p, z, w); }
+  static __device__ __forceinline__ float part(P a, int) { return a; }
 };
 template <class T>
 struct Lane16 {
   static constexpr int V = 2;
-  static __device__ __forceinline__ void put(void* p, const float (&x)[2]) { *(uint32_t*)p = pack2(x[0], x[1], T()); }
+  using P = uint64_t;
+  static __device__ __forceinline__ P make(float a, float b) { return both(a, b); }
+  static __device__ __forceinline__ uint32_t word(uint32_t at) {
+    uint32_t x;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+    return x;
+  }
+  static __device__ __forceinline__ void put(void* p, P x) {
+    const float2 f = parts(x);
+    *(uint32_t*)p = pack2(f.x, f.y, T());
+  }
+  static __device__ __forceinline__ P mul(P a, P b) { return mul2(a, b); }
+  static __device__ __forceinline__ P add(P a, P b) { return add2(a, b); }
+  static __device__ __forceinline__ P sub(P a, P b) { return fma2(b, both(-1.0f, -1.0f), a); }
+  static __device__ __forceinline__ P fma(P a, P b, P c) { return fma2(a, b, c); }
+  static __device__ __forceinline__ P pick(bool first, P a, P b) { return first ? a : b; }
+  static __device__ __forceinline__ void gates(P p, P& z, P& w) {
+    const float2 f = parts(p);
+    const float2 x = parts(mul2(both(fabsf(f.x), fabsf(f.y)), both(-LOG2E, -LOG2E)));
+    const P e = both(ex2(x.x), ex2(x.y));
+    const float2 y = parts(add2(e, both(1.0f, 1.0f)));
+    const float2 r = make_float2(rcp(y.x), rcp(y.y)), s = parts(mul2(e, both(r.x, r.y)));
+    z = both(f.x < 0.0f ? s.x : r.x, f.y < 0.0f ? s.y : r.y), w = both(f.x < 0.0f ? r.x : s.x, f.y < 0.0f ? r.y : s.y);
+  }
+  static __device__ __forceinline__ float part(P a, int v) { return v ? parts(a).y : parts(a).x; }
 };
 template <>
 struct Lane<__nv_bfloat16> : Lane16<__nv_bfloat16> {
-  static __device__ __forceinline__ void get(const void* p, float (&x)[2]) {
-    const uint32_t u = *(const uint32_t*)p;
-    x[0] = __uint_as_float(u << 16), x[1] = __uint_as_float(u & 0xffff0000u);
+  static __device__ __forceinline__ P get(uint32_t at) {
+    const uint32_t u = word(at);
+    return both(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
   }
 };
 template <>
 struct Lane<__half> : Lane16<__half> {
-  static __device__ __forceinline__ void get(const void* p, float (&x)[2]) {
-    const float2 f = __half22float2(*(const __half2*)p);
-    x[0] = f.x, x[1] = f.y;
+  static __device__ __forceinline__ P get(uint32_t at) {
+    const uint32_t u = word(at);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
+    return both(f.x, f.y);
   }
 };
-
-// fp32 channels of a state array, V at a time (even channels: 8 bytes aligned)
-template <int V>
-__device__ __forceinline__ void get_state(const float* s, float (&x)[V]) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = s[v];
+template <class L>
+__device__ __forceinline__ typename L::P get_state(const float* s) {
+  if constexpr (L::V == 1) return s[0];
+  else return *reinterpret_cast<const uint64_t*>(s);
 }
-template <int V>
-__device__ __forceinline__ void put_state(float* s, const float (&x)[V]) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) s[v] = x[v];
+template <class L>
+__device__ __forceinline__ void put_state(float* s, typename L::P x) {
+  if constexpr (L::V == 1) s[0] = x;
+  else *reinterpret_cast<uint64_t*>(s) = x;
 }
 
 // Where sequences begin and end among the rows of a part.  Row r0 + i stands for bit i, i <= TILE.
@@ -123,10 +165,11 @@ struct Brought {
   Marks marks;
 };
 
-template <int V, int WIN>
+template <class L>
 struct Shared {
-  float2 agg[WARPS][32 * V];               // (A, B) of the warps' rows
-  float2 win[WIN][32 * V];                 // of the parts before, nearest first
+  static constexpr int WIN = 32 / L::V;    // parts looked back at
+  typename L::P agg_a[WARPS][32], agg_b[WARPS][32];   // A and B of the warps' rows
+  typename L::P win_a[WIN][32], win_b[WIN][32];       // of the parts before, nearest first
   uint32_t has[WARPS];                     // a warp's rows hold a sequence's beginning: A does not count
   uint32_t status[WIN];
   Brought brought[2];
@@ -135,6 +178,11 @@ struct Shared {
   int from;
   int abort, never;
 };
+
+// The buffers come behind it: a part of fewer rows, taken backwards, has positions whose rows would lie
+// up to 15 rows below its buffer; they are read there with the others and not used.
+template <class L>
+constexpr int SHARED = ((int)sizeof(Shared<L>) + 1023) / 1024 * 1024;
 
 // The rows of a part.
 struct Part {
@@ -156,6 +204,31 @@ __device__ __forceinline__ Part part_of(const GsArgs& a, const S* s, int64_t k) 
 __device__ __forceinline__ int row_in(const GsArgs& a, const Part& t, int i) { return a.reverse ? t.count - 1 - i : i; }
 
 __device__ __forceinline__ bool bound(const Marks& m, int d) { return (m.bound[d >> 5] >> (d & 31)) & 1u; }
+// 16 of the bits from number `low` on (below 0: zeros).
+__device__ __forceinline__ uint32_t bits16(const Marks& m, int low) {
+  if (low <= -16) return 0;
+  const int l = low < 0 ? 0 : low, w = l >> 5;
+  const uint32_t x = __funnelshift_r(m.bound[w], m.bound[w + 1 < 6 ? w + 1 : 5], l & 31);
+  return (low < 0 ? x << -low : x) & 0xffffu;
+}
+// Of a warp's 16 positions, bit i for the i-th: rows of sequences, first rows, last rows.
+struct Mine {
+  uint32_t valid, begins, ends;
+};
+__device__ __forceinline__ Mine mine_of(const GsArgs& a, const Part& t, const Marks& m, int warp) {
+  const int i0 = warp * RPW;
+  const int lo = (a.reverse ? t.count - t.hi : t.lo) - i0, hi = (a.reverse ? t.count - t.lo : t.hi) - i0;
+  Mine r;
+  r.valid = (hi <= 0 ? 0u : hi >= RPW ? 0xffffu : (1u << hi) - 1u) & (lo <= 0 ? 0xffffu : lo >= RPW ? 0u : 0xffffu << lo);
+  if (a.reverse) {   // position i is row count - 1 - i: it begins with the row's upper border
+    r.begins = __brev(bits16(m, t.count - i0 - RPW + 1)) >> 16;
+    r.ends = __brev(bits16(m, t.count - i0 - RPW)) >> 16;
+  } else {
+    r.begins = bits16(m, i0), r.ends = bits16(m, i0 + 1);
+  }
+  r.begins &= r.valid, r.ends &= r.valid;
+  return r;
+}
 // The sequence of a row that is its first (or last), by the row's lower or upper border.
 __device__ __forceinline__ int64_t sequence(const GsArgs& a, const Marks& m, int d, bool lower) {
   return clamp64(lower ? m.last[d] : (int64_t)m.first[d + 1] - 1, 0, a.n_seq - 1);
@@ -305,23 +378,19 @@ __device__ __forceinline__ void begin(const GsArgs& a, S* s) {
 // Among the warps that compute.
 __device__ __forceinline__ void meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-// What a run of rows makes of what comes before it.
-__device__ __forceinline__ float through(bool has, float2 f, float before) { return has ? f.y : fmaf(f.x, before, f.y); }
-
-// The warps' (A, B), in their order (BACK: the last first), as one; `before` only where no
-// sequence begins.
-template <bool BACK, class S>
-__device__ __forceinline__ float2 joined(const S* s, int c, bool& has) {
-  float2 f = make_float2(1.0f, 0.0f);
-  has = false;
+// The warps' (A, B), in their order (BACK: the last first), as one; A does not count if `has`.
+template <class L, bool BACK>
+__device__ __forceinline__ void joined(const Shared<L>* s, int lane, typename L::P& fa, typename L::P& fb, bool& has) {
+  fa = L::make(1.0f, 1.0f), fb = L::make(0.0f, 0.0f), has = false;
 #pragma unroll
   for (int i = 0; i < WARPS; ++i) {
     const int u = BACK ? WARPS - 1 - i : i;
-    const float2 g = s->agg[u][c];
-    if (s->has[u]) f = make_float2(0.0f, g.y), has = true;
-    else f.x *= g.x, f.y = fmaf(g.x, f.y, g.y);
+    const typename L::P ga = s->agg_a[u][lane], gb = s->agg_b[u][lane];
+    const bool h = s->has[u];
+    has = has || h;
+    fb = L::pick(h, gb, L::fma(ga, fb, gb));
+    fa = L::mul(ga, fa);
   }
-  return f;
 }
 
 __device__ __forceinline__ unsigned long long word(uint32_t what, float x) {
@@ -332,36 +401,45 @@ __device__ __forceinline__ void leave(unsigned long long* p, unsigned long long 
 }
 __device__ __forceinline__ ulonglong2 look(const ulonglong2* p) {
   ulonglong2 v;
-  asm volatile("ld.relaxed.gpu.global.v2.u64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "l"(p) : "memory");
+  asm volatile("ld.relaxed.gpu.global.v2.u64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "l"(p));
   return v;
 }
 
 // What the parts before part k (BACK: behind it) leave for this CTA's channels: false if the wait for
 // them expired.  All warps that compute; `in`: the lane has channels, c the first of them.
-template <bool BACK, int V, int WIN>
-__device__ __forceinline__ bool look_back(const GsArgs& a, Shared<V, WIN>* s, int64_t k, int c, bool in, float (&carry)[V]) {
+template <class L, bool BACK>
+__device__ __forceinline__ bool look_back(const GsArgs& a, Shared<L>* s, int64_t k, int c, bool in, typename L::P& carry) {
+  constexpr int V = L::V, WIN = Shared<L>::WIN, EACH = WIN / WARPS;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t there = BACK ? a.parts - 1 - k : k;           // so many parts there are
   uint64_t t0 = 0;
   for (int round = 0;; ++round) {
+    ulonglong2 u[EACH][V];                                    // all under way before the first is used
 #pragma unroll
-    for (int i = 0; i < WIN / WARPS; ++i) {
-      const int d = warp * (WIN / WARPS) + i;
-      bool ready = true, whole = true, some = false;
-      if (d < there && in) {
-        const int64_t at = BACK ? k + 1 + d : k - 1 - d;
+    for (int i = 0; i < EACH; ++i) {
+      const int d = warp * EACH + i;
+      const int64_t at = BACK ? k + 1 + d : k - 1 - d;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const ulonglong2 u = look(a.words + at * a.C + c + v);
-          const uint32_t what = (uint32_t)(u.y >> 32);
-          whole = whole && what == WHOLE, some = some || what == WHOLE;
-          ready = ready && (what == WHOLE || (what == PARTIAL && u.x >> 32 == PARTIAL));
-          s->win[d][lane * V + v] = make_float2(__uint_as_float((uint32_t)u.x), __uint_as_float((uint32_t)u.y));
-        }
+      for (int v = 0; v < V; ++v) {
+        u[i][v] = make_ulonglong2(0, (unsigned long long)WHOLE << 32);
+        if (d < there && in) u[i][v] = look(a.words + at * a.C + c + v);
       }
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int d = warp * EACH + i;
+      bool ready = true, whole = true, some = false;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const uint32_t what = (uint32_t)(u[i][v].y >> 32);
+        whole = whole && what == WHOLE, some = some || (in && what == WHOLE);
+        ready = ready && (what == WHOLE || (what == PARTIAL && u[i][v].x >> 32 == PARTIAL));
+      }
+      s->win_a[d][lane] = L::make(__uint_as_float((uint32_t)u[i][0].x), __uint_as_float((uint32_t)u[i][V - 1].x));
+      s->win_b[d][lane] = L::make(__uint_as_float((uint32_t)u[i][0].y), __uint_as_float((uint32_t)u[i][V - 1].y));
       // all channels of a part alike: a part seen while h replaces B counts as not there
       const bool all_whole = __all_sync(FULL, whole), all_ready = __all_sync(FULL, ready), any = __any_sync(FULL, some);
-      if (lane == 0) s->status[d] = d >= there || all_whole ? WHOLE : all_ready && !any ? PARTIAL : 0u;
+      if (lane == 0) s->status[d] = all_whole ? WHOLE : all_ready && !any ? PARTIAL : 0u;
     }
     meet();
     if (warp == 0) {
@@ -382,83 +460,101 @@ __device__ __forceinline__ bool look_back(const GsArgs& a, Shared<V, WIN>* s, in
     if (*(volatile int*)&s->abort) return false;
   }
   const int from = s->from;
-#pragma unroll
-  for (int v = 0; v < V; ++v) carry[v] = from < there ? s->win[from][lane * V + v].y : 0.0f;
-  for (int d = from - 1; d >= 0; --d)
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float2 f = s->win[d][lane * V + v];
-      carry[v] = fmaf(f.x, carry[v], f.y);
-    }
+  carry = s->win_b[from][lane];
+  for (int d = from - 1; d >= 0; --d) carry = L::fma(s->win_a[d][lane], carry, s->win_b[d][lane]);
   return true;
 }
 
 // (A, B) of a part, or B alone where the part holds a sequence's beginning, for those behind it.
-template <bool BACK, int V, int WIN>
-__device__ __forceinline__ void leave_part(const GsArgs& a, const Shared<V, WIN>* s, int64_t k, int c, int lane) {
+template <class L>
+__device__ __forceinline__ void leave_part(const GsArgs& a, int64_t k, int c, typename L::P fa, typename L::P fb, bool has) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    bool has;
-    const float2 f = joined<BACK>(s, lane * V + v, has);
+  for (int v = 0; v < L::V; ++v) {
     unsigned long long* w = &a.words[k * a.C + c + v].x;
-    if (!has) leave(w, word(PARTIAL, f.x));
-    leave(w + 1, word(has ? WHOLE : PARTIAL, f.y));
+    if (!has) leave(w, word(PARTIAL, L::part(fa, v)));
+    leave(w + 1, word(has ? WHOLE : PARTIAL, L::part(fb, v)));
   }
 }
-template <bool BACK, int V, int WIN>
-__device__ __forceinline__ void leave_whole(const GsArgs& a, const Shared<V, WIN>* s, int64_t k, int c, int lane,
-                                            const float (&carry)[V]) {
+
+__device__ __forceinline__ float lds(uint32_t at) {
+  float x;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ void sts(uint32_t at, float x) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory"); }
+
+// The barrier between what a warp has read of a buffer and the next copy into it.
+template <class S>
+__device__ __forceinline__ void release(S* s, int buf, int lane) {
+  __syncwarp();
+  if (lane == 0) sm100::mbar_arrive(smem_addr(&s->empty[buf]));
+}
+
+// The carry into the part, given the warps' (A, B): false if a wait expired.  ALONE: `carry` is already
+// what the parts before have made of it.
+template <class L, bool BACK, bool ALONE>
+__device__ __forceinline__ bool carry_into(const GsArgs& a, Shared<L>* s, int64_t k, int c, bool in, const Part& t,
+                                           const Marks& m, typename L::P& carry) {
+  if constexpr (ALONE) return true;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // what is before this part counts if its first position is a row within a sequence
+  const int d = row_in(a, t, BACK ? t.count - 1 : 0);
+  const bool inside = d >= t.lo && d < t.hi && !bound(m, BACK != (a.reverse != 0) ? d + 1 : d);
+  typename L::P fa, fb;
+  bool has = false;
+  if (warp == 0) {
+    joined<L, BACK>(s, lane, fa, fb, has);
+    if (in) leave_part<L>(a, k, c, fa, fb, has);
+  }
+  carry = L::make(0.0f, 0.0f);
+  if (!inside) return true;
+  if (!look_back<L, BACK>(a, s, k, c, in, carry)) return false;
+  if (warp == 0 && in && !has) {
+    const typename L::P h = L::fma(fa, carry, fb);
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    bool has;
-    const float2 f = joined<BACK>(s, lane * V + v, has);
-    if (!has) leave(&a.words[k * a.C + c + v].y, word(WHOLE, fmaf(f.x, carry[v], f.y)));
+    for (int v = 0; v < L::V; ++v) leave(&a.words[k * a.C + c + v].y, word(WHOLE, L::part(h, v)));
   }
+  return true;
 }
+
+static_assert(sizeof(Shared<Lane<float>>) >= RPW * 128, "room below the buffers");
 
 // ---------------------------------------------------------------- forward
 
-// (A, B) of the warp's rows, and their z and w.  KEEP: a sequence's first row has its h for a z (its
-// state before is read once only: the CTA with the sequence's end may write the state after it to the
-// same place as soon as this part has left its B).
-template <class T, int V, bool KEEP>
-__device__ __forceinline__ bool rows_forward(const GsArgs& a, const Part& t, const Marks& m, const uint8_t* raw, int c,
-                                             bool in, float (&z)[RPW][V], float (&w)[RPW][V], float2 (&f)[V]) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  bool has = false;
+// A and B of the warp's rows; of each row w and z n (KEEP_Z: z).  At a sequence's first
+// row z n is its h: the state before is read once only, since the CTA with the sequence's end may write
+// the state after it to the same place as soon as this part has left its B.
+// (Rows of no sequence are computed with: none of a sequence's comes after them without its first.)
+template <class L, bool KEEP_Z>
+__device__ __forceinline__ void rows_forward(const GsArgs& a, const Part& t, const Marks& m, const Mine& my, uint32_t at,
+                                             int step, int c, bool in, typename L::P (&z)[RPW], typename L::P (&w)[RPW],
+                                             typename L::P& fa, typename L::P& fb) {
+  using P = typename L::P;
+  fa = L::make(1.0f, 1.0f), fb = L::make(0.0f, 0.0f);
 #pragma unroll
-  for (int v = 0; v < V; ++v) f[v] = make_float2(1.0f, 0.0f);
-#pragma unroll
-  for (int i = 0; i < RPW; ++i) {
-    const int d = row_in(a, t, warp * RPW + i);
-    if (d < t.lo || d >= t.hi) continue;
-    const bool begins = bound(m, a.reverse ? d + 1 : d);
+  for (int i = 0; i < RPW; ++i, at += step) {
+    const P p = L::get(at), n = L::get(at + PIECE);
+    const bool begins = (my.begins >> i) & 1u;
+    L::gates(p, z[i], w[i]);
+    const P x = L::mul(z[i], n);
     if (begins) {
-      has = true;
-      float s0[V] = {};
-      if (a.state_in && in) get_state<V>(a.state_in + sequence(a, m, d, !a.reverse) * a.C + c, s0);
-#pragma unroll
-      for (int v = 0; v < V; ++v) f[v] = make_float2(0.0f, s0[v]);
+      fb = L::make(0.0f, 0.0f);
+      if (a.state_in && in)
+        fb = get_state<L>(a.state_in + sequence(a, m, row_in(a, t, (threadIdx.x >> 5) * RPW + i), !a.reverse) * a.C + c);
     }
-    float p[V], n[V];
-    Lane<T>::get(raw + d * 128 + 4 * lane, p);
-    Lane<T>::get(raw + PIECE + d * 128 + 4 * lane, n);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      gate(p[v], z[i][v], w[i][v]);
-      f[v].x *= w[i][v];
-      f[v].y = fmaf(w[i][v], f[v].y, z[i][v] * n[v]);
-      if (KEEP && begins) z[i][v] = f[v].y;
-    }
+    fa = L::mul(fa, w[i]);
+    fb = L::fma(w[i], fb, x);
+    if constexpr (!KEEP_Z) z[i] = L::pick(begins, fb, x);
   }
-  return has;
 }
 
-template <class T, int WIN, bool ALONE>
+template <class T, bool ALONE>
 __global__ void __launch_bounds__(NT, CTAS) scan_kernel(const __grid_constant__ GsArgs a) {
-  constexpr int V = Lane<T>::V, WIDE = 32 * V;
-  extern __shared__ __align__(128) uint8_t smem[];
-  Shared<V, WIN>* s = reinterpret_cast<Shared<V, WIN>*>(smem + 4 * PIECE);
+  using L = Lane<T>;
+  using P = typename L::P;
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  Shared<L>* s = reinterpret_cast<Shared<L>*>(smem_raw);
+  uint8_t* smem = smem_raw + SHARED<L>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // sequences of no rows: what is before them is what is after them
   if (a.state_out)
@@ -472,7 +568,7 @@ __global__ void __launch_bounds__(NT, CTAS) scan_kernel(const __grid_constant__ 
     return;
   }
   volatile int* abort = &s->abort;
-  float carry[V] = {};
+  P carry = L::make(0.0f, 0.0f);
   bool ok = true;
   for (int n = 0;; ++n) {
     const int buf = n & 1;
@@ -482,71 +578,41 @@ __global__ void __launch_bounds__(NT, CTAS) scan_kernel(const __grid_constant__ 
     ok = __all_sync(FULL, sm100::mbar_wait(smem_addr(&s->full[buf]), (n >> 1) & 1, abort, a.limit_ns));
     if (!ok) break;
     const int64_t k = b.k;
-    const int c = b.c0 + lane * V;
-    const bool in = c < a.C;
+    const int c = b.c0 + lane * L::V;
+    const bool in = c < a.C, pass = ALONE && b.kind == PASS;
     const Part t = part_of(a, s, k);
     const Marks& m = b.marks;
-    const uint8_t* raw = smem + buf * 2 * PIECE;
-    float z[RPW][V], w[RPW][V];
-    float2 f[V];
-    const bool has = rows_forward<T, V, true>(a, t, m, raw, c, in, z, w, f);
-#pragma unroll
-    for (int v = 0; v < V; ++v) s->agg[warp][lane * V + v] = f[v];
-    if (lane == 0) s->has[warp] = has;
+    const Mine my = mine_of(a, t, m, warp);
+    const int d0 = row_in(a, t, warp * RPW), dir = a.reverse ? -1 : 1;
+    const uint32_t at = smem_addr(smem + buf * 2 * PIECE) + (my.valid ? d0 * 128 + lane * 4 : 0);
+    P x[RPW], w[RPW], fa, fb;
+    rows_forward<L, false>(a, t, m, my, at, my.valid ? 128 * dir : 0, c, in, x, w, fa, fb);
+    s->agg_a[warp][lane] = fa, s->agg_b[warp][lane] = fb;
+    if (lane == 0) s->has[warp] = my.begins != 0;
     meet();
-    if constexpr (ALONE) {
-      if (b.kind == PASS) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          bool h;
-          const float2 g = joined<false>(s, lane * V + v, h);
-          carry[v] = through(h, g, carry[v]);
-        }
-        __syncwarp();
-        if (lane == 0) sm100::mbar_arrive(smem_addr(&s->empty[buf]));
-        meet();
-        continue;
-      }
-    } else {
-      // what is before this part counts if its first position is a row within a sequence
-      const int d0 = row_in(a, t, 0);
-      const bool inside = d0 >= t.lo && d0 < t.hi && !bound(m, a.reverse ? d0 + 1 : d0);
-      if (warp == 0 && in) leave_part<false>(a, s, k, c, lane);
-#pragma unroll
-      for (int v = 0; v < V; ++v) carry[v] = 0.0f;
-      if (inside) {
-        if (!look_back<false, V, WIN>(a, s, k, c, in, carry)) {
-          ok = false;
-          break;
-        }
-        if (warp == 0 && in) leave_whole<false>(a, s, k, c, lane, carry);
-      }
+    if (pass) {
+      bool has;
+      joined<L, false>(s, lane, fa, fb, has);
+      carry = L::pick(has, fb, L::fma(fa, carry, fb));
+      release(s, buf, lane);
+      meet();
+      continue;
     }
-    if (a.saved && warp == 0 && in) put_state<V>(a.saved + k * a.C + c, carry);
-    float h[V];
+    ok = carry_into<L, false, ALONE>(a, s, k, c, in, t, m, carry);
+    if (!ok) break;
+    if (a.saved && warp == 0 && in) put_state<L>(a.saved + k * a.C + c, carry);
+    P h = carry;
+    for (int u = 0; u < warp; ++u) h = L::pick(s->has[u], s->agg_b[u][lane], L::fma(s->agg_a[u][lane], h, s->agg_b[u][lane]));
+    const uint32_t put = in ? my.valid : 0u, ends = in && a.state_out ? my.ends : 0u;
+    T* out = (T*)a.out + (t.row0 + d0) * a.os + c;
+    const int64_t step = dir * a.os;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      h[v] = carry[v];
-      for (int u = 0; u < warp; ++u) h[v] = through(s->has[u], s->agg[u][lane * V + v], h[v]);
+    for (int i = 0; i < RPW; ++i, out += step) {
+      h = L::pick((my.begins >> i) & 1u, x[i], L::fma(w[i], h, x[i]));
+      if ((put >> i) & 1u) L::put(out, h);
+      if ((ends >> i) & 1u) put_state<L>(a.state_out + sequence(a, m, row_in(a, t, warp * RPW + i), a.reverse) * a.C + c, h);
     }
-    T* out = (T*)a.out + c;
-#pragma unroll
-    for (int i = 0; i < RPW; ++i) {
-      const int d = row_in(a, t, warp * RPW + i);
-      const int64_t row = t.row0 + d;
-      if (d < t.lo || d >= t.hi) continue;
-      const bool begins = bound(m, a.reverse ? d + 1 : d);
-      float n[V];
-      Lane<T>::get(raw + PIECE + d * 128 + 4 * lane, n);
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = begins ? z[i][v] : fmaf(w[i][v], h[v], z[i][v] * n[v]);
-      if (in) {
-        Lane<T>::put(out + row * a.os, h);
-        if (a.state_out && bound(m, a.reverse ? d : d + 1)) put_state<V>(a.state_out + sequence(a, m, d, a.reverse) * a.C + c, h);
-      }
-    }
-    __syncwarp();
-    if (lane == 0) sm100::mbar_arrive(smem_addr(&s->empty[buf]));
+    release(s, buf, lane);
     meet();
   }
   if (!ok && lane == 0 && atomicExch(&s->abort, 1) == 0) atomicAdd(a.expired, 1ull);
@@ -554,13 +620,15 @@ __global__ void __launch_bounds__(NT, CTAS) scan_kernel(const __grid_constant__ 
 
 // ---------------------------------------------------------------- backward
 
-template <class T, int WIN, bool ALONE>
+template <class T, bool ALONE>
 __global__ void __launch_bounds__(NT, CTAS) backward_kernel(const __grid_constant__ GsArgs a) {
-  constexpr int V = Lane<T>::V, WIDE = 32 * V;
-  extern __shared__ __align__(128) uint8_t smem[];
-  Shared<V, WIN>* s = reinterpret_cast<Shared<V, WIN>*>(smem + 6 * PIECE);
+  using L = Lane<T>;
+  using P = typename L::P;
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  Shared<L>* s = reinterpret_cast<Shared<L>*>(smem_raw);
+  uint8_t* smem = smem_raw + SHARED<L>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // sequences of no rows: what is before them is what is after them
+  // sequences of no rows: what is behind them is what is before them
   if (a.d_state_in)
     for (int64_t b = (int64_t)blockIdx.x * (WARPS + 1) + warp; b < a.n_seq; b += (int64_t)gridDim.x * (WARPS + 1))
       if (a.offs[b] >= a.offs[b + 1])
@@ -572,7 +640,7 @@ __global__ void __launch_bounds__(NT, CTAS) backward_kernel(const __grid_constan
     return;
   }
   volatile int* abort = &s->abort;
-  float carry[V] = {};
+  P carry = L::make(0.0f, 0.0f);
   bool ok = true;
   for (int n = 0;; ++n) {
     const int buf = n & 1;
@@ -582,136 +650,105 @@ __global__ void __launch_bounds__(NT, CTAS) backward_kernel(const __grid_constan
     ok = __all_sync(FULL, sm100::mbar_wait(smem_addr(&s->full[buf]), (n >> 1) & 1, abort, a.limit_ns));
     if (!ok) break;
     const int64_t k = b.k;
-    const int c = b.c0 + lane * V;
-    const bool in = c < a.C;
+    const int c = b.c0 + lane * L::V;
+    const bool in = c < a.C, pass = ALONE && b.kind == PASS;
     const Part t = part_of(a, s, k);
     const Marks& m = b.marks;
-    uint8_t* raw = smem + buf * 3 * PIECE;
-    float z[RPW][V], w[RPW][V];
+    const Mine my = mine_of(a, t, m, warp);
+    const int d0 = row_in(a, t, warp * RPW), dir = a.reverse ? -1 : 1;
+    const uint32_t at0 = smem_addr(smem + buf * 3 * PIECE) + (my.valid ? d0 * 128 + lane * 4 : 0);
+    const int step0 = my.valid ? 128 * dir : 0;
+    P z[RPW], w[RPW], fa, fb;
     {
       // the states again, from the one saved before the part
-      float2 f[V];
-      const bool has = rows_forward<T, V, false>(a, t, m, raw, c, in, z, w, f);
-#pragma unroll
-      for (int v = 0; v < V; ++v) s->agg[warp][lane * V + v] = f[v];
-      if (lane == 0) s->has[warp] = has;
+      rows_forward<L, true>(a, t, m, my, at0, step0, c, in, z, w, fa, fb);
+      s->agg_a[warp][lane] = fa, s->agg_b[warp][lane] = fb;
+      if (lane == 0) s->has[warp] = my.begins != 0;
+      P h = L::make(0.0f, 0.0f);
+      if (in) h = get_state<L>(a.saved + k * a.C + c);
       meet();
-      float h[V] = {};
-      if (in) get_state<V>(a.saved + k * a.C + c, h);
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        for (int u = 0; u < warp; ++u) h[v] = through(s->has[u], s->agg[u][lane * V + v], h[v]);
+      for (int u = 0; u < warp; ++u) h = L::pick(s->has[u], s->agg_b[u][lane], L::fma(s->agg_a[u][lane], h, s->agg_b[u][lane]));
       // z w (n - h) takes the place of p and n, 4 bytes a channel
+      uint32_t at = at0;
+      if (my.valid) {
 #pragma unroll
-      for (int i = 0; i < RPW; ++i) {
-        const int d = row_in(a, t, warp * RPW + i);
-        if (d < t.lo || d >= t.hi) continue;
-        if (bound(m, a.reverse ? d + 1 : d)) {
-#pragma unroll
-          for (int v = 0; v < V; ++v) h[v] = 0.0f;
-          if (a.state_in && in) get_state<V>(a.state_in + sequence(a, m, d, !a.reverse) * a.C + c, h);
-        }
-        float n[V];
-        uint8_t* at = raw + d * 128 + 4 * lane;
-        Lane<T>::get(at + PIECE, n);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          *reinterpret_cast<float*>(at + v * PIECE) = z[i][v] * w[i][v] * (n[v] - h[v]);
-          h[v] = fmaf(w[i][v], h[v], z[i][v] * n[v]);
+        for (int i = 0; i < RPW; ++i, at += step0) {
+          const P n = L::get(at + PIECE);
+          if ((my.begins >> i) & 1u) {
+            h = L::make(0.0f, 0.0f);
+            if (a.state_in && in)
+              h = get_state<L>(a.state_in + sequence(a, m, row_in(a, t, warp * RPW + i), !a.reverse) * a.C + c);
+          }
+          const P q = L::mul(L::mul(z[i], w[i]), L::sub(n, h));
+          h = L::fma(w[i], h, L::mul(z[i], n));
+          if ((my.valid >> i) & 1u) {
+            sts(at, L::part(q, 0));
+            if constexpr (L::V == 2) sts(at + PIECE, L::part(q, 1));
+          }
         }
       }
       meet();
     }
     // what comes from behind: e before the warp's rows = A e after them + B.  A sequence's last row gets
     // its results here: what its state's gradient is may be written over once this part has left its B.
-    bool has = false;
-    float2 f[V];
+    fa = L::make(1.0f, 1.0f), fb = L::make(0.0f, 0.0f);
+    if (my.valid) {
+      uint32_t at = at0 + (RPW - 1) * step0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) f[v] = make_float2(1.0f, 0.0f);
-#pragma unroll
-    for (int i = RPW - 1; i >= 0; --i) {
-      const int d = row_in(a, t, warp * RPW + i);
-      if (d < t.lo || d >= t.hi) continue;
-      const bool ends = bound(m, a.reverse ? d : d + 1);
-      if (ends) {
-        has = true;
-        float e[V] = {};
-        if (a.d_state_out && in) get_state<V>(a.d_state_out + sequence(a, m, d, a.reverse) * a.C + c, e);
-#pragma unroll
-        for (int v = 0; v < V; ++v) f[v] = make_float2(0.0f, e[v]);
-      }
-      float g[V];
-      uint8_t* at = raw + d * 128 + 4 * lane;
-      Lane<T>::get(at + 2 * PIECE, g);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float D = g[v] + f[v].y;
-        f[v].x *= w[i][v], f[v].y = w[i][v] * D;
-        if (ends) z[i][v] *= D, w[i][v] = f[v].y, *reinterpret_cast<float*>(at + v * PIECE) *= D;
+      for (int i = RPW - 1; i >= 0; --i, at -= step0) {
+        if (!((my.valid >> i) & 1u)) continue;
+        const bool ends = (my.ends >> i) & 1u;
+        if (ends) {
+          fb = L::make(0.0f, 0.0f);
+          if (a.d_state_out && in)
+            fb = get_state<L>(a.d_state_out + sequence(a, m, row_in(a, t, warp * RPW + i), a.reverse) * a.C + c);
+        }
+        const P D = L::add(L::get(at + 2 * PIECE), fb);
+        fa = L::mul(fa, w[i]), fb = L::mul(w[i], D);
+        if (ends) {
+          z[i] = L::mul(z[i], D), w[i] = fb;
+          sts(at, lds(at) * L::part(D, 0));
+          if constexpr (L::V == 2) sts(at + PIECE, lds(at + PIECE) * L::part(D, 1));
+        }
       }
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) s->agg[warp][lane * V + v] = f[v];
-    if (lane == 0) s->has[warp] = has;
+    s->agg_a[warp][lane] = fa, s->agg_b[warp][lane] = fb;
+    if (lane == 0) s->has[warp] = my.ends != 0;
     meet();
-    if constexpr (ALONE) {
-      if (b.kind == PASS) {
+    if (pass) {
+      bool has;
+      joined<L, true>(s, lane, fa, fb, has);
+      carry = L::pick(has, fb, L::fma(fa, carry, fb));
+      release(s, buf, lane);
+      meet();
+      continue;
+    }
+    ok = carry_into<L, true, ALONE>(a, s, k, c, in, t, m, carry);
+    if (!ok) break;
+    P e = carry;
+    for (int u = WARPS - 1; u > warp; --u)
+      e = L::pick(s->has[u], s->agg_b[u][lane], L::fma(s->agg_a[u][lane], e, s->agg_b[u][lane]));
+    const uint32_t put = in ? my.valid : 0u, begins = in && a.d_state_in ? my.begins : 0u;
+    const int64_t step1 = dir * a.dps, step2 = dir * a.dns;
+    T* dp = (T*)a.dp + (t.row0 + d0) * a.dps + (RPW - 1) * step1 + c;
+    T* dn = (T*)a.dn + (t.row0 + d0) * a.dns + (RPW - 1) * step2 + c;
+    if (my.valid) {
+      uint32_t at = at0 + (RPW - 1) * step0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          bool h;
-          const float2 g = joined<true>(s, lane * V + v, h);
-          carry[v] = through(h, g, carry[v]);
+      for (int i = RPW - 1; i >= 0; --i, at -= step0, dp -= step1, dn -= step2) {
+        if (!((my.valid >> i) & 1u)) continue;
+        const P D = L::pick((my.ends >> i) & 1u, L::make(1.0f, 1.0f), L::add(L::get(at + 2 * PIECE), e));
+        const P q = L::make(lds(at), L::V == 2 ? lds(at + PIECE) : 0.0f);
+        e = L::mul(w[i], D);
+        if ((put >> i) & 1u) {
+          L::put(dp, L::mul(q, D));
+          L::put(dn, L::mul(z[i], D));
         }
-        __syncwarp();
-        if (lane == 0) sm100::mbar_arrive(smem_addr(&s->empty[buf]));
-        meet();
-        continue;
-      }
-    } else {
-      const int d1 = row_in(a, t, t.count - 1);
-      const bool inside = d1 >= t.lo && d1 < t.hi && !bound(m, a.reverse ? d1 : d1 + 1);
-      if (warp == 0 && in) leave_part<true>(a, s, k, c, lane);
-#pragma unroll
-      for (int v = 0; v < V; ++v) carry[v] = 0.0f;
-      if (inside) {
-        if (!look_back<true, V, WIN>(a, s, k, c, in, carry)) {
-          ok = false;
-          break;
-        }
-        if (warp == 0 && in) leave_whole<true>(a, s, k, c, lane, carry);
+        if ((begins >> i) & 1u)
+          put_state<L>(a.d_state_in + sequence(a, m, row_in(a, t, warp * RPW + i), !a.reverse) * a.C + c, e);
       }
     }
-    float e[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      e[v] = carry[v];
-      for (int u = WARPS - 1; u > warp; --u) e[v] = through(s->has[u], s->agg[u][lane * V + v], e[v]);
-    }
-    T *dp = (T*)a.dp + c, *dn = (T*)a.dn + c;
-#pragma unroll
-    for (int i = RPW - 1; i >= 0; --i) {
-      const int d = row_in(a, t, warp * RPW + i);
-      const int64_t row = t.row0 + d;
-      if (d < t.lo || d >= t.hi) continue;
-      const bool ends = bound(m, a.reverse ? d : d + 1);
-      float g[V], x[V], y[V];
-      const uint8_t* at = raw + d * 128 + 4 * lane;
-      Lane<T>::get(at + 2 * PIECE, g);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float D = ends ? 1.0f : g[v] + e[v];
-        x[v] = *reinterpret_cast<const float*>(at + v * PIECE) * D;
-        y[v] = z[i][v] * D;
-        e[v] = w[i][v] * D;
-      }
-      if (in) {
-        Lane<T>::put(dp + row * a.dps, x);
-        Lane<T>::put(dn + row * a.dns, y);
-        if (a.d_state_in && bound(m, a.reverse ? d + 1 : d)) put_state<V>(a.d_state_in + sequence(a, m, d, !a.reverse) * a.C + c, e);
-      }
-    }
-    __syncwarp();
-    if (lane == 0) sm100::mbar_arrive(smem_addr(&s->empty[buf]));
+    release(s, buf, lane);
     meet();
   }
   if (!ok && lane == 0 && atomicExch(&s->abort, 1) == 0) atomicAdd(a.expired, 1ull);
@@ -841,10 +878,10 @@ int check(const Call& f, const GsArgs& a) {
 
 template <class T, bool BACK, bool ALONE>
 int launch(const Call& f, GsArgs& a, cudaStream_t st) {
-  constexpr int V = Lane<T>::V, WIN = BACK && V == 2 ? 16 : 32;
+  constexpr int V = Lane<T>::V;
   constexpr auto kern = [] {
-    if constexpr (BACK) return &backward_kernel<T, WIN, ALONE>;
-    else return &scan_kernel<T, WIN, ALONE>;
+    if constexpr (BACK) return &backward_kernel<T, ALONE>;
+    else return &scan_kernel<T, ALONE>;
   }();
   a.parts = (a.n_rows + TILE - 1) / TILE, a.blocks = (a.C + 32 * V - 1) / (32 * V);
   a.limit_ns = operator_limit_ns(), a.expired = operator_expired();
@@ -852,7 +889,7 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
   if (a.n_rows > 0 && (!make_map(&a.tp, f.dtype, f.p, a.n_rows, a.C, f.ps) || !make_map(&a.tn, f.dtype, f.n, a.n_rows, a.C, f.ns) ||
                        (BACK && !make_map(&a.tg, f.dtype, f.g, a.n_rows, a.C, f.gs))))
     return TRACKFIT_ERR_CUDA;
-  const size_t smem = (BACK ? 6 : 4) * PIECE + sizeof(Shared<V, WIN>);
+  const size_t smem = (BACK ? 6 : 4) * PIECE + SHARED<Lane<T>>;
   const cudaError_t e = allow_smem<kern>(smem);
   if (e != cudaSuccess) return tf_status_from_cuda(e);
   int64_t grid = a.parts * a.blocks;
