@@ -518,8 +518,8 @@ int trackfit_gated_scan(int32_t dtype, const void* gate, int64_t gate_stride, co
  *   D_t = g_t + (1 - z_{t+1}) D_{t+1},  dn_t = z_t D_t,  dp_t = z_t (1 - z_t) (n_t - h_{t-1}) D_t
  *   gate, cand, offsets, reverse, state_in   as they were in the forward call (state_in's
  *               values too: a call whose state_out was state_in keeps a copy for this one).
- *   saved       what the forward call wrote there (the states at every 128 rows; those in
- *               between are formed again).
+ *   saved       what the forward call wrote there (a state of every 128 rows or fewer; those
+ *               in between are formed again).
  *   d_out       g, [n_rows][channels].
  *   d_state_out fp32 [n_seq][channels], the gradients of state_out, or NULL (zeros).
  *   d_state_in  the same shape, the gradients of state_in, or NULL; may be d_state_out.
