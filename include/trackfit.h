@@ -504,8 +504,8 @@ int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, con
  *               before it), or NULL; may be state_in.
  *   saved       trackfit_gated_scan_saved() bytes, 16-byte aligned, for
  *               trackfit_gated_scan_backward, or NULL.
- *   workspace   trackfit_gated_scan_workspace() bytes, 16-byte aligned (the parts of the rows
- *               are joined through it; NULL when that is 0).
+ *   workspace   trackfit_gated_scan_workspace() bytes, 16-byte aligned (sequences of more than 32
+ *               rows on average are cut and their parts joined through it; NULL when that is 0).
  * z and 1 - z are both off by (2 |p| + 10) 2^-24 of themselves at most, however near to 0. */
 size_t trackfit_gated_scan_saved(int64_t n_rows, int32_t channels);
 size_t trackfit_gated_scan_workspace(int32_t dtype, int64_t n_rows, int64_t n_seq, int32_t channels);
@@ -518,8 +518,8 @@ int trackfit_gated_scan(int32_t dtype, const void* gate, int64_t gate_stride, co
  *   D_t = g_t + (1 - z_{t+1}) D_{t+1},  dn_t = z_t D_t,  dp_t = z_t (1 - z_t) (n_t - h_{t-1}) D_t
  *   gate, cand, offsets, reverse, state_in   as they were in the forward call (state_in's
  *               values too: a call whose state_out was state_in keeps a copy for this one).
- *   saved       what the forward call wrote there (a state of every 128 rows or fewer; those
- *               in between are formed again).
+ *   saved       what the forward call wrote there (a state of every 32 rows; those in between
+ *               are formed again).
  *   d_out       g, [n_rows][channels].
  *   d_state_out fp32 [n_seq][channels], the gradients of state_out, or NULL (zeros).
  *   d_state_in  the same shape, the gradients of state_in, or NULL; may be d_state_out.

@@ -64,10 +64,11 @@ def test_scan_backward_refusals(lib, kw, want):
 def test_scan_sizes(lib):
     saved, ws = lib.trackfit_gated_scan_saved, lib.trackfit_gated_scan_workspace
     assert saved(0, 64) == 0 and saved(-1, 64) == 0 and saved(100, 12) == 0
-    assert saved(1, 64) == 64 * 4 and saved(100, 8) == 8 * 4 and 2 * 8 * 4 <= saved(129, 8) <= 4 * 8 * 4
+    assert saved(1, 64) == 64 * 4 and saved(32, 8) == 8 * 4 and saved(33, 8) == 2 * 8 * 4
     assert 4 * T.gated_scan_saved(1000, 24) == saved(1000, 24) >= 8 * 24 * 4
     for bad in ((5, 100, 1, 64), (1, -1, 1, 64), (1, 100, -1, 64), (1, 100, 1, 60)):
         assert ws(*bad) == 0
+    assert ws(1, 640, 20, 64) == 0 and ws(1, 641, 20, 64) > 0
     for t in range(3):
         n = ws(t, 100000, 3, 64)
         assert ws(t, 0, 3, 64) == 0 and ws(t, 200000, 3, 64) >= n
