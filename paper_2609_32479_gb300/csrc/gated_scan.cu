@@ -5,17 +5,16 @@
 //   D_t = g_t + e_t,  e_{t-1} = w_t D_t,  dn = z D,  dp = z w (n - h_{t-1}) D
 //
 // Bound by memory: three values a row and channel are moved forward, five backward.  A warp takes
-// windows of 32 rows x 128 bytes of channels, one row after the other; a lane has one channel (16
-// bits: two neighbouring ones, in instructions that take two).  All of a window's loads are under way
-// together; no warp waits for another.
+// windows of 32 rows x 128 bytes of channels, brought by TMA, one row after the other; a lane has one channel (16
+// bits: two neighbouring ones, in instructions that take two).  No warp waits for another.
 //
 // Short sequences (32 rows on average at most): a warp takes the sequences that begin in its rows, as
 // far as they reach, so that it begins with a state that it knows.
 //
 // Long ones: what stands before a run of rows acts on it through one number a channel,
 // h_last = A h_before + B with A the product of the w.  A first kernel forms (A, B) of all windows
-// from the first row of their segment (a CTA's 16 warps' rows) on, a second the states before the
-// segments, one after the other; then every window's first state is two loads and one multiply-add
+// from the first row of their segment (a CTA's rows) on, a second the states before the
+// segments, one after the other; then every window's first state is a few loads and multiply-adds
 // away.  So p and n are read twice.  (One pass, in which parts of 128 rows wait for what the part before
 // leaves them, moves less, but was slower: with 128 rows under way in a CTA, a row's few instructions
 // and the look back at other CTAs' results take longer than the rows' transfer; 5 sequences of up to
@@ -29,12 +28,15 @@
 
 #include <cudaTypedefs.h>
 
+#include <utility>
+
 namespace {
 using namespace seqops;
 
 constexpr int WINDOW = 32;                 // positions, and from one saved state to the next
-constexpr int SEG_WARPS = 16;              // of a segment
-constexpr int ROW_WARPS = 4, BACK_WARPS = 4;
+constexpr int GROUP = 8;                   // rows whose gates are formed side by side
+constexpr int WARPS = 8;                   // of a CTA, forward; of a segment
+constexpr int BACK_WARPS = 4;
 constexpr int MAX_CHANNELS = 1 << 16;
 constexpr int SHORT = 32;                  // rows of a sequence on average
 constexpr uint64_t LOAD_NS = 2000000000ull;
@@ -47,7 +49,7 @@ struct Order {
 
 struct GsArgs {
   const void *p, *n, *g;
-  CUtensorMap tp, tn, tg;                  // backward: boxes of 128 bytes x 32 rows
+  CUtensorMap tp, tn, tg;                  // boxes of 128 bytes x 32 rows
   void *out, *dp, *dn;
   int64_t ps, ns, gs, os, dps, dns;        // row strides in elements
   const int64_t* offs;
@@ -59,10 +61,10 @@ struct GsArgs {
   float* saved;                            // [windows][C]: the state before a window
   int64_t windows, segments;
   int each, chunk;                         // windows of a segment's warp; positions whose sequences a warp takes
-  // long sequences: by window, what comes before it in its segment; by segment, all of it and the state
-  // before it
-  float *win_a, *win_b, *seg_a, *seg_b, *seg_s;
-  uint32_t *win_has, *seg_has;
+  // long sequences: by window, what comes before it in its warp's windows; by warp, what comes before it in
+  // its segment; by segment, all of it and the state before it
+  float *win_a, *win_b, *warp_a, *warp_b, *seg_a, *seg_b, *seg_s;
+  uint32_t *win_has, *warp_has, *seg_has;
   unsigned long long* expired;
 };
 
@@ -166,36 +168,42 @@ __device__ __forceinline__ int64_t border_at(const GsArgs& a, const Order& o, in
   return lo;
 }
 
-// The sequences among a window's positions: bit i for the i-th.
-struct Marks {
-  int64_t pos;                             // the first position
+// A window: up to 32 positions, all rows of sequences, and the sequences among them, bit i for the i-th.
+struct Window {
+  int64_t pos;
+  int count;
   int64_t first;                           // the first border at or behind it
-  uint32_t valid, begins, ends;            // rows of sequences, first rows, last rows
+  uint32_t begins, ends;                   // first rows, last rows
 };
-// Given the first border's number: a whole warp.
-__device__ __forceinline__ Marks marks_of(const GsArgs& a, const Order& o, int64_t pos, int64_t first, int lane) {
-  Marks m;
-  m.pos = pos, m.first = first;
+// From `pos` on, in [lo, hi), given the first border's number; `after` gets that of the next window's.  A whole warp.
+__device__ __forceinline__ Window window_at(const GsArgs& a, const Order& o, int64_t pos, int64_t lo, int64_t hi, int64_t first,
+                                            int lane, int64_t& after) {
+  Window m;
+  m.pos = pos < lo ? lo : pos;
+  m.count = (int)clamp64((pos + WINDOW < hi ? pos + WINDOW : hi) - m.pos, 0, WINDOW);
+  m.first = after = first;
   uint32_t bits = 0, last = 0;
-  for (int64_t i = first;; i += 32) {
-    const int64_t d = i + lane <= a.n_seq ? border(a, o, i + lane) - pos : INT64_MAX;
+  for (;;) {
+    const int64_t b = after + lane <= a.n_seq ? border(a, o, after + lane) - m.pos : INT64_MAX;
+    const int d = b > WINDOW ? WINDOW + 1 : b < 0 ? -1 : (int)b;
     bits |= __reduce_or_sync(FULL, d >= 0 && d < WINDOW ? 1u << d : 0u);
     last |= __any_sync(FULL, d == WINDOW) ? 1u : 0u;
-    if (__any_sync(FULL, d > WINDOW)) break;
+    const int n = __popc(__ballot_sync(FULL, b < pos + WINDOW - m.pos));
+    after += n;
+    if (n < 32) break;
   }
-  const int64_t lo = border(a, o, 0) - pos, hi = border(a, o, a.n_seq) - pos;
-  m.valid = (hi <= 0 ? 0u : hi >= WINDOW ? FULL : (1u << hi) - 1u) & (lo <= 0 ? FULL : lo >= WINDOW ? 0u : FULL << lo);
-  const int64_t r0 = row_of(o, pos), r1 = row_of(o, pos + WINDOW - 1);   // (offsets that break the rules: no row beyond the array)
-  if ((r0 < r1 ? r0 : r1) < 0 || (r0 < r1 ? r1 : r0) >= a.n_rows) {
-    const int64_t p0 = o.back ? o.t + 1 - a.n_rows : o.t, q0 = p0 - pos, q1 = p0 + a.n_rows - pos;
-    m.valid &= (q1 <= 0 ? 0u : q1 >= WINDOW ? FULL : (1u << q1) - 1u) & (q0 <= 0 ? FULL : q0 >= WINDOW ? 0u : FULL << q0);
-  }
-  m.begins = bits & m.valid, m.ends = (bits >> 1 | last << 31) & m.valid;
+  const uint32_t valid = m.count >= 32 ? FULL : (1u << m.count) - 1u;
+  m.begins = bits & valid, m.ends = (bits >> 1 | last << 31) & valid;
   return m;
+}
+// The positions that are rows of sequences (and, whatever the offsets say, of the array).
+__device__ __forceinline__ void extent(const GsArgs& a, const Order& o, int64_t& lo, int64_t& hi) {
+  const int64_t p0 = o.back ? o.t + 1 - a.n_rows : o.t;
+  lo = clamp64(border(a, o, 0), p0, p0 + a.n_rows), hi = clamp64(border(a, o, a.n_seq), lo, p0 + a.n_rows);
 }
 // The sequence that begins with position i of the window (or, `ends`, ends with it): the last border there,
 // or the one before the first behind it.  A whole warp.
-__device__ __noinline__ int64_t sequence(const GsArgs& a, const Order& o, const Marks& m, int i, bool ends) {
+__device__ __noinline__ int64_t sequence(const GsArgs& a, const Order& o, const Window& m, int i, bool ends) {
   const int64_t pos = m.pos + i + (ends ? 1 : 0);
   int64_t j = m.first;
   for (int64_t at = m.first;; at += 32) {
@@ -206,31 +214,50 @@ __device__ __noinline__ int64_t sequence(const GsArgs& a, const Order& o, const 
   }
   return sequence_of(a, o, j - 1);
 }
-
-// A window's words of an array (a lane's 4 bytes of each row), loads under way together.
-template <class T>
-__device__ __forceinline__ void load(const GsArgs& a, const Order& o, const Marks& m, const void* from, int64_t stride, int c,
-                                     bool in, uint32_t (&x)[WINDOW]) {
-  const uint8_t* at = (const uint8_t*)from + (row_of(o, m.pos) * stride + c) * (int64_t)sizeof(T);
-  const int64_t step = (o.back ? -stride : stride) * (int64_t)sizeof(T);
-  const uint32_t mask = in ? m.valid : 0u;
-#pragma unroll
-  for (int i = 0; i < WINDOW; ++i, at += step) {
-    x[i] = 0;
-    if ((mask >> i) & 1u) x[i] = __ldg(reinterpret_cast<const uint32_t*>(at));
-  }
-}
-
-// What is before a row that is a sequence's first: the state given, or zeros.  A whole warp.
+// What is before position i, a sequence's first (`ends`: behind its last): the state given, or zeros.  A whole warp.
 template <class L>
-__device__ __forceinline__ typename L::P given(const GsArgs& a, const Order& o, const Marks& m, int i, const float* states,
-                                               int c, bool in) {
+__device__ __forceinline__ typename L::P given(const GsArgs& a, const Order& o, const Window& m, int i, bool ends,
+                                               const float* states, int c, bool in) {
   typename L::P h = L::make(0.0f, 0.0f);
   if (states) {
-    const int64_t b = sequence(a, o, m, i, false);
+    const int64_t b = sequence(a, o, m, i, ends);
     if (in) h = get_state<L>(states + b * a.C + c);
   }
   return h;
+}
+
+// A warp's buffer for a window: 32 rows of 128 bytes of each array, brought by one lane.
+constexpr int BLOCK = WINDOW * 128;
+template <int ARRAYS>
+__device__ __forceinline__ void bring(uint32_t to, uint32_t full, const Order& o, int64_t pos, int c, const CUtensorMap* x,
+                                      const CUtensorMap* y, const CUtensorMap* z) {
+  sm100::fence_proxy_async_smem();         // (what was written into the buffer, before the copy into it)
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) {
+    const int r0 = (int)row_of(o, o.back ? pos + WINDOW - 1 : pos);   // the lowest row (it may be below the array)
+    sm100::mbar_arrive_expect_tx(full, ARRAYS * BLOCK);
+    sm100::tma_load_2d(to, x, full, c, r0);
+    sm100::tma_load_2d(to + BLOCK, y, full, c, r0);
+    if constexpr (ARRAYS == 3) sm100::tma_load_2d(to + 2 * BLOCK, z, full, c, r0);
+  }
+}
+__device__ __forceinline__ bool brought(uint32_t full, uint32_t parity) {
+  int never = 0;
+  return __all_sync(FULL, sm100::mbar_wait(full, parity, &never, LOAD_NS));
+}
+__device__ __forceinline__ uint32_t lds(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ void sts(uint32_t at, float x) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory"); }
+// A lane's word of position i in a buffer is at `at` + i `step`.
+struct Walk {
+  uint32_t at;
+  int step;
+};
+__device__ __forceinline__ Walk walk_of(const Order& o, uint32_t buffer) {
+  return {buffer + 4 * (threadIdx.x & 31) + (o.back ? (WINDOW - 1) * 128 : 0), o.back ? -128 : 128};
 }
 
 // Sequences of no rows: what is before them is what is after them.
@@ -246,79 +273,92 @@ __device__ __forceinline__ void empty_sequences(const GsArgs& a, float* to, cons
 
 // (A, B) of the windows: of h, or (BACK) of e in the flipped order, where B = w (g + B).
 template <class T, bool BACK>
-__global__ void __launch_bounds__(SEG_WARPS * 32) sums_kernel(const __grid_constant__ GsArgs a) {
+__global__ void __launch_bounds__(WARPS * 32, 3) sums_kernel(const __grid_constant__ GsArgs a) {
   using L = Lane<T>;
   using P = typename L::P;
-  constexpr int MOST = 4;
-  __shared__ P sum_a[SEG_WARPS][32], sum_b[SEG_WARPS][32];
-  __shared__ uint32_t sum_has[SEG_WARPS];
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ P sum_a[WARPS][32], sum_b[WARPS][32];
+  __shared__ uint32_t sum_has[WARPS];
+  __shared__ uint64_t bars[WARPS];
   const Order& o = BACK ? a.flipped : a.order;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t seg = blockIdx.x / a.blocks;
-  const int block = (int)(blockIdx.x % a.blocks), c = (block * 32 + lane) * L::V;
+  const int block = (int)(blockIdx.x % a.blocks), c0 = block * 32 * L::V, c = c0 + lane * L::V;
   const bool in = c < a.C;
-  const int64_t w0 = (seg * SEG_WARPS + warp) * a.each;
+  const uint32_t full = smem_addr(&bars[warp]), buffer = smem_addr(smem) + warp * 2 * BLOCK;
+  if (lane == 0) {
+    sm100::mbar_init(full, 1);
+    sm100::fence_mbar_init();
+  }
+  __syncwarp();
+  const Walk walk = walk_of(o, buffer);
+  const float* states = BACK ? a.d_state_out : a.state_in;
+  const int64_t unit = seg * WARPS + warp, w0 = unit * a.each;
   P fa = L::make(1.0f, 1.0f), fb = L::make(0.0f, 0.0f);
-  bool has = false;
-  P before_a[MOST], before_b[MOST];        // before each window, from the warp's first on
-  bool before_has[MOST];
-  int64_t first = w0 < a.windows ? border_at(a, o, w0 * WINDOW, lane) : 0;
-#pragma unroll
-  for (int e = 0; e < MOST; ++e) {
-    before_a[e] = fa, before_b[e] = fb, before_has[e] = has;
-    if (e >= a.each || w0 + e >= a.windows) continue;
-    const Marks m = marks_of(a, o, (w0 + e) * WINDOW, first, lane);
-    // the next window's first border: behind those at this one's positions
-    for (;;) {
-      const int64_t b = first + lane <= a.n_seq ? border(a, o, first + lane) : INT64_MAX;
-      const int n = __popc(__ballot_sync(FULL, b < m.pos + WINDOW));
-      first += n;
-      if (n < 32) break;
+  bool has = false, ok = true;
+  uint32_t parity = 0;
+  int64_t lo, hi, next = 0;
+  extent(a, o, lo, hi);
+  if (w0 < a.windows) next = border_at(a, o, w0 * WINDOW > lo ? w0 * WINDOW : lo, lane);
+  for (int e = 0; e < a.each && w0 + e < a.windows; ++e) {
+    if (in) {
+      put_state<L>(a.win_a + (w0 + e) * a.C + c, fa);
+      put_state<L>(a.win_b + (w0 + e) * a.C + c, fb);
     }
-    // rows before the last first row do not count behind the window, but for what ends there (nothing here)
-    uint32_t x[WINDOW], y[WINDOW];
-    load<T>(a, o, m, a.p, a.ps, c, in, x);
-    if constexpr (BACK) load<T>(a, o, m, a.g, a.gs, c, in, y);
-    else load<T>(a, o, m, a.n, a.ns, c, in, y);
+    if (lane == 0 && block == 0) a.win_has[w0 + e] = has;
+    const int64_t pos = (w0 + e) * WINDOW;
+    if (pos >= hi || pos + WINDOW <= lo) continue;
+    const Window m = window_at(a, o, pos, lo, hi, next, lane, next);
+    bring<2>(buffer, full, o, m.pos, c0, &a.tp, BACK ? &a.tg : &a.tn, nullptr);
+    ok = brought(full, parity) && ok;
+    parity ^= 1;
+    const uint32_t slow = states ? m.begins : 0u;
+    for (int i0 = 0; i0 < m.count; i0 += GROUP) {
+      P w[GROUP], x[GROUP];
 #pragma unroll
-    for (int i = 0; i < WINDOW; ++i) {
-      if (!((m.valid >> i) & 1u)) continue;
-      if ((m.begins >> i) & 1u) {
-        fb = given<L>(a, o, m, i, BACK ? a.d_state_out : a.state_in, c, in);
-        has = true;
+      for (int i = 0; i < GROUP; ++i) {
+        const uint32_t at = walk.at + (i0 + i) * walk.step;
+        P z;
+        L::gates(L::get(lds(at)), z, w[i]);
+        const P y = L::get(lds(at + BLOCK));
+        x[i] = BACK ? y : L::mul(z, y);
       }
-      P z, w;
-      L::gates(L::get(x[i]), z, w);
-      fa = L::mul(fa, w);
-      if constexpr (BACK) fb = L::mul(w, L::add(L::get(y[i]), fb));
-      else fb = L::fma(w, fb, L::mul(z, L::get(y[i])));
+      const int left = m.count - i0;
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i) {
+        const bool begins = (m.begins >> (i0 + i)) & 1u;
+        has = has || begins;
+        P before = L::pick(begins, L::make(0.0f, 0.0f), fb);
+        if ((slow >> (i0 + i)) & 1u) before = given<L>(a, o, m, i0 + i, false, states, c, in);
+        const P ta = L::mul(fa, w[i]);
+        P tb;
+        if constexpr (BACK) tb = L::mul(w[i], L::add(x[i], before));
+        else tb = L::fma(w[i], before, x[i]);
+        fa = L::pick(i < left, ta, fa), fb = L::pick(i < left, tb, fb);
+      }
     }
+    __syncwarp();
   }
   sum_a[warp][lane] = fa, sum_b[warp][lane] = fb;
   if (lane == 0) sum_has[warp] = has;
   __syncthreads();
+  if (!ok && lane == 0) atomicAdd(a.expired, 1ull);
   // from the segment's first row on
   P ga = L::make(1.0f, 1.0f), gb = L::make(0.0f, 0.0f);
   bool gh = false;
-  for (int u = 0; u < SEG_WARPS; ++u) {
-    if (u == warp) {
-#pragma unroll
-      for (int e = 0; e < MOST; ++e) {
-        if (e >= a.each || w0 + e >= a.windows) continue;
-        const P b = L::pick(before_has[e], before_b[e], L::fma(before_a[e], gb, before_b[e]));
-        if (in) {
-          put_state<L>(a.win_a + (w0 + e) * a.C + c, L::mul(before_a[e], ga));
-          put_state<L>(a.win_b + (w0 + e) * a.C + c, b);
-        }
-        if (lane == 0 && block == 0) a.win_has[w0 + e] = gh || before_has[e];
-      }
-    }
+  auto on = [&](int u) {
     const bool h = sum_has[u];
     gb = L::pick(h, sum_b[u][lane], L::fma(sum_a[u][lane], gb, sum_b[u][lane]));
     ga = L::mul(sum_a[u][lane], ga);
     gh = gh || h;
+  };
+  for (int u = 0; u < warp; ++u) on(u);
+  if (w0 < a.windows) {
+    if (in) put_state<L>(a.warp_a + unit * a.C + c, ga), put_state<L>(a.warp_b + unit * a.C + c, gb);
+    if (lane == 0 && block == 0) a.warp_has[unit] = gh;
   }
-  if (warp == 0) {
+  if (warp == WARPS - 1) {
+    on(warp);
     if (in) put_state<L>(a.seg_a + seg * a.C + c, ga), put_state<L>(a.seg_b + seg * a.C + c, gb);
     if (lane == 0 && block == 0) a.seg_has[seg] = gh;
   }
@@ -350,221 +390,254 @@ __global__ void __launch_bounds__(64) chain_kernel(const __grid_constant__ GsArg
 // What comes into a window from before it.
 template <class L>
 __device__ __forceinline__ typename L::P into(const GsArgs& a, int64_t window, int c, bool in) {
-  typename L::P h = L::make(0.0f, 0.0f);
+  using P = typename L::P;
+  P h = L::make(0.0f, 0.0f);
   if (in) {
-    h = get_state<L>(a.win_b + window * a.C + c);
-    if (!a.win_has[window])
-      h = L::fma(get_state<L>(a.win_a + window * a.C + c),
-                 get_state<L>(a.seg_s + window / (SEG_WARPS * a.each) * a.C + c), h);
+    const int64_t unit = window / a.each, seg = unit / WARPS;
+    const P wa = get_state<L>(a.win_a + window * a.C + c), wb = get_state<L>(a.win_b + window * a.C + c);
+    const P ua = get_state<L>(a.warp_a + unit * a.C + c), ub = get_state<L>(a.warp_b + unit * a.C + c);
+    const P s = get_state<L>(a.seg_s + seg * a.C + c);
+    const P u = L::pick(a.warp_has[unit] != 0, ub, L::fma(ua, s, ub));
+    h = L::pick(a.win_has[window] != 0, wb, L::fma(wa, u, wb));
   }
   return h;
 }
 
 // ---------------------------------------------------------------- forward
 
+// A window's rows, brought, from the state h before them to the one after.
 template <class T>
-__device__ __forceinline__ void window_forward(const GsArgs& a, const Marks& m, int c, bool in, typename Lane<T>::P& h) {
+__device__ __forceinline__ void window_forward(const GsArgs& a, const Window& m, const Walk& walk, int c, bool in,
+                                               typename Lane<T>::P& h) {
   using L = Lane<T>;
   using P = typename L::P;
   const Order& o = a.order;
-  uint32_t x[WINDOW], y[WINDOW];
-  load<T>(a, o, m, a.p, a.ps, c, in, x);
-  load<T>(a, o, m, a.n, a.ns, c, in, y);
   T* out = (T*)a.out + row_of(o, m.pos) * a.os + c;
   const int64_t step = o.back ? -a.os : a.os;
-  const uint32_t ends = a.state_out ? m.ends : 0u;
+  const uint32_t slow = a.state_in ? m.begins : 0u, ends = a.state_out ? m.ends : 0u;
+#pragma unroll 1
+  for (int i0 = 0; i0 < m.count; i0 += GROUP) {
+    P w[GROUP], x[GROUP];
 #pragma unroll
-  for (int i = 0; i < WINDOW; ++i, out += step) {
-    if (!((m.valid >> i) & 1u)) continue;
-    if ((m.begins >> i) & 1u) h = given<L>(a, o, m, i, a.state_in, c, in);
-    P z, w;
-    L::gates(L::get(x[i]), z, w);
-    h = L::fma(w, h, L::mul(z, L::get(y[i])));
-    if (in) L::put(out, h);
-    if ((ends >> i) & 1u) {
-      const int64_t b = sequence(a, o, m, i, true);
-      if (in) put_state<L>(a.state_out + b * a.C + c, h);
+    for (int i = 0; i < GROUP; ++i) {
+      const uint32_t at = walk.at + (i0 + i) * walk.step;
+      P z;
+      L::gates(L::get(lds(at)), z, w[i]);
+      x[i] = L::mul(z, L::get(lds(at + BLOCK)));
+    }
+    const int left = in ? m.count - i0 : 0;
+    const uint32_t begins = m.begins >> i0;
+    if (((slow | ends) >> i0 & ((1u << GROUP) - 1u)) == 0) {
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i, out += step) {
+        h = L::fma(w[i], L::pick((begins >> i) & 1u, L::make(0.0f, 0.0f), h), x[i]);
+        if (i < left) L::put(out, h);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i, out += step) {
+        if (i0 + i >= m.count) break;
+        if ((begins >> i) & 1u) h = given<L>(a, o, m, i0 + i, false, a.state_in, c, in);
+        h = L::fma(w[i], h, x[i]);
+        if (in) L::put(out, h);
+        if ((ends >> (i0 + i)) & 1u) {
+          const int64_t b = sequence(a, o, m, i0 + i, true);
+          if (in) put_state<L>(a.state_out + b * a.C + c, h);
+        }
+      }
     }
   }
 }
 
 template <class T, bool LONG>
-__global__ void __launch_bounds__(ROW_WARPS * 32) rows_kernel(const __grid_constant__ GsArgs a) {
+__global__ void __launch_bounds__(WARPS * 32, 3) rows_kernel(const __grid_constant__ GsArgs a) {
   using L = Lane<T>;
   using P = typename L::P;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t bars[WARPS];
   empty_sequences(a, a.state_out, a.state_in);
-  const int lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t unit = (int64_t)blockIdx.x * WARPS + warp;
   const int64_t k = unit / a.blocks;
-  const int c = ((int)(unit % a.blocks) * 32 + lane) * L::V;
+  const int c0 = (int)(unit % a.blocks) * 32 * L::V, c = c0 + lane * L::V;
   const bool in = c < a.C;
+  const uint32_t full = smem_addr(&bars[warp]), buffer = smem_addr(smem) + warp * 2 * BLOCK;
+  if (lane == 0) {
+    sm100::mbar_init(full, 1);
+    sm100::fence_mbar_init();
+  }
+  __syncwarp();
+  const Order& o = a.order;
+  const Walk walk = walk_of(o, buffer);
   P h = L::make(0.0f, 0.0f);
+  bool ok = true;
+  int64_t lo, hi, next;
+  if (a.n_rows == 0) return;
+  extent(a, o, lo, hi);
   if constexpr (LONG) {
-    if (k >= a.windows) return;
-    const Marks m = marks_of(a, a.order, k * WINDOW, border_at(a, a.order, k * WINDOW, lane), lane);
+    const int64_t pos = k * WINDOW, from = pos < lo ? lo : pos;
+    if (k >= a.windows || from >= hi || from >= pos + WINDOW) return;
+    bring<2>(buffer, full, o, from, c0, &a.tp, &a.tn, nullptr);
+    const Window m = window_at(a, o, pos, lo, hi, border_at(a, o, from, lane), lane, next);
     if (!(m.begins & 1u)) h = into<L>(a, k, c, in);
     if (a.saved && in) put_state<L>(a.saved + k * a.C + c, h);
-    window_forward<T>(a, m, c, in, h);
+    ok = brought(full, 0);
+    window_forward<T>(a, m, walk, c, in, h);
   } else {
     // the sequences that begin in [from, from + chunk)
     const int64_t from = k * a.chunk, upto = from + a.chunk;
-    if (from >= a.n_rows) return;
-    int64_t first = border_at(a, a.order, from, lane);
-    if (first > a.n_seq) return;
-    int64_t pos = border(a, a.order, first);
-    if (pos >= upto) return;
-    pos = pos / WINDOW * WINDOW;
+    if (from >= hi) return;
+    next = border_at(a, o, from, lane);
+    if (next > a.n_seq) return;
+    int64_t pos = border(a, o, next);
+    if (pos >= upto || pos >= hi || pos < lo) return;
+    uint32_t parity = 0;
     bool begun = false;
-    for (; pos < a.n_rows; pos += WINDOW) {
-      Marks m = marks_of(a, a.order, pos, first, lane);
-      // the next window's first border
-      for (;;) {
-        const int64_t b = first + lane <= a.n_seq ? border(a, a.order, first + lane) : INT64_MAX;
-        const int n = __popc(__ballot_sync(FULL, b < pos + WINDOW));
-        first += n;
-        if (n < 32) break;
-      }
-      // not the rows before the first of these sequences, nor those from the first behind them on
-      if (!begun) m.valid &= m.begins ? FULL << (__ffs(m.begins) - 1) : 0u;
+    for (bool more = true; more && ok; pos += WINDOW, parity ^= 1) {
+      bring<2>(buffer, full, o, pos, c0, &a.tp, &a.tn, nullptr);
+      Window m = window_at(a, o, pos, lo, hi, next, lane, next);
+      // as far as the first row of the sequences behind these
       const uint32_t behind = upto <= pos ? FULL : upto - pos < WINDOW ? FULL << (upto - pos) : 0u;
       const uint32_t stop = m.begins & behind;
-      if (stop) m.valid &= (stop & -stop) - 1u;
-      m.begins &= m.valid, m.ends &= m.valid;
+      more = stop == 0 && pos + WINDOW < hi && !(pos + WINDOW >= upto && m.ends >> (WINDOW - 1));
+      if (stop) {
+        m.count = __ffs(stop) - 1;
+        m.begins &= (stop & -stop) - 1u, m.ends &= (stop & -stop) - 1u;
+      }
       if (a.saved && in && begun) put_state<L>(a.saved + pos / WINDOW * a.C + c, h);
-      window_forward<T>(a, m, c, in, h);
       begun = true;
-      if (stop || pos + WINDOW >= upto && first > a.n_seq) break;
+      ok = brought(full, parity);
+      window_forward<T>(a, m, walk, c, in, h);
     }
   }
+  if (!ok && lane == 0) atomicAdd(a.expired, 1ull);
 }
 
 // ---------------------------------------------------------------- backward
 
-template <class L>
-struct BackBuffer {                        // of a warp; rows of 128 bytes
-  uint32_t p[WINDOW][32], n[WINDOW][32], g[WINDOW][32];
-  uint32_t more[L::V == 2 ? WINDOW : 1][32];
-};
-
-// A window's rows: states upwards, D downwards.  e: what comes into the last row from behind it, and then
-// out of the first.
+// A window's rows, brought: states from h upwards, D downwards.  e: what comes into the last row from behind
+// it, and then out of the first.
 template <class T>
-__device__ __forceinline__ bool window_backward(const GsArgs& a, const Marks& m, BackBuffer<Lane<T>>* s, uint32_t full,
-                                                uint32_t parity, int c, bool in, typename Lane<T>::P h,
-                                                typename Lane<T>::P& e) {
+__device__ __forceinline__ void window_backward(const GsArgs& a, const Window& m, const Walk& walk, int c, bool in,
+                                                typename Lane<T>::P h, typename Lane<T>::P& e) {
   using L = Lane<T>;
   using P = typename L::P;
   const Order& o = a.order;
-  const int lane = threadIdx.x & 31;
-  const int64_t r0 = row_of(o, o.back ? m.pos + WINDOW - 1 : m.pos);   // the lowest row (it may be below the array)
-  int never = 0;
-  if (lane == 0) {
-    sm100::mbar_arrive_expect_tx(full, 3 * WINDOW * 128);
-    sm100::tma_load_2d(smem_addr(s->p), &a.tp, full, c, (int)r0);
-    sm100::tma_load_2d(smem_addr(s->n), &a.tn, full, c, (int)r0);
-    sm100::tma_load_2d(smem_addr(s->g), &a.tg, full, c, (int)r0);
+  const uint32_t slow = a.state_in ? m.begins : 0u;
+#pragma unroll 1
+  for (int i0 = 0; i0 < m.count; i0 += GROUP) {
+    // z w (n - h) takes the place of n (16 bits: of n and a block more)
+    P z[GROUP], w[GROUP], n[GROUP];
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+      const uint32_t at = walk.at + (i0 + i) * walk.step;
+      L::gates(L::get(lds(at)), z[i], w[i]);
+      n[i] = L::get(lds(at + BLOCK));
+    }
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+      const uint32_t at = walk.at + (i0 + i) * walk.step;
+      h = L::pick((m.begins >> (i0 + i)) & 1u, L::make(0.0f, 0.0f), h);
+      if ((slow >> (i0 + i)) & 1u) h = given<L>(a, o, m, i0 + i, false, a.state_in, c, in);
+      const P q = L::mul(L::mul(z[i], w[i]), L::sub(n[i], h));
+      h = L::fma(w[i], h, L::mul(z[i], n[i]));
+      sts(at + BLOCK, L::part(q, 0));
+      if constexpr (L::V == 2) sts(at + 3 * BLOCK, L::part(q, 1));
+    }
   }
-  if (!__all_sync(FULL, sm100::mbar_wait(full, parity, &never, LOAD_NS))) return false;
-  const int d0 = o.back ? WINDOW - 1 : 0, dir = o.back ? -1 : 1;
-#pragma unroll 8
-  for (int i = 0; i < WINDOW; ++i) {
-    if (!((m.valid >> i) & 1u)) continue;
-    const int d = d0 + dir * i;
-    if ((m.begins >> i) & 1u) h = given<L>(a, o, m, i, a.state_in, c, in);
-    P z, w;
-    L::gates(L::get(s->p[d][lane]), z, w);
-    const P n = L::get(s->n[d][lane]);
-    const P q = L::mul(L::mul(z, w), L::sub(n, h));
-    h = L::fma(w, h, L::mul(z, n));
-    s->n[d][lane] = __float_as_uint(L::part(q, 0));
-    if constexpr (L::V == 2) s->more[d][lane] = __float_as_uint(L::part(q, 1));
-  }
-  const int64_t last = row_of(o, m.pos + WINDOW - 1);
+  const int top = (m.count - 1) / GROUP * GROUP;
+  const int64_t row = row_of(o, m.pos + top + GROUP - 1);
   const int64_t step1 = o.back ? a.dps : -a.dps, step2 = o.back ? a.dns : -a.dns;
-  T *dp = (T*)a.dp + last * a.dps + c, *dn = (T*)a.dn + last * a.dns + c;
-#pragma unroll 8
-  for (int i = WINDOW - 1; i >= 0; --i, dp += step1, dn += step2) {
-    if (!((m.valid >> i) & 1u)) continue;
-    const int d = d0 + dir * i;
-    if ((m.ends >> i) & 1u) {
-      e = L::make(0.0f, 0.0f);
-      if (a.d_state_out) {
-        const int64_t b = sequence(a, o, m, i, true);
-        if (in) e = get_state<L>(a.d_state_out + b * a.C + c);
+  T *dp = (T*)a.dp + row * a.dps + c, *dn = (T*)a.dn + row * a.dns + c;
+  const uint32_t last = a.d_state_out ? m.ends : 0u, begins = a.d_state_in ? m.begins : 0u;
+#pragma unroll 1
+  for (int i0 = top; i0 >= 0; i0 -= GROUP) {
+    P z[GROUP], w[GROUP], g[GROUP], q[GROUP];
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+      const uint32_t at = walk.at + (i0 + i) * walk.step;
+      L::gates(L::get(lds(at)), z[i], w[i]);
+      g[i] = L::get(lds(at + 2 * BLOCK));
+      q[i] = L::make(__uint_as_float(lds(at + BLOCK)), L::V == 2 ? __uint_as_float(lds(at + 3 * BLOCK)) : 0.0f);
+    }
+    const int left = m.count - i0;
+#pragma unroll
+    for (int i = GROUP - 1; i >= 0; --i, dp += step1, dn += step2) {
+      P f = L::pick((m.ends >> (i0 + i)) & 1u, L::make(0.0f, 0.0f), e);
+      if ((last >> (i0 + i)) & 1u) f = given<L>(a, o, m, i0 + i, true, a.d_state_out, c, in);
+      const P D = L::add(g[i], f);
+      e = L::pick(i < left, L::mul(w[i], D), e);
+      if (in && i < left) {
+        L::put(dp, L::mul(q[i], D));
+        L::put(dn, L::mul(z[i], D));
+      }
+      if ((begins >> (i0 + i)) & 1u) {
+        const int64_t b = sequence(a, o, m, i0 + i, false);
+        if (in) put_state<L>(a.d_state_in + b * a.C + c, e);
       }
     }
-    P z, w;
-    L::gates(L::get(s->p[d][lane]), z, w);
-    const P D = L::add(L::get(s->g[d][lane]), e);
-    P q;
-    if constexpr (L::V == 2) q = L::make(__uint_as_float(s->n[d][lane]), __uint_as_float(s->more[d][lane]));
-    else q = L::make(__uint_as_float(s->n[d][lane]), 0.0f);
-    e = L::mul(w, D);
-    if (in) {
-      L::put(dp, L::mul(q, D));
-      L::put(dn, L::mul(z, D));
-    }
-    if (a.d_state_in && ((m.begins >> i) & 1u)) {
-      const int64_t b = sequence(a, o, m, i, false);
-      if (in) put_state<L>(a.d_state_in + b * a.C + c, e);
-    }
   }
-  sm100::fence_proxy_async_smem();         // (what was written into the buffer, before the next copy into it)
   __syncwarp();
-  return true;
 }
 
 template <class T, bool LONG>
 __global__ void __launch_bounds__(BACK_WARPS * 32) back_kernel(const __grid_constant__ GsArgs a) {
   using L = Lane<T>;
   using P = typename L::P;
+  constexpr int BLOCKS = L::V == 2 ? 4 : 3;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint64_t bars[BACK_WARPS];
   empty_sequences(a, a.d_state_in, a.d_state_out);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t full = smem_addr(&bars[warp]);
+  const uint32_t full = smem_addr(&bars[warp]), buffer = smem_addr(smem) + warp * BLOCKS * BLOCK;
   if (lane == 0) {
     sm100::mbar_init(full, 1);
     sm100::fence_mbar_init();
   }
   __syncwarp();
-  BackBuffer<L>* s = reinterpret_cast<BackBuffer<L>*>(smem) + warp;
   const int64_t unit = (int64_t)blockIdx.x * BACK_WARPS + warp;
   const int64_t k = unit / a.blocks;
   const int c0 = (int)(unit % a.blocks) * 32 * L::V, c = c0 + lane * L::V;
   const bool in = c < a.C;
   const Order& o = a.order;
+  const Walk walk = walk_of(o, buffer);
   bool ok = true;
   P e = L::make(0.0f, 0.0f), h = e;
+  int64_t lo, hi, next;
+  if (a.n_rows == 0) return;
+  extent(a, o, lo, hi);
   if constexpr (LONG) {
-    if (k >= a.windows) return;
-    const Marks m = marks_of(a, o, k * WINDOW, border_at(a, o, k * WINDOW, lane), lane);
-    if (!(m.ends >> (WINDOW - 1))) e = into<L>(a, a.windows - 1 - k, c, in);
+    const int64_t pos = k * WINDOW, from = pos < lo ? lo : pos;
+    if (k >= a.windows || from >= hi || from >= pos + WINDOW) return;
+    bring<3>(buffer, full, o, from, c0, &a.tp, &a.tn, &a.tg);
+    const Window m = window_at(a, o, pos, lo, hi, border_at(a, o, from, lane), lane, next);
+    if (!((m.ends >> (m.count - 1)) & 1u)) e = into<L>(a, a.windows - 1 - k, c, in);
     if (in) h = get_state<L>(a.saved + k * a.C + c);
-    ok = window_backward<T>(a, m, s, full, 0, c, in, h, e);
+    ok = brought(full, 0);
+    window_backward<T>(a, m, walk, c, in, h, e);
   } else {
+    // the sequences that begin in [from, upto), the last window first
     const int64_t from = k * a.chunk, upto = from + a.chunk;
-    if (from >= a.n_rows) return;
+    if (from >= hi) return;
     int64_t j = border_at(a, o, from, lane);
     if (j > a.n_seq) return;
-    const int64_t lo = border(a, o, j);
-    if (lo >= upto) return;
+    const int64_t run = border(a, o, j);
+    if (run >= upto || run >= hi || run < lo) return;
     j = border_at(a, o, upto, lane);
-    const int64_t hi = border(a, o, j <= a.n_seq ? j : a.n_seq);
+    const int64_t end = j <= a.n_seq && border(a, o, j) < hi ? border(a, o, j) : hi;
     uint32_t parity = 0;
-    for (int64_t pos = (hi - 1) / WINDOW * WINDOW; ok && hi > lo && pos >= 0 && pos + WINDOW > lo; pos -= WINDOW, parity ^= 1) {
+    for (int64_t pos = run + (end - run - 1) / WINDOW * WINDOW; ok && end > run && pos >= run; pos -= WINDOW, parity ^= 1) {
+      bring<3>(buffer, full, o, pos, c0, &a.tp, &a.tn, &a.tg);
       // the first border at or behind the window's first position
       for (;;) {
         const int n = __popc(__ballot_sync(FULL, j - 1 - lane >= 0 && border(a, o, j - 1 - lane) >= pos));
         j -= n;
         if (n < 32) break;
       }
-      Marks m = marks_of(a, o, pos, j, lane);
-      if (lo > pos) m.valid &= FULL << (lo - pos);
-      if (hi - pos < WINDOW) m.valid &= (1u << (hi - pos)) - 1u;
-      m.begins &= m.valid, m.ends &= m.valid;
-      if (in && lo < pos) h = get_state<L>(a.saved + pos / WINDOW * a.C + c);
-      ok = window_backward<T>(a, m, s, full, parity, c, in, h, e);
+      const Window m = window_at(a, o, pos, lo, end, j, lane, next);
+      if (in && pos > run) h = get_state<L>(a.saved + pos / WINDOW * a.C + c);
+      ok = brought(full, parity);
+      window_backward<T>(a, m, walk, c, in, h, e);
     }
   }
   if (!ok && lane == 0) atomicAdd(a.expired, 1ull);
@@ -658,8 +731,8 @@ int64_t windows_of(int64_t n_rows) { return (n_rows + WINDOW - 1) / WINDOW; }
 
 size_t workspace_bytes(int64_t n_rows, int64_t n_seq, int32_t channels) {
   if (!is_long(n_rows, n_seq)) return 0;
-  const size_t w = windows_of(n_rows), s = (w + SEG_WARPS - 1) / SEG_WARPS;    // (segments at most)
-  return (w * 2 + s * 3 + n_seq) * channels * 4 + (w + s) * 4;
+  const size_t w = windows_of(n_rows), s = (w + WARPS - 1) / WARPS;            // (segments at most)
+  return (w * 4 + s * 3 + n_seq) * channels * 4 + (2 * w + s) * 4;
 }
 
 // A call of the scan, forward or backward.
@@ -697,23 +770,22 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
   // positions in the other order, windows the same: position' = 32 windows - 1 - position
   const int64_t end = a.windows * WINDOW;
   a.flipped = f.reverse ? Order{0, end - N} : Order{1, end - 1};
-  if (BACK) {
-    a.expired = operator_expired();
-    if (!a.expired) return TRACKFIT_ERR_CUDA;
-    if (N > 0 && (!make_map(&a.tp, f.dtype, a.p, N, a.C, a.ps) || !make_map(&a.tn, f.dtype, a.n, N, a.C, a.ns) ||
-                  !make_map(&a.tg, f.dtype, a.g, N, a.C, a.gs)))
-      return TRACKFIT_ERR_CUDA;
-  }
+  a.expired = operator_expired();
+  if (!a.expired) return TRACKFIT_ERR_CUDA;
+  if (N > 0 && (!make_map(&a.tp, f.dtype, a.p, N, a.C, a.ps) || !make_map(&a.tn, f.dtype, a.n, N, a.C, a.ns) ||
+                (BACK && !make_map(&a.tg, f.dtype, a.g, N, a.C, a.gs))))
+    return TRACKFIT_ERR_CUDA;
   const bool lng = is_long(N, a.n_seq);
-  int64_t units;
+  int64_t n_units;
   if (lng) {
     // as many windows a warp as leave every SM two segments
-    a.each = 4;
-    while (a.each > 1 && (a.windows + SEG_WARPS * a.each - 1) / (SEG_WARPS * a.each) * a.blocks < 2 * 152) a.each /= 2;
-    a.segments = (a.windows + SEG_WARPS * a.each - 1) / (SEG_WARPS * a.each);
-    float* w = (float*)f.workspace;
-    const int64_t per = a.windows * a.C, seg = a.segments * a.C;
-    a.win_a = w, a.win_b = w + per, a.seg_a = w + 2 * per, a.seg_b = a.seg_a + seg, a.seg_s = a.seg_b + seg;
+    a.each = 8;
+    while (a.each > 1 && (a.windows + WARPS * a.each - 1) / (WARPS * a.each) * a.blocks < 2 * 152) a.each /= 2;
+    a.segments = (a.windows + WARPS * a.each - 1) / (WARPS * a.each);
+    const int64_t per = a.windows * a.C, seg = a.segments * a.C, units = (a.windows + a.each - 1) / a.each;
+    a.win_a = (float*)f.workspace, a.win_b = a.win_a + per, a.warp_a = a.win_b + per, a.warp_b = a.warp_a + units * a.C;
+    a.seg_a = a.warp_b + units * a.C, a.seg_b = a.seg_a + seg, a.seg_s = a.seg_b + seg;
+    if (a.segments * a.blocks > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
     // the states given are read again where their sequences begin (end), when the state after a sequence
     // may already stand in the same place: then from a copy
     float* copy = a.seg_s + seg;
@@ -723,32 +795,32 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
       if (e != cudaSuccess) return tf_status_from_cuda(e);
       given = copy;
     }
-    a.win_has = (uint32_t*)(copy + a.n_seq * a.C), a.seg_has = a.win_has + a.windows;
-    if (a.segments * a.blocks > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
-    sums_kernel<T, BACK><<<(unsigned)(a.segments * a.blocks), SEG_WARPS * 32, 0, st>>>(a);
+    a.win_has = (uint32_t*)(copy + a.n_seq * a.C), a.warp_has = a.win_has + a.windows, a.seg_has = a.warp_has + units;
+    constexpr auto sums = sums_kernel<T, BACK>;
+    constexpr size_t smem = 2 * BLOCK * WARPS;
+    const cudaError_t e = allow_smem<sums>(smem + 8192);
+    if (e != cudaSuccess) return tf_status_from_cuda(e);
+    sums<<<(unsigned)(a.segments * a.blocks), WARPS * 32, smem, st>>>(a);
     chain_kernel<<<(unsigned)((a.C + 63) / 64), 64, 0, st>>>(a);
-    units = a.windows * a.blocks;
+    n_units = a.windows * a.blocks;
   } else {
-    // 64 rows a warp: about an eighth more than its own are a sequence's rest; fewer where warps are few
-    a.chunk = 64;
-    while (a.chunk > 16 && (N + a.chunk - 1) / a.chunk * a.blocks < 152 * 16) a.chunk /= 2;
-    units = (N + a.chunk - 1) / a.chunk * a.blocks;
+    // 128 rows a warp: the rest of its last sequence is a few rows more; fewer where warps are few
+    a.chunk = 128;
+    while (a.chunk > 16 && (N + a.chunk - 1) / a.chunk * a.blocks < 152 * 24) a.chunk /= 2;
+    n_units = (N + a.chunk - 1) / a.chunk * a.blocks;
   }
-  constexpr int warps = BACK ? BACK_WARPS : ROW_WARPS;
-  int64_t grid = (units + warps - 1) / warps;
+  constexpr int warps = BACK ? BACK_WARPS : WARPS;
+  int64_t grid = (n_units + warps - 1) / warps;
   if (grid < 1) grid = a.n_seq < 8 * 152 ? (a.n_seq + warps - 1) / warps : 2 * 152;    // states of empty sequences only
   if (grid > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
-  if constexpr (BACK) {
-    constexpr size_t smem = sizeof(BackBuffer<L>) * BACK_WARPS;
-    constexpr auto k0 = back_kernel<T, false>, k1 = back_kernel<T, true>;
-    const cudaError_t e = lng ? allow_smem<k1>(smem) : allow_smem<k0>(smem);
-    if (e != cudaSuccess) return tf_status_from_cuda(e);
-    if (lng) k1<<<(unsigned)grid, warps * 32, smem, st>>>(a);
-    else k0<<<(unsigned)grid, warps * 32, smem, st>>>(a);
-  } else {
-    if (lng) rows_kernel<T, true><<<(unsigned)grid, warps * 32, 0, st>>>(a);
-    else rows_kernel<T, false><<<(unsigned)grid, warps * 32, 0, st>>>(a);
-  }
+  constexpr size_t smem = (BACK ? (L::V == 2 ? 4 : 3) : 2) * BLOCK * warps;
+  constexpr auto kernels = [] {
+    if constexpr (BACK) return std::make_pair(&back_kernel<T, false>, &back_kernel<T, true>);
+    else return std::make_pair(&rows_kernel<T, false>, &rows_kernel<T, true>);
+  }();
+  const cudaError_t e = lng ? allow_smem<kernels.second>(smem + 1024) : allow_smem<kernels.first>(smem + 1024);   // (with the barriers)
+  if (e != cudaSuccess) return tf_status_from_cuda(e);
+  (lng ? kernels.second : kernels.first)<<<(unsigned)grid, warps * 32, smem, st>>>(a);
   return launched();
 }
 
