@@ -35,6 +35,7 @@ using namespace seqops;
 
 constexpr int WINDOW = 32;                 // positions, and from one saved state to the next
 constexpr int GROUP = 8;                   // rows whose gates are formed side by side
+constexpr uint32_t GROUP_BITS = (1u << GROUP) - 1u;
 constexpr int WARPS = 8;                   // of a CTA, forward; of a segment
 constexpr int BACK_WARPS = 4;
 constexpr int MAX_CHANNELS = 1 << 16;
@@ -324,17 +325,21 @@ __global__ void __launch_bounds__(WARPS * 32, 3) sums_kernel(const __grid_consta
         x[i] = BACK ? y : L::mul(z, y);
       }
       const int left = m.count - i0;
+      has = has || (m.begins >> i0 & GROUP_BITS) != 0;
+      auto row = [&](int i, P before) {
+        fa = L::mul(fa, w[i]);
+        if constexpr (BACK) fb = L::mul(w[i], L::add(x[i], before));
+        else fb = L::fma(w[i], before, x[i]);
+      };
+      if (left >= GROUP && (slow >> i0 & GROUP_BITS) == 0) {
 #pragma unroll
-      for (int i = 0; i < GROUP; ++i) {
-        const bool begins = (m.begins >> (i0 + i)) & 1u;
-        has = has || begins;
-        P before = L::pick(begins, L::make(0.0f, 0.0f), fb);
-        if ((slow >> (i0 + i)) & 1u) before = given<L>(a, o, m, i0 + i, false, states, c, in);
-        const P ta = L::mul(fa, w[i]);
-        P tb;
-        if constexpr (BACK) tb = L::mul(w[i], L::add(x[i], before));
-        else tb = L::fma(w[i], before, x[i]);
-        fa = L::pick(i < left, ta, fa), fb = L::pick(i < left, tb, fb);
+        for (int i = 0; i < GROUP; ++i) row(i, L::pick((m.begins >> (i0 + i)) & 1u, L::make(0.0f, 0.0f), fb));
+      } else {
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) {
+          if (i >= left) break;
+          row(i, (m.begins >> (i0 + i)) & 1u ? given<L>(a, o, m, i0 + i, false, states, c, in) : fb);
+        }
       }
     }
     __syncwarp();
@@ -427,7 +432,7 @@ __device__ __forceinline__ void window_forward(const GsArgs& a, const Window& m,
     }
     const int left = in ? m.count - i0 : 0;
     const uint32_t begins = m.begins >> i0;
-    if (((slow | ends) >> i0 & ((1u << GROUP) - 1u)) == 0) {
+    if (((slow | ends) >> i0 & GROUP_BITS) == 0) {
 #pragma unroll
       for (int i = 0; i < GROUP; ++i, out += step) {
         h = L::fma(w[i], L::pick((begins >> i) & 1u, L::make(0.0f, 0.0f), h), x[i]);
@@ -534,15 +539,26 @@ __device__ __forceinline__ void window_backward(const GsArgs& a, const Window& m
       L::gates(L::get(lds(at)), z[i], w[i]);
       n[i] = L::get(lds(at + BLOCK));
     }
-#pragma unroll
-    for (int i = 0; i < GROUP; ++i) {
+    const uint32_t firsts = m.begins >> i0;
+    auto row = [&](int i) {
       const uint32_t at = walk.at + (i0 + i) * walk.step;
-      h = L::pick((m.begins >> (i0 + i)) & 1u, L::make(0.0f, 0.0f), h);
-      if ((slow >> (i0 + i)) & 1u) h = given<L>(a, o, m, i0 + i, false, a.state_in, c, in);
       const P q = L::mul(L::mul(z[i], w[i]), L::sub(n[i], h));
       h = L::fma(w[i], h, L::mul(z[i], n[i]));
       sts(at + BLOCK, L::part(q, 0));
       if constexpr (L::V == 2) sts(at + 3 * BLOCK, L::part(q, 1));
+    };
+    if ((slow >> i0 & GROUP_BITS) == 0) {
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i) {
+        h = L::pick((firsts >> i) & 1u, L::make(0.0f, 0.0f), h);
+        row(i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i) {
+        if ((firsts >> i) & 1u) h = given<L>(a, o, m, i0 + i, false, a.state_in, c, in);
+        row(i);
+      }
     }
   }
   const int top = (m.count - 1) / GROUP * GROUP;
@@ -561,19 +577,32 @@ __device__ __forceinline__ void window_backward(const GsArgs& a, const Window& m
       q[i] = L::make(__uint_as_float(lds(at + BLOCK)), L::V == 2 ? __uint_as_float(lds(at + 3 * BLOCK)) : 0.0f);
     }
     const int left = m.count - i0;
+    const uint32_t lasts = m.ends >> i0;
+    if (left >= GROUP && ((last | begins) >> i0 & GROUP_BITS) == 0) {
 #pragma unroll
-    for (int i = GROUP - 1; i >= 0; --i, dp += step1, dn += step2) {
-      P f = L::pick((m.ends >> (i0 + i)) & 1u, L::make(0.0f, 0.0f), e);
-      if ((last >> (i0 + i)) & 1u) f = given<L>(a, o, m, i0 + i, true, a.d_state_out, c, in);
-      const P D = L::add(g[i], f);
-      e = L::pick(i < left, L::mul(w[i], D), e);
-      if (in && i < left) {
-        L::put(dp, L::mul(q[i], D));
-        L::put(dn, L::mul(z[i], D));
+      for (int i = GROUP - 1; i >= 0; --i, dp += step1, dn += step2) {
+        const P D = L::add(g[i], L::pick((lasts >> i) & 1u, L::make(0.0f, 0.0f), e));
+        e = L::mul(w[i], D);
+        if (in) {
+          L::put(dp, L::mul(q[i], D));
+          L::put(dn, L::mul(z[i], D));
+        }
       }
-      if ((begins >> (i0 + i)) & 1u) {
-        const int64_t b = sequence(a, o, m, i0 + i, false);
-        if (in) put_state<L>(a.d_state_in + b * a.C + c, e);
+    } else {
+#pragma unroll
+      for (int i = GROUP - 1; i >= 0; --i, dp += step1, dn += step2) {
+        if (i >= left) continue;
+        if ((lasts >> i) & 1u) e = given<L>(a, o, m, i0 + i, true, a.d_state_out, c, in);
+        const P D = L::add(g[i], e);
+        e = L::mul(w[i], D);
+        if (in) {
+          L::put(dp, L::mul(q[i], D));
+          L::put(dn, L::mul(z[i], D));
+        }
+        if ((begins >> (i0 + i)) & 1u) {
+          const int64_t b = sequence(a, o, m, i0 + i, false);
+          if (in) put_state<L>(a.d_state_in + b * a.C + c, e);
+        }
       }
     }
   }
