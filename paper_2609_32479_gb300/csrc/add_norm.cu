@@ -6,7 +6,7 @@
 //
 // A pass over memory, which bounds it: each value is read once and written once.  G threads hold a
 // row, V pieces of 16 bytes each, s in fp32 as it was added up; the sum of squares and the largest
-// |y| go through the G threads (a part of a warp, or eight warps through shared memory).  Narrow
+// |y| go through the G threads (a part of a warp, or two to eight warps through shared memory).  Narrow
 // rows: a few rows' loads are under way together.
 #include "seq_ops.cuh"
 
@@ -61,10 +61,13 @@ __device__ __forceinline__ float over_row(float v, float* at) {
   return v;
 }
 
+// (rows that a part of a warp holds: CTAs of 256 threads; wider ones: a CTA a row)
+__host__ __device__ constexpr int threads_of(int G) { return G > 32 ? G : NT; }
+
 template <class T, bool EIGHT, int G, int V, int ROWS>
-__global__ void __launch_bounds__(NT) norm_kernel(const NormArgs a) {
-  constexpr int VE = 16 / sizeof(T), GROUPS = NT / G;
-  static_assert(G <= 32 || (ROWS == 1 && G == NT), "eight warps take one row at a time");
+__global__ void __launch_bounds__(threads_of(G)) norm_kernel(const NormArgs a) {
+  constexpr int VE = 16 / sizeof(T), GROUPS = threads_of(G) / G;
+  static_assert(G <= 32 || ROWS == 1, "the warps of a CTA take one row at a time");
   __shared__ float part[2][2][NT / 32];
   const int e = threadIdx.x % G;
   const float inv_c = 1.0f / (float)a.C;
@@ -171,8 +174,9 @@ __global__ void __launch_bounds__(NT) norm_kernel(const NormArgs a) {
 template <class T, bool EIGHT, int G, int V, int ROWS>
 int launch(const NormArgs& a, cudaStream_t st) {
   // four CTAs of an SM keep enough loads under way; few rows are spread over more CTAs
-  const int64_t need = (a.n + NT / G * ROWS - 1) / (NT / G * ROWS), most = 152 * 8;
-  norm_kernel<T, EIGHT, G, V, ROWS><<<(unsigned)(need < most ? need : most), NT, 0, st>>>(a);
+  constexpr int threads = threads_of(G), rows = threads / G * ROWS;
+  const int64_t need = (a.n + rows - 1) / rows, most = 152 * 8 * (NT / threads);
+  norm_kernel<T, EIGHT, G, V, ROWS><<<(unsigned)(need < most ? need : most), threads, 0, st>>>(a);
   return launched();
 }
 
@@ -181,12 +185,14 @@ int by_width(const NormArgs& a, cudaStream_t st) {
   const int v = a.C * (int)sizeof(T) / 16;   // 16-byte pieces of a row
   // a row at a time while the rows are too few to fill the GPU
   const bool few = a.n <= 152 * 32;
+  if (v <= 2) return few ? launch<T, EIGHT, 2, 1, 1>(a, st) : launch<T, EIGHT, 2, 1, 4>(a, st);
   if (v <= 8) return few ? launch<T, EIGHT, 8, 1, 1>(a, st) : launch<T, EIGHT, 8, 1, 4>(a, st);
   if (v <= 16) return few ? launch<T, EIGHT, 16, 1, 1>(a, st) : launch<T, EIGHT, 16, 1, 4>(a, st);
   if (v <= 32) return few ? launch<T, EIGHT, 32, 1, 1>(a, st) : launch<T, EIGHT, 32, 1, 4>(a, st);
   if (v <= 64) return few ? launch<T, EIGHT, 32, 2, 1>(a, st) : launch<T, EIGHT, 32, 2, 2>(a, st);
   if (v <= 128) return launch<T, EIGHT, 32, 4, 1>(a, st);
-  if (v <= 512) return launch<T, EIGHT, NT, 2, 1>(a, st);
+  if (v <= 256) return launch<T, EIGHT, 64, 4, 1>(a, st);
+  if (v <= 512) return launch<T, EIGHT, 128, 4, 1>(a, st);
   if (v <= 1024) return launch<T, EIGHT, NT, 4, 1>(a, st);
   if (v <= 2048) return launch<T, EIGHT, NT, 8, 1>(a, st);
   if constexpr (sizeof(T) == 4) return launch<T, EIGHT, NT, 16, 1>(a, st);

@@ -1,4 +1,4 @@
-// Rows times a weight matrix for up to 16 rows: the weights are read once, and that
+// Rows times a weight matrix for up to 64 rows (fp32: 16): the weights are read once, and that
 // bounds it.
 //
 // 16 and 8 bits: a warp takes 16 outputs and a part of K with the weights as the product's A (16 x 16) and the rows
@@ -40,7 +40,7 @@ __device__ __forceinline__ uint4 load16(const uint8_t* p, bool there) {
 template <class T, bool EIGHT, int NT>
 __global__ void __launch_bounds__(WARPS * 32) product_few_kernel(const ProductArgs a) {
   constexpr int SZ = EIGHT ? 1 : 2, KS = 64 / SZ;     // channels that four lanes' 16 bytes hold
-  constexpr int ROWS = 8 * NT, AHEAD = 4;
+  constexpr int ROWS = 8 * NT, AHEAD = NT <= 2 ? 4 : 2;
   __shared__ float sums[WARPS][ROWS][17];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int m0 = blockIdx.x * 16;
@@ -89,19 +89,21 @@ __global__ void __launch_bounds__(WARPS * 32) product_few_kernel(const ProductAr
   }
   __syncthreads();
   constexpr int VE = 16 / sizeof(T), PER = 16 / VE;   // threads of a row
-  const int r = threadIdx.x / PER, c = threadIdx.x % PER * VE;
-  if (r >= ROWS || r >= a.n || m0 + c >= a.M) return;
-  float y[VE] = {};
+  const int c = threadIdx.x % PER * VE;
+  for (int r = threadIdx.x / PER; r < ROWS; r += WARPS * 32 / PER) {
+    if (r >= a.n || m0 + c >= a.M) return;
+    float y[VE] = {};
 #pragma unroll
-  for (int w = 0; w < WARPS; ++w)
+    for (int w = 0; w < WARPS; ++w)
 #pragma unroll
-    for (int i = 0; i < VE; ++i) y[i] += sums[w][r][c + i];
-  const int64_t col = m0 + c;
-  const uint4 none = make_uint4(0, 0, 0, 0);
-  const uint4 gate = a.gate ? *reinterpret_cast<const uint4*>((const T*)a.gate + r * a.gs + col) : none;
-  const uint4 res = a.res ? *reinterpret_cast<const uint4*>((const T*)a.res + r * a.rs + col) : none;
-  finish<T, EIGHT>(a, y, EIGHT ? a.x_scales[r] : 1.0f, (int)col, gate, res);
-  *reinterpret_cast<uint4*>((T*)a.out + r * a.os + col) = pack(y, T());
+      for (int i = 0; i < VE; ++i) y[i] += sums[w][r][c + i];
+    const int64_t col = m0 + c;
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const uint4 gate = a.gate ? *reinterpret_cast<const uint4*>((const T*)a.gate + r * a.gs + col) : none;
+    const uint4 res = a.res ? *reinterpret_cast<const uint4*>((const T*)a.res + r * a.rs + col) : none;
+    finish<T, EIGHT>(a, y, EIGHT ? a.x_scales[r] : 1.0f, (int)col, gate, res);
+    *reinterpret_cast<uint4*>((T*)a.out + r * a.os + col) = pack(y, T());
+  }
 }
 
 // fp32: a warp takes four outputs and a part of K, a lane four channels of 128; the lanes' sums are
@@ -160,7 +162,9 @@ template <class T, bool EIGHT>
 int launch(const ProductArgs& a, cudaStream_t st) {
   const unsigned grid = (unsigned)((a.M + 15) / 16);
   if (a.n <= 8) product_few_kernel<T, EIGHT, 1><<<grid, WARPS * 32, 0, st>>>(a);
-  else product_few_kernel<T, EIGHT, 2><<<grid, WARPS * 32, 0, st>>>(a);
+  else if (a.n <= 16) product_few_kernel<T, EIGHT, 2><<<grid, WARPS * 32, 0, st>>>(a);
+  else if (a.n <= 32) product_few_kernel<T, EIGHT, 4><<<grid, WARPS * 32, 0, st>>>(a);
+  else product_few_kernel<T, EIGHT, 8><<<grid, WARPS * 32, 0, st>>>(a);
   return launched();
 }
 

@@ -283,27 +283,41 @@ __global__ void __launch_bounds__(THREADS, 1) product_tc_kernel(const __grid_con
           if (lane == 0) bulk_wait_read_keep(1);   // of this warp's pieces, the one before the last was in this slot
           __syncwarp();
         }
-#pragma unroll 1
-        for (int h = 0; h < 128 / 64; ++h) {         // 64 bytes of outputs at a time
-          constexpr int N = 64 / (int)sizeof(T);
-          const int col = n0 + h * N;
-          float v[N];
-          if constexpr (N == 32) tmem_ld32(acc + j * PC + h * N, v);
-          else tmem_ld16(acc + j * PC + h * N, v);
-          tmem_ld_wait();
-          if (col < p.a.M) {
+        // 32 outputs at a time (16 bits: the second 32 are on their way with the first)
+        float v[PC / 32][32];
 #pragma unroll
-            for (int i = 0; i < N; i += VE) {
-              if (col + i >= p.a.M) break;
-              const uint32_t piece = (uint32_t)(((h * 64 + i * (int)sizeof(T)) >> 4) ^ (r & 7)) << 4;
-              float y[VE];
+        for (int h = 0; h < PC / 32; ++h) tmem_ld32(acc + j * PC + h * 32, v[h]);
+        tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < VE; ++e) y[e] = v[i + e];
-              uint32_t g[4] = {}, x[4] = {};
-              if (p.a.gate) lds4(its + piece, g);
-              if (p.a.res) lds4(mine + piece, x);
-              finish<T, EIGHT>(p.a, y, xs, col + i, make_uint4(g[0], g[1], g[2], g[3]), make_uint4(x[0], x[1], x[2], x[3]));
-              sts4(mine + piece, pack(y, T()));
+        for (int h = 0; h < PC / 32; ++h) {
+          const int col = n0 + h * 32, left = p.a.M - col;
+          auto put = [&](int i) {
+            const uint32_t piece = (uint32_t)(((h * 32 + i) * (int)sizeof(T) >> 4) ^ (r & 7)) << 4;
+            float y[VE];
+#pragma unroll
+            for (int e = 0; e < VE; ++e) y[e] = v[h][i + e];
+            uint32_t g[4] = {}, x[4] = {};
+            if (p.a.gate) lds4(its + piece, g);
+            if (p.a.res) lds4(mine + piece, x);
+            gated<T>(p.a, y, make_uint4(g[0], g[1], g[2], g[3]), make_uint4(x[0], x[1], x[2], x[3]));
+            sts4(mine + piece, pack(y, T()));
+          };
+          if (left >= 32) {
+            activated<EIGHT>(p.a, v[h], xs, col);
+#pragma unroll
+            for (int i = 0; i < 32; i += VE) put(i);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {         // (outputs are a multiple of 8)
+              if (i >= left) break;
+              float y[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = v[h][i + e];
+              activated<EIGHT>(p.a, y, xs, col + i);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[h][i + e] = y[e];
+#pragma unroll
+              for (int e = 0; e < 8; e += VE) put(i + e);
             }
           }
         }
