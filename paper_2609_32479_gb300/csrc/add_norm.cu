@@ -149,9 +149,9 @@ __global__ void __launch_bounds__(threads_of(G)) norm_kernel(const NormArgs a) {
           for (int i = 0; i < VE; ++i) most = fmaxf(most, fabsf(s[v][i]));
         }
       }
-      float back = 1.0f;
+      float back = 1.0f, scale = 1.0f;
       if constexpr (EIGHT) {
-        const float scale = fmaxf(over_row<G, true>(most, part[turn][1]) / LARGEST, LEAST_SCALE);
+        scale = fmaxf(over_row<G, true>(most, part[turn][1]) / LARGEST, LEAST_SCALE);
         back = 1.0f / scale;
         if (e == 0 && r < a.n) a.scales[r] = scale;
       }
@@ -161,7 +161,12 @@ __global__ void __launch_bounds__(threads_of(G)) norm_kernel(const NormArgs a) {
         if (r >= a.n || c >= a.C) continue;
         if constexpr (EIGHT) {
 #pragma unroll
-          for (int i = 0; i < VE; ++i) s[v][i] *= back;
+          for (int i = 0; i < VE; ++i) {
+            // the quotient, by its remainder as good as rounded once: a value near a border of two 8-bit
+            // values goes the way that it should
+            const float q = s[v][i] * back;
+            s[v][i] = fmaf(fmaf(-q, scale, s[v][i]), back, q);
+          }
           put8((uint8_t*)a.out + r * a.os + c, s[v]);
         } else {
           *reinterpret_cast<uint4*>((T*)a.out + r * a.os + c) = pack(s[v], T());

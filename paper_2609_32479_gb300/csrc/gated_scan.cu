@@ -74,10 +74,12 @@ __device__ __forceinline__ float rcp(float x) {   // (1 ulp; for x in [1, 2])
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// z and w of a gate, each accurate however near to 0: from 2^(-|p| log2 e) and 1 over one more than it.
+// z and w of a gate: the smaller, e / (1 + e) with e = 2^(-|p| log2 e), accurate however near to 0, and one
+// less that, so that they add up to 1 (in the 1,000 rows that a slow channel remembers an error of their
+// sum, always of one sign, would add up too: the states' error was ten times as large).
 __device__ __forceinline__ void gate(float p, float& z, float& w) {
-  const float e = ex2(-LOG2E * fabsf(p)), r = rcp(1.0f + e), s = e * r;
-  z = p < 0.0f ? s : r, w = p < 0.0f ? r : s;
+  const float e = ex2(-LOG2E * fabsf(p)), s = e * rcp(1.0f + e), b = 1.0f - s;
+  z = p < 0.0f ? s : b, w = p < 0.0f ? b : s;
 }
 
 // A lane's channels of a row: 4 bytes, one or two fp32 values (two in the instructions that take two).
@@ -117,8 +119,9 @@ struct Lane16 {
     const float2 x = parts(mul2(both(fabsf(f.x), fabsf(f.y)), both(-LOG2E, -LOG2E)));
     const P e = both(ex2(x.x), ex2(x.y));
     const float2 y = parts(add2(e, both(1.0f, 1.0f)));
-    const float2 r = make_float2(rcp(y.x), rcp(y.y)), s = parts(mul2(e, both(r.x, r.y)));
-    z = both(f.x < 0.0f ? s.x : r.x, f.y < 0.0f ? s.y : r.y), w = both(f.x < 0.0f ? r.x : s.x, f.y < 0.0f ? r.y : s.y);
+    const P small = mul2(e, both(rcp(y.x), rcp(y.y)));
+    const float2 s = parts(small), b = parts(fma2(small, both(-1.0f, -1.0f), both(1.0f, 1.0f)));
+    z = both(f.x < 0.0f ? s.x : b.x, f.y < 0.0f ? s.y : b.y), w = both(f.x < 0.0f ? b.x : s.x, f.y < 0.0f ? b.y : s.y);
   }
   static __device__ __forceinline__ float part(P a, int v) { return v ? parts(a).y : parts(a).x; }
 };

@@ -1,7 +1,7 @@
-// Rows times a weight matrix for up to 64 rows (fp32: 16): the weights are read once, and that
+// Rows times a weight matrix for up to 64 rows of 16 or 8 bits: the weights are read once, and that
 // bounds it.
 //
-// 16 and 8 bits: a warp takes 16 outputs and a part of K with the weights as the product's A (16 x 16) and the rows
+// A warp takes 16 outputs and a part of K with the weights as the product's A (16 x 16) and the rows
 // as its B (16 x 8).  Which channel stands where in a product does not matter as long as it is the
 // same in both, so a lane's 16 bytes of a weight row, as they come from memory, are its part of two
 // products (four of 8 bits, turned to fp16, exactly).  No shared memory on the way; the warps' sums
@@ -106,58 +106,6 @@ __global__ void __launch_bounds__(WARPS * 32) product_few_kernel(const ProductAr
   }
 }
 
-// fp32: a warp takes four outputs and a part of K, a lane four channels of 128; the lanes' sums are
-// added at the end.  Multiplied and added in fp32 throughout.
-template <int NR>
-__global__ void __launch_bounds__(WARPS * 32) product_few_fp32_kernel(const ProductArgs a) {
-  __shared__ float sums[WARPS][NR][4];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int m0 = blockIdx.x * 4;
-  const int steps = (a.K + 127) / 128, per = (steps + WARPS - 1) / WARPS;
-  const int s0 = warp * per, s1 = s0 + per < steps ? s0 + per : steps;
-  const float *w = (const float*)a.w + (int64_t)m0 * a.ws, *x = (const float*)a.x;
-  float acc[NR][4] = {};
-#pragma unroll 2
-  for (int s = s0; s < s1; ++s) {
-    const int k = s * 128 + 4 * lane;
-    if (k >= a.K) continue;
-    float4 u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = __ldg(reinterpret_cast<const float4*>(w + i * a.ws + k));
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      if (r >= a.n) break;
-      const float4 v = __ldg(reinterpret_cast<const float4*>(x + r * a.xs + k));
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        acc[r][i] = fmaf(v.w, u[i].w, fmaf(v.z, u[i].z, fmaf(v.y, u[i].y, fmaf(v.x, u[i].x, acc[r][i]))));
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    if (r >= a.n) break;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) acc[r][i] += __shfl_xor_sync(FULL, acc[r][i], o);
-      if (lane == 0) sums[warp][r][i] = acc[r][i];
-    }
-  }
-  __syncthreads();
-  const int r = threadIdx.x;
-  if (r >= NR || r >= a.n) return;
-  float y[4] = {};
-#pragma unroll
-  for (int i = 0; i < WARPS; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] += sums[i][r][e];
-  const uint4 none = make_uint4(0, 0, 0, 0);
-  const uint4 gate = a.gate ? *reinterpret_cast<const uint4*>((const float*)a.gate + r * a.gs + m0) : none;
-  const uint4 res = a.res ? *reinterpret_cast<const uint4*>((const float*)a.res + r * a.rs + m0) : none;
-  finish<float, false>(a, y, 1.0f, m0, gate, res);
-  *reinterpret_cast<uint4*>((float*)a.out + r * a.os + m0) = pack(y, 0.0f);
-}
-
 template <class T, bool EIGHT>
 int launch(const ProductArgs& a, cudaStream_t st) {
   const unsigned grid = (unsigned)((a.M + 15) / 16);
@@ -174,12 +122,5 @@ int seqops::product_few(int32_t dtype, const ProductArgs& a, cudaStream_t st) {
   if (a.x_scales)
     return dtype == TRACKFIT_FP32 ? launch<float, true>(a, st)
            : dtype == TRACKFIT_BF16_PROJ ? launch<__nv_bfloat16, true>(a, st) : launch<__half, true>(a, st);
-  if (dtype == TRACKFIT_FP32) {
-    const unsigned grid = (unsigned)(a.M / 4);
-    if (a.n <= 4) product_few_fp32_kernel<4><<<grid, WARPS * 32, 0, st>>>(a);
-    else if (a.n <= 8) product_few_fp32_kernel<8><<<grid, WARPS * 32, 0, st>>>(a);
-    else product_few_fp32_kernel<16><<<grid, WARPS * 32, 0, st>>>(a);
-    return launched();
-  }
   return dtype == TRACKFIT_BF16_PROJ ? launch<__nv_bfloat16, false>(a, st) : launch<__half, false>(a, st);
 }

@@ -446,11 +446,20 @@ int launch(const ProductArgs& a, int bn, cudaStream_t st) {
 
 template <class T, bool EIGHT>
 int by_tile(const ProductArgs& a, cudaStream_t st) {
-  // A tile as wide as the outputs, else 256; where tiles are too few for the SMs, narrower, as long
-  // as the pieces of outputs stay whole.
   constexpr int PC = 128 / sizeof(T);
   auto tiles = [&](int rows, int bn) { return (a.n + rows - 1) / rows * ((a.M + bn - 1) / bn); };
-  if (a.M > 128 && tiles(256, 256) >= 64) return launch<T, 2, EIGHT>(a, 256, st);
+  if (a.M > 128 && tiles(256, 256) >= 64) {
+    // Pairs, where they fill the SMs.  A step of K takes as long as its rows of x and W take into the SM:
+    // 128 + bn / 2 of them (8011 x 4096 x 4096: 201 us with 256 outputs, 248 with 192, whose 22 tiles do
+    // little more).  The width with the least of that in all; where outputs are several tiles, of whole pieces.
+    int bn = a.M <= 256 ? (a.M + 31) / 32 * 32 : 256;
+    auto cost = [&](int b) { return (int64_t)((a.M + b - 1) / b) * (128 + b / 2); };
+    for (int b = 192; a.M > 256 && b >= 128; b -= 64)
+      if (b % PC == 0 && cost(b) < cost(bn)) bn = b;
+    return launch<T, 2, EIGHT>(a, bn, st);
+  }
+  // a tile as wide as the outputs, up to 256; where tiles are too few for the SMs, narrower, as long as the
+  // pieces of outputs stay whole
   int bn = a.M > 256 ? 256 : (a.M + 15) / 16 * 16;
   while (bn > PC && tiles(128, bn) < 152) bn = (bn / 2 + PC - 1) / PC * PC;
   return launch<T, 1, EIGHT>(a, bn, st);

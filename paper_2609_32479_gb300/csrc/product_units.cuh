@@ -110,7 +110,7 @@ __device__ __forceinline__ void finish(const ProductArgs& a, float (&y)[VE], flo
 // product_tc.cu: 16-bit and 8-bit operands by the tensor cores, many rows.
 int product_tc(int32_t dtype, const ProductArgs& a, cudaStream_t st);
 // product_few.cu: few rows, where the weights are what is read.
-constexpr int PRODUCT_FEW = 64, PRODUCT_FEW_FP32 = 16;
+constexpr int PRODUCT_FEW = 64;
 int product_few(int32_t dtype, const ProductArgs& a, cudaStream_t st);
 
 }  // namespace seqops
