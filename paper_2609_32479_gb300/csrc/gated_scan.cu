@@ -264,6 +264,10 @@ __device__ __forceinline__ Walk walk_of(const Order& o, uint32_t buffer) {
   return {buffer + 4 * (threadIdx.x & 31) + (o.back ? (WINDOW - 1) * 128 : 0), o.back ? -128 : 128};
 }
 
+// The three kernels of long sequences begin while the one before them ends, with what does not need its
+// results, and wait for these here (a kernel is done only after the one before it is).
+__device__ __forceinline__ void after_kernels_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Sequences of no rows: what is before them is what is after them.
 __device__ __forceinline__ void empty_sequences(const GsArgs& a, float* to, const float* from) {
   if (!to) return;
@@ -378,6 +382,7 @@ __global__ void __launch_bounds__(64) chain_kernel(const __grid_constant__ GsArg
   if (c >= a.C) return;
   constexpr int AHEAD = 16;
   float s = 0.0f;
+  after_kernels_before();
   for (int64_t g = 0; g < a.segments; g += AHEAD) {
     float x[AHEAD], y[AHEAD];
     bool h[AHEAD];
@@ -483,10 +488,16 @@ __global__ void __launch_bounds__(WARPS * 32, 3) rows_kernel(const __grid_consta
   if (a.n_rows == 0) return;
   extent(a, o, lo, hi);
   if constexpr (LONG) {
+    // the last windows first: their rows are in L2, from the sums
+    const int64_t k = a.windows - 1 - unit / a.blocks;
     const int64_t pos = k * WINDOW, from = pos < lo ? lo : pos;
-    if (k >= a.windows || from >= hi || from >= pos + WINDOW) return;
+    if (k < 0 || from >= hi || from >= pos + WINDOW) {
+      after_kernels_before();
+      return;
+    }
     bring<2>(buffer, full, o, from, c0, &a.tp, &a.tn, nullptr);
     const Window m = window_at(a, o, pos, lo, hi, border_at(a, o, from, lane), lane, next);
+    after_kernels_before();
     if (!(m.begins & 1u)) h = into<L>(a, k, c, in);
     if (a.saved && in) put_state<L>(a.saved + k * a.C + c, h);
     ok = brought(full, 0);
@@ -640,9 +651,13 @@ __global__ void __launch_bounds__(BACK_WARPS * 32) back_kernel(const __grid_cons
   extent(a, o, lo, hi);
   if constexpr (LONG) {
     const int64_t pos = k * WINDOW, from = pos < lo ? lo : pos;
-    if (k >= a.windows || from >= hi || from >= pos + WINDOW) return;
+    if (k >= a.windows || from >= hi || from >= pos + WINDOW) {
+      after_kernels_before();
+      return;
+    }
     bring<3>(buffer, full, o, from, c0, &a.tp, &a.tn, &a.tg);
     const Window m = window_at(a, o, pos, lo, hi, border_at(a, o, from, lane), lane, next);
+    after_kernels_before();
     if (!((m.ends >> (m.count - 1)) & 1u)) e = into<L>(a, a.windows - 1 - k, c, in);
     if (in) h = get_state<L>(a.saved + k * a.C + c);
     ok = brought(full, 0);
@@ -793,6 +808,16 @@ int check(const Call& f, const GsArgs& a) {
   return TRACKFIT_OK;
 }
 
+// A kernel that may begin before the one in front of it in the stream has ended.
+inline cudaError_t follow(void (*kernel)(GsArgs), unsigned grid, int threads, size_t smem, cudaStream_t st, const GsArgs& a) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(grid), cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem, cfg.stream = st, cfg.attrs = &at, cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 template <class T, bool BACK>
 int launch(const Call& f, GsArgs& a, cudaStream_t st) {
   using L = Lane<T>;
@@ -833,7 +858,8 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
     const cudaError_t e = allow_smem<sums>(smem + 8192);
     if (e != cudaSuccess) return tf_status_from_cuda(e);
     sums<<<(unsigned)(a.segments * a.blocks), WARPS * 32, smem, st>>>(a);
-    chain_kernel<<<(unsigned)((a.C + 63) / 64), 64, 0, st>>>(a);
+    const cudaError_t e1 = follow(chain_kernel, (unsigned)((a.C + 63) / 64), 64, 0, st, a);
+    if (e1 != cudaSuccess) return tf_status_from_cuda(e1);
     n_units = a.windows * a.blocks;
   } else {
     // 128 rows a warp: the rest of its last sequence is a few rows more; fewer where warps are few
@@ -852,7 +878,12 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
   }();
   const cudaError_t e = lng ? allow_smem<kernels.second>(smem + 1024) : allow_smem<kernels.first>(smem + 1024);   // (with the barriers)
   if (e != cudaSuccess) return tf_status_from_cuda(e);
-  (lng ? kernels.second : kernels.first)<<<(unsigned)grid, warps * 32, smem, st>>>(a);
+  if (!lng) {
+    kernels.first<<<(unsigned)grid, warps * 32, smem, st>>>(a);
+  } else {
+    const cudaError_t e2 = follow(kernels.second, (unsigned)grid, warps * 32, smem, st, a);
+    if (e2 != cudaSuccess) return tf_status_from_cuda(e2);
+  }
   return launched();
 }
 

@@ -353,6 +353,132 @@ __global__ void __launch_bounds__(THREADS, 1) product_tc_kernel(const __grid_con
   }
 }
 
+// ---------------------------------------------------------------- few tiles
+
+// A tile of 128 x BN by a cluster of CTAs, each with a part of K: their sums go to shared memory, and each
+// CTA finishes a part of the tile out of all of them, in their order.
+//   warp 0      TMA loads
+//   warp 1      products, tensor memory
+//   warps 2-5   the sums from tensor memory; all: the epilogue
+constexpr int SPLIT_THREADS = 192;
+
+struct SplitBars {
+  uint64_t full[MAX_STAGES], empty[MAX_STAGES], done;
+  uint32_t tmem;
+  int abort, never;
+};
+
+__device__ __forceinline__ float from_cta(uint32_t at, int rank) {
+  uint32_t u;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(u) : "r"(at), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(u) : "memory");
+  return v;
+}
+
+template <class T, bool EIGHT>
+__global__ void __launch_bounds__(SPLIT_THREADS, 1) product_split_kernel(const __grid_constant__ TcArgs p, int split) {
+  constexpr int VE = 16 / sizeof(T), KB = EIGHT ? 128 : 64;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const int stage_bytes = (128 + p.bn) * 128;
+  float* sums = reinterpret_cast<float*>(smem_raw + (base - raw) + p.stages * stage_bytes);   // [BN][128 rows]
+  SplitBars* bars = reinterpret_cast<SplitBars*>(sums + p.bn * 128);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) mbar_init(smem_u32(&bars->full[s]), 1), mbar_init(smem_u32(&bars->empty[s]), 1);
+    mbar_init(smem_u32(&bars->done), 1);
+    bars->abort = bars->never = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&bars->tmem), 128);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem;
+  volatile int *abort = &bars->abort, *never = &bars->never;
+  const int part = blockIdx.x % split, tile = blockIdx.x / split;
+  const int tm = tile / p.tiles_n, tn = tile % p.tiles_n, m0 = tm * 128, n0 = tn * p.bn;
+  const int k_lo = p.kblocks * part / split, k_hi = p.kblocks * (part + 1) / split;
+  auto fail = [&] {
+    if (atomicExch(&bars->abort, 1) == 0) atomicAdd(p.expired, 1ull);
+  };
+  if (warp == 0 && lane == 0) {
+    int s = 0, issued = 0;
+    uint32_t ph = 0;
+    for (int k = k_lo; k < k_hi; ++k) {
+      if (!mbar_wait(smem_u32(&bars->empty[s]), ph ^ 1u, abort, p.limit_ns)) {
+        fail();
+        break;
+      }
+      const uint32_t at = base + (uint32_t)(s * stage_bytes), full = smem_u32(&bars->full[s]);
+      mbar_arrive_expect_tx(full, (uint32_t)stage_bytes);
+      tma_load_2d(at, &p.tx, full, k * KB, m0);
+      tma_load_2d(at + 128 * 128, &p.tw, full, k * KB, n0);
+      ++issued;
+      if (++s == p.stages) s = 0, ph ^= 1u;
+    }
+    if (*abort)
+      for (int i = issued < p.stages ? 0 : issued - p.stages; i < issued; ++i)
+        mbar_wait(smem_u32(&bars->full[i % p.stages]), (uint32_t)(i / p.stages) & 1u, never, DRAIN_NS);
+  } else if (warp == 1 && lane == 0) {
+    int s = 0;
+    uint32_t ph = 0;
+    for (int k = k_lo; k < k_hi; ++k) {
+      if (!mbar_wait(smem_u32(&bars->full[s]), ph, abort, p.limit_ns)) {
+        fail();
+        break;
+      }
+      tc_fence_after();
+      const uint32_t at = base + (uint32_t)(s * stage_bytes);
+      const uint64_t da = sdesc_sw128(at, 16, 1024), db = sdesc_sw128(at + 128 * 128, 16, 1024);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma<1, EIGHT>(tmem, da + 2 * i, db + 2 * i, p.idesc, k > k_lo || i ? 1u : 0u);
+      commit<1>(smem_u32(&bars->empty[s]));
+      if (++s == p.stages) s = 0, ph ^= 1u;
+    }
+    commit<1>(smem_u32(&bars->done));
+    if (!mbar_wait(smem_u32(&bars->done), 0, never, DRAIN_NS)) fail();   // (before the tensor memory goes)
+  } else if (warp >= 2) {
+    const bool ok = __all_sync(FULL, mbar_wait(smem_u32(&bars->done), 0, abort, p.limit_ns));
+    if (!ok && lane == 0) fail();
+    tc_fence_after();
+    const int r = 32 * (warp & 3) + lane;
+    for (int c = 0; c < p.bn; c += 16) {
+      float v[16];
+      tmem_ld16(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + c, v);
+      tmem_ld_wait();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sums[(c + i) * 128 + r] = v[i];
+    }
+    tc_fence_before();
+  }
+  __syncwarp();
+  cluster_sync();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, 128);
+  const int items = p.bn / VE * 128, lo = items * part / split, hi = items * (part + 1) / split;
+  for (int i = lo + (int)threadIdx.x; i < hi; i += SPLIT_THREADS) {
+    const int r = i & 127, c = (i >> 7) * VE;
+    const int64_t row = (int64_t)m0 + r;
+    if (row >= p.a.n || n0 + c >= p.a.M) continue;
+    float y[VE] = {};
+    for (int u = 0; u < split; ++u)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) y[e] += from_cta(smem_u32(sums + (c + e) * 128 + r), u);
+    const int64_t col = n0 + c;
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const uint4 gate = p.a.gate ? *reinterpret_cast<const uint4*>((const T*)p.a.gate + row * p.a.gs + col) : none;
+    const uint4 res = p.a.res ? *reinterpret_cast<const uint4*>((const T*)p.a.res + row * p.a.rs + col) : none;
+    finish<T, EIGHT>(p.a, y, EIGHT ? p.a.x_scales[row] : 1.0f, (int)col, gate, res);
+    *reinterpret_cast<uint4*>((T*)p.a.out + row * p.a.os + col) = pack(y, T());
+  }
+  cluster_sync();   // no CTA goes while another reads its sums
+}
+
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
     void* f = nullptr;
@@ -445,6 +571,34 @@ int launch(const ProductArgs& a, int bn, cudaStream_t st) {
 }
 
 template <class T, bool EIGHT>
+int launch_split(const ProductArgs& a, int bn, int split, cudaStream_t st) {
+  TcArgs p = {};
+  p.a = a;
+  const int size = EIGHT ? 1 : (int)sizeof(T);
+  const CUtensorMapDataType in = EIGHT ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : map_type<T>();
+  if (!make_map(&p.tx, a.x, a.n, a.K, a.xs, size, in, 128) || !make_map(&p.tw, a.w, a.M, a.K, a.ws, size, in, bn))
+    return TRACKFIT_ERR_CUDA;
+  p.tiles_m = (int)((a.n + 127) / 128), p.tiles_n = (a.M + bn - 1) / bn;
+  p.kblocks = (a.K * size + 127) / 128, p.bn = bn;
+  const int room = (SMEM - RESERVED - bn * 512) / ((128 + bn) * 128);
+  p.stages = room < MAX_STAGES ? room : MAX_STAGES;
+  p.idesc = idesc_f16(128, bn, !EIGHT && __is_same(T, __nv_bfloat16) ? 1u : 0u, false, false);
+  p.limit_ns = operator_limit_ns(), p.expired = operator_expired();
+  if (!p.expired) return TRACKFIT_ERR_CUDA;
+  constexpr auto kern = product_split_kernel<T, EIGHT>;
+  cudaError_t e = allow_smem<kern>(SMEM);
+  if (e != cudaSuccess) return tf_status_from_cuda(e);
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = split, at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(p.tiles_m * p.tiles_n * split)), cfg.blockDim = dim3(SPLIT_THREADS);
+  cfg.dynamicSmemBytes = SMEM, cfg.stream = st, cfg.attrs = &at, cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, kern, p, split);
+  return e == cudaSuccess ? launched() : tf_status_from_cuda(e);
+}
+
+template <class T, bool EIGHT>
 int by_tile(const ProductArgs& a, cudaStream_t st) {
   constexpr int PC = 128 / sizeof(T);
   auto tiles = [&](int rows, int bn) { return (a.n + rows - 1) / rows * ((a.M + bn - 1) / bn); };
@@ -458,6 +612,13 @@ int by_tile(const ProductArgs& a, cudaStream_t st) {
       if (b % PC == 0 && cost(b) < cost(bn)) bn = b;
     return launch<T, 2, EIGHT>(a, bn, st);
   }
+  // Few tiles and a long K: tiles of up to 64 outputs, each by a cluster, with four steps of K a CTA at least
+  // (100 x 4096 x 256: @SPLIT@).
+  const int steps = (a.K * (EIGHT ? 1 : (int)sizeof(T)) + 127) / 128;
+  const int sbn = a.M > 64 ? 64 : (a.M + 15) / 16 * 16;
+  int split = 1;
+  while (split < 8 && tiles(128, sbn) * split * 2 <= 152 && steps >= 8 * split) split *= 2;
+  if (split > 1) return launch_split<T, EIGHT>(a, sbn, split, st);
   // a tile as wide as the outputs, up to 256; where tiles are too few for the SMs, narrower, as long as the
   // pieces of outputs stay whole
   int bn = a.M > 256 ? 256 : (a.M + 15) / 16 * 16;
