@@ -12,10 +12,10 @@
 // far as they reach, so that it begins with a state that it knows.
 //
 // Long ones: what stands before a run of rows acts on it through one number a channel,
-// h_last = A h_before + B with A the product of the w.  A first kernel forms (A, B) of all windows
+// h_last = A h_before + B with A the product of the w.  A first kernel forms (A, B) of every warp's windows
 // from the first row of their segment (a CTA's rows) on, a second the states before the
-// segments, one after the other; then every window's first state is a few loads and multiply-adds
-// away.  So p and n are read twice.  (One pass, in which parts of 128 rows wait for what the part before
+// segments, one after the other; then the first state of every warp's windows is three loads and a
+// multiply-add away.  So p and n are read twice.  (One pass, in which parts of 128 rows wait for what the part before
 // leaves them, moves less, but was slower: with 128 rows under way in a CTA, a row's few instructions
 // and the look back at other CTAs' results take longer than the rows' transfer; 5 sequences of up to
 // 30,000 rows of 512 channels in bf16 took 205 us forward, tracks of 8 to 20 rows 390.)
@@ -62,10 +62,11 @@ struct GsArgs {
   float* saved;                            // [windows][C]: the state before a window
   int64_t windows, segments;
   int each, chunk;                         // windows of a segment's warp; positions whose sequences a warp takes
-  // long sequences: by window, what comes before it in its warp's windows; by warp, what comes before it in
-  // its segment; by segment, all of it and the state before it
-  float *win_a, *win_b, *warp_a, *warp_b, *seg_a, *seg_b, *seg_s;
-  uint32_t *win_has, *warp_has, *seg_has;
+  // long sequences: by warp, what comes before its windows in its segment; by segment, all of it and the
+  // state before it
+  int64_t units;                           // warps' windows
+  float *warp_a, *warp_b, *seg_a, *seg_b, *seg_s;
+  uint32_t *warp_has, *seg_has;
   unsigned long long* expired;
 };
 
@@ -170,6 +171,15 @@ __device__ __forceinline__ int64_t border_at(const GsArgs& a, const Order& o, in
     hi = nhi < hi ? nhi : hi;
   }
   return lo;
+}
+
+// The same, given the number j of one at or behind it: the borders below it, 32 at a time.
+__device__ __forceinline__ int64_t border_down(const GsArgs& a, const Order& o, int64_t pos, int64_t j, int lane) {
+  for (;;) {
+    const int n = __popc(__ballot_sync(FULL, j - 1 - lane >= 0 && border(a, o, j - 1 - lane) >= pos));
+    j -= n;
+    if (n < 32) return j;
+  }
 }
 
 // A window: up to 32 positions, all rows of sequences, and the sequences among them, bit i for the i-th.
@@ -279,7 +289,7 @@ __device__ __forceinline__ void empty_sequences(const GsArgs& a, float* to, cons
 
 // ---------------------------------------------------------------- long sequences: before the rows
 
-// (A, B) of the windows: of h, or (BACK) of e in the flipped order, where B = w (g + B).
+// (A, B) of the warps' windows: of h, or (BACK) of e in the flipped order, where B = w (g + B).
 template <class T, bool BACK>
 __global__ void __launch_bounds__(WARPS * 32, 3) sums_kernel(const __grid_constant__ GsArgs a) {
   using L = Lane<T>;
@@ -309,18 +319,12 @@ __global__ void __launch_bounds__(WARPS * 32, 3) sums_kernel(const __grid_consta
   extent(a, o, lo, hi);
   if (w0 < a.windows) next = border_at(a, o, w0 * WINDOW > lo ? w0 * WINDOW : lo, lane);
   for (int e = 0; e < a.each && w0 + e < a.windows; ++e) {
-    if (in) {
-      put_state<L>(a.win_a + (w0 + e) * a.C + c, fa);
-      put_state<L>(a.win_b + (w0 + e) * a.C + c, fb);
-    }
-    if (lane == 0 && block == 0) a.win_has[w0 + e] = has;
     const int64_t pos = (w0 + e) * WINDOW;
     if (pos >= hi || pos + WINDOW <= lo) continue;
     const Window m = window_at(a, o, pos, lo, hi, next, lane, next);
     bring<2>(buffer, full, o, m.pos, c0, &a.tp, BACK ? &a.tg : &a.tn, nullptr);
     ok = brought(full, parity) && ok;
     parity ^= 1;
-    const uint32_t slow = states ? m.begins : 0u;
     for (int i0 = 0; i0 < m.count; i0 += GROUP) {
       P w[GROUP], x[GROUP];
 #pragma unroll
@@ -338,9 +342,9 @@ __global__ void __launch_bounds__(WARPS * 32, 3) sums_kernel(const __grid_consta
         if constexpr (BACK) fb = L::mul(w[i], L::add(x[i], before));
         else fb = L::fma(w[i], before, x[i]);
       };
-      if (left >= GROUP && (slow >> i0 & GROUP_BITS) == 0) {
+      if (left >= GROUP && (m.begins >> i0 & GROUP_BITS) == 0) {
 #pragma unroll
-        for (int i = 0; i < GROUP; ++i) row(i, L::pick((m.begins >> (i0 + i)) & 1u, L::make(0.0f, 0.0f), fb));
+        for (int i = 0; i < GROUP; ++i) row(i, fb);
       } else {
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) {
@@ -400,18 +404,13 @@ __global__ void __launch_bounds__(64) chain_kernel(const __grid_constant__ GsArg
   }
 }
 
-// What comes into a window from before it.
+// What comes into a warp's windows from before them.
 template <class L>
-__device__ __forceinline__ typename L::P into(const GsArgs& a, int64_t window, int c, bool in) {
-  using P = typename L::P;
-  P h = L::make(0.0f, 0.0f);
+__device__ __forceinline__ typename L::P into(const GsArgs& a, int64_t unit, int c, bool in) {
+  typename L::P h = L::make(0.0f, 0.0f);
   if (in) {
-    const int64_t unit = window / a.each, seg = unit / WARPS;
-    const P wa = get_state<L>(a.win_a + window * a.C + c), wb = get_state<L>(a.win_b + window * a.C + c);
-    const P ua = get_state<L>(a.warp_a + unit * a.C + c), ub = get_state<L>(a.warp_b + unit * a.C + c);
-    const P s = get_state<L>(a.seg_s + seg * a.C + c);
-    const P u = L::pick(a.warp_has[unit] != 0, ub, L::fma(ua, s, ub));
-    h = L::pick(a.win_has[window] != 0, wb, L::fma(wa, u, wb));
+    h = get_state<L>(a.warp_b + unit * a.C + c);
+    if (!a.warp_has[unit]) h = L::fma(get_state<L>(a.warp_a + unit * a.C + c), get_state<L>(a.seg_s + unit / WARPS * a.C + c), h);
   }
   return h;
 }
@@ -440,7 +439,13 @@ __device__ __forceinline__ void window_forward(const GsArgs& a, const Window& m,
     }
     const int left = in ? m.count - i0 : 0;
     const uint32_t begins = m.begins >> i0;
-    if (((slow | ends) >> i0 & GROUP_BITS) == 0) {
+    if (left >= GROUP && ((m.begins | ends) >> i0 & GROUP_BITS) == 0) {
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i, out += step) {
+        h = L::fma(w[i], h, x[i]);
+        L::put(out, h);
+      }
+    } else if (((slow | ends) >> i0 & GROUP_BITS) == 0) {
 #pragma unroll
       for (int i = 0; i < GROUP; ++i, out += step) {
         h = L::fma(w[i], L::pick((begins >> i) & 1u, L::make(0.0f, 0.0f), h), x[i]);
@@ -489,19 +494,26 @@ __global__ void __launch_bounds__(WARPS * 32, 3) rows_kernel(const __grid_consta
   extent(a, o, lo, hi);
   if constexpr (LONG) {
     // the last windows first: their rows are in L2, from the sums
-    const int64_t k = a.windows - 1 - unit / a.blocks;
-    const int64_t pos = k * WINDOW, from = pos < lo ? lo : pos;
-    if (k < 0 || from >= hi || from >= pos + WINDOW) {
+    const int64_t u = a.units - 1 - unit / a.blocks;
+    const int64_t first = u * a.each * WINDOW, upto = first + a.each * WINDOW < hi ? first + a.each * WINDOW : hi;
+    const int64_t from = first < lo ? lo : first;
+    if (u < 0 || from >= upto) {
       after_kernels_before();
       return;
     }
-    bring<2>(buffer, full, o, from, c0, &a.tp, &a.tn, nullptr);
-    const Window m = window_at(a, o, pos, lo, hi, border_at(a, o, from, lane), lane, next);
-    after_kernels_before();
-    if (!(m.begins & 1u)) h = into<L>(a, k, c, in);
-    if (a.saved && in) put_state<L>(a.saved + k * a.C + c, h);
-    ok = brought(full, 0);
-    window_forward<T>(a, m, walk, c, in, h);
+    uint32_t parity = 0;
+    next = border_at(a, o, from, lane);
+    for (int64_t pos = from / WINDOW * WINDOW; pos < upto && ok; pos += WINDOW, parity ^= 1) {
+      bring<2>(buffer, full, o, pos < lo ? lo : pos, c0, &a.tp, &a.tn, nullptr);
+      const Window m = window_at(a, o, pos, lo, hi, next, lane, next);
+      if (parity == 0 && pos <= from) {
+        after_kernels_before();
+        if (!(m.begins & 1u)) h = into<L>(a, u, c, in);
+      }
+      if (a.saved && in) put_state<L>(a.saved + pos / WINDOW * a.C + c, h);
+      ok = brought(full, parity);
+      window_forward<T>(a, m, walk, c, in, h);
+    }
   } else {
     // the sequences that begin in [from, from + chunk)
     const int64_t from = k * a.chunk, upto = from + a.chunk;
@@ -650,18 +662,28 @@ __global__ void __launch_bounds__(BACK_WARPS * 32) back_kernel(const __grid_cons
   if (a.n_rows == 0) return;
   extent(a, o, lo, hi);
   if constexpr (LONG) {
-    const int64_t pos = k * WINDOW, from = pos < lo ? lo : pos;
-    if (k >= a.windows || from >= hi || from >= pos + WINDOW) {
+    // (windows as the flipped order's warps had them: from the last position on)
+    const int64_t end = (a.windows - k * a.each) * WINDOW, first = end - a.each * WINDOW;
+    const int64_t from = first < lo ? lo : first, upto = end < hi ? end : hi;
+    if (k >= a.units || from >= upto) {
       after_kernels_before();
       return;
     }
-    bring<3>(buffer, full, o, from, c0, &a.tp, &a.tn, &a.tg);
-    const Window m = window_at(a, o, pos, lo, hi, border_at(a, o, from, lane), lane, next);
-    after_kernels_before();
-    if (!((m.ends >> (m.count - 1)) & 1u)) e = into<L>(a, a.windows - 1 - k, c, in);
-    if (in) h = get_state<L>(a.saved + k * a.C + c);
-    ok = brought(full, 0);
-    window_backward<T>(a, m, walk, c, in, h, e);
+    uint32_t parity = 0;
+    int64_t j = border_at(a, o, upto, lane);
+    for (int64_t pos = (upto - 1) / WINDOW * WINDOW; pos + WINDOW > from && pos >= 0 && ok; pos -= WINDOW, parity ^= 1) {
+      const int64_t start = pos < lo ? lo : pos;
+      bring<3>(buffer, full, o, start, c0, &a.tp, &a.tn, &a.tg);
+      j = border_down(a, o, start, j, lane);
+      const Window m = window_at(a, o, pos, lo, hi, j, lane, next);
+      if (parity == 0 && pos + WINDOW >= upto) {
+        after_kernels_before();
+        if (!((m.ends >> (m.count - 1)) & 1u)) e = into<L>(a, k, c, in);
+      }
+      if (in) h = get_state<L>(a.saved + pos / WINDOW * a.C + c);
+      ok = brought(full, parity);
+      window_backward<T>(a, m, walk, c, in, h, e);
+    }
   } else {
     // the sequences that begin in [from, upto), the last window first
     const int64_t from = k * a.chunk, upto = from + a.chunk;
@@ -675,12 +697,7 @@ __global__ void __launch_bounds__(BACK_WARPS * 32) back_kernel(const __grid_cons
     uint32_t parity = 0;
     for (int64_t pos = run + (end - run - 1) / WINDOW * WINDOW; ok && end > run && pos >= run; pos -= WINDOW, parity ^= 1) {
       bring<3>(buffer, full, o, pos, c0, &a.tp, &a.tn, &a.tg);
-      // the first border at or behind the window's first position
-      for (;;) {
-        const int n = __popc(__ballot_sync(FULL, j - 1 - lane >= 0 && border(a, o, j - 1 - lane) >= pos));
-        j -= n;
-        if (n < 32) break;
-      }
+      j = border_down(a, o, pos, j, lane);
       const Window m = window_at(a, o, pos, lo, end, j, lane, next);
       if (in && pos > run) h = get_state<L>(a.saved + pos / WINDOW * a.C + c);
       ok = brought(full, parity);
@@ -779,7 +796,7 @@ int64_t windows_of(int64_t n_rows) { return (n_rows + WINDOW - 1) / WINDOW; }
 size_t workspace_bytes(int64_t n_rows, int64_t n_seq, int32_t channels) {
   if (!is_long(n_rows, n_seq)) return 0;
   const size_t w = windows_of(n_rows), s = (w + WARPS - 1) / WARPS;            // (segments at most)
-  return (w * 4 + s * 3 + n_seq) * channels * 4 + (2 * w + s) * 4;
+  return (w * 2 + s * 3 + n_seq) * channels * 4 + (w + s) * 4;
 }
 
 // A call of the scan, forward or backward.
@@ -839,9 +856,10 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
     a.each = 8;
     while (a.each > 1 && (a.windows + WARPS * a.each - 1) / (WARPS * a.each) * a.blocks < 2 * 152) a.each /= 2;
     a.segments = (a.windows + WARPS * a.each - 1) / (WARPS * a.each);
-    const int64_t per = a.windows * a.C, seg = a.segments * a.C, units = (a.windows + a.each - 1) / a.each;
-    a.win_a = (float*)f.workspace, a.win_b = a.win_a + per, a.warp_a = a.win_b + per, a.warp_b = a.warp_a + units * a.C;
-    a.seg_a = a.warp_b + units * a.C, a.seg_b = a.seg_a + seg, a.seg_s = a.seg_b + seg;
+    a.units = (a.windows + a.each - 1) / a.each;
+    const int64_t seg = a.segments * a.C;
+    a.warp_a = (float*)f.workspace, a.warp_b = a.warp_a + a.units * a.C;
+    a.seg_a = a.warp_b + a.units * a.C, a.seg_b = a.seg_a + seg, a.seg_s = a.seg_b + seg;
     if (a.segments * a.blocks > 0x7fffffff) return TRACKFIT_ERR_UNSUPPORTED;
     // the states given are read again where their sequences begin (end), when the state after a sequence
     // may already stand in the same place: then from a copy
@@ -852,7 +870,7 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
       if (e != cudaSuccess) return tf_status_from_cuda(e);
       given = copy;
     }
-    a.win_has = (uint32_t*)(copy + a.n_seq * a.C), a.warp_has = a.win_has + a.windows, a.seg_has = a.warp_has + units;
+    a.warp_has = (uint32_t*)(copy + a.n_seq * a.C), a.seg_has = a.warp_has + a.units;
     constexpr auto sums = sums_kernel<T, BACK>;
     constexpr size_t smem = 2 * BLOCK * WARPS;
     const cudaError_t e = allow_smem<sums>(smem + 8192);
@@ -860,7 +878,7 @@ int launch(const Call& f, GsArgs& a, cudaStream_t st) {
     sums<<<(unsigned)(a.segments * a.blocks), WARPS * 32, smem, st>>>(a);
     const cudaError_t e1 = follow(chain_kernel, (unsigned)((a.C + 63) / 64), 64, 0, st, a);
     if (e1 != cudaSuccess) return tf_status_from_cuda(e1);
-    n_units = a.windows * a.blocks;
+    n_units = a.units * a.blocks;
   } else {
     // 128 rows a warp: the rest of its last sequence is a few rows more; fewer where warps are few
     a.chunk = 128;

@@ -1,7 +1,7 @@
 // Rows times a weight matrix and the product's epilogue:
 //   out = residual + act(x W^T [* x_scales w_scales] + bias) * sigma(gate)
 //
-// Up to 64 rows of 16 or 8 bits go to product_few.cu, more to product_tc.cu, fp32 to the kernel here:
+// Up to 16 rows of 16 or 8 bits go to product_few.cu, more to product_tc.cu, fp32 to the kernel here:
 // tiles on the CUDA cores, 16 channels at a time through two buffers in shared memory, the next one's
 // loads under way while one is used.  A thread adds up RM x RN sums, two neighbouring ones in an
 // instruction, in fp32 and in the order of the channels.  Where tiles are few, a cluster of CTAs has a

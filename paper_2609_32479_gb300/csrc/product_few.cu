@@ -1,4 +1,4 @@
-// Rows times a weight matrix for up to 64 rows of 16 or 8 bits: the weights are read once, and that
+// Rows times a weight matrix for up to 16 rows of 16 or 8 bits: the weights are read once, and that
 // bounds it.
 //
 // A warp takes 16 outputs and a part of K with the weights as the product's A (16 x 16) and the rows
@@ -40,7 +40,7 @@ __device__ __forceinline__ uint4 load16(const uint8_t* p, bool there) {
 template <class T, bool EIGHT, int NT>
 __global__ void __launch_bounds__(WARPS * 32) product_few_kernel(const ProductArgs a) {
   constexpr int SZ = EIGHT ? 1 : 2, KS = 64 / SZ;     // channels that four lanes' 16 bytes hold
-  constexpr int ROWS = 8 * NT, AHEAD = NT <= 2 ? 4 : 2;
+  constexpr int ROWS = 8 * NT, AHEAD = 4;
   __shared__ float sums[WARPS][ROWS][17];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int m0 = blockIdx.x * 16;
@@ -110,9 +110,7 @@ template <class T, bool EIGHT>
 int launch(const ProductArgs& a, cudaStream_t st) {
   const unsigned grid = (unsigned)((a.M + 15) / 16);
   if (a.n <= 8) product_few_kernel<T, EIGHT, 1><<<grid, WARPS * 32, 0, st>>>(a);
-  else if (a.n <= 16) product_few_kernel<T, EIGHT, 2><<<grid, WARPS * 32, 0, st>>>(a);
-  else if (a.n <= 32) product_few_kernel<T, EIGHT, 4><<<grid, WARPS * 32, 0, st>>>(a);
-  else product_few_kernel<T, EIGHT, 8><<<grid, WARPS * 32, 0, st>>>(a);
+  else product_few_kernel<T, EIGHT, 2><<<grid, WARPS * 32, 0, st>>>(a);
   return launched();
 }
 

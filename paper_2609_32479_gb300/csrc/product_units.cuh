@@ -109,8 +109,9 @@ __device__ __forceinline__ void finish(const ProductArgs& a, float (&y)[VE], flo
 
 // product_tc.cu: 16-bit and 8-bit operands by the tensor cores, many rows.
 int product_tc(int32_t dtype, const ProductArgs& a, cudaStream_t st);
-// product_few.cu: few rows, where the weights are what is read.
-constexpr int PRODUCT_FEW = 64;
+// product_few.cu: few rows, where the weights are what is read (24 rows through 4096 x 4096 in bf16: 25 us
+// there, 19 by the tiles; 16: 21 and 19, but 9.0 and 10.9 through 1024 x 1024, 6.8 and 10.9 from 128 to 768).
+constexpr int PRODUCT_FEW = 16;
 int product_few(int32_t dtype, const ProductArgs& a, cudaStream_t st);
 
 }  // namespace seqops
