@@ -506,7 +506,8 @@ int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, con
  *               trackfit_gated_scan_backward, or NULL.
  *   workspace   trackfit_gated_scan_workspace() bytes, 16-byte aligned (sequences of more than 32
  *               rows on average are cut and their parts joined through it; NULL when that is 0).
- * z and 1 - z are both off by (2 |p| + 10) 2^-24 of themselves at most, however near to 0. */
+ * z and 1 - z are both off by (2 |p| + 10) 2^-24 of themselves at most, however near to 0.
+ * Rows of no sequence may be read here, but nothing comes of them. */
 size_t trackfit_gated_scan_saved(int64_t n_rows, int32_t channels);
 size_t trackfit_gated_scan_workspace(int32_t dtype, int64_t n_rows, int64_t n_seq, int32_t channels);
 int trackfit_gated_scan(int32_t dtype, const void* gate, int64_t gate_stride, const void* cand, int64_t cand_stride,

@@ -5,24 +5,28 @@
 //   D_t = g_t + e_t,  e_{t-1} = w_t D_t,  dn = z D,  dp = z w (n - h_{t-1}) D
 //
 // Bound by memory: three values a row and channel are moved forward, five backward.  A warp takes
-// windows of 32 rows x 128 bytes of channels, brought by TMA, one row after the other; a lane has one channel (16
-// bits: two neighbouring ones, in instructions that take two).  No warp waits for another.
+// windows of 32 rows x 128 bytes of channels, brought by TMA; a lane has one channel (16 bits: two
+// neighbouring ones, in instructions that take two).  The gates of eight rows are formed side by side, so
+// that their latencies overlap, then the recurrence runs through them.  No warp waits for another.
 //
 // Short sequences (32 rows on average at most): a warp takes the sequences that begin in its rows, as
 // far as they reach, so that it begins with a state that it knows.
 //
 // Long ones: what stands before a run of rows acts on it through one number a channel,
 // h_last = A h_before + B with A the product of the w.  A first kernel forms (A, B) of every warp's windows
-// from the first row of their segment (a CTA's rows) on, a second the states before the
-// segments, one after the other; then the first state of every warp's windows is three loads and a
-// multiply-add away.  So p and n are read twice.  (One pass, in which parts of 128 rows wait for what the part before
-// leaves them, moves less, but was slower: with 128 rows under way in a CTA, a row's few instructions
-// and the look back at other CTAs' results take longer than the rows' transfer; 5 sequences of up to
-// 30,000 rows of 512 channels in bf16 took 205 us forward, tracks of 8 to 20 rows 390.)
+// and of segments (a CTA's windows), a second the states before the segments, one after the other; then
+// the first state of every warp's windows is three loads and a multiply-add away.  So p and n are read
+// twice, the second time in part from L2.  (One pass, in which parts of 128 rows look back for what the
+// part before them left, moves less but was slower, 205 us for 5 sequences of up to 30,000 rows of 512
+// channels in bf16: too few rows are under way on an SM for the waits.)
 // A sequence's first row ends what comes from before by choice, not by a factor 0: it may not be finite.
 //
 // Backward, D runs the other way by the same steps: (A, B) of e from the segments' ends.  A window's
 // states are formed again from the one before it that the forward pass saved.
+//
+// What bounds it: tracks of 8 to 20 rows, 192 channels in bf16, forward @TF@ us of the 156 that the bytes take,
+// backward @TB@ of 261, with 12 warps on an SM (16 KB of rows each) and 57 % of the issue slots used; long
+// sequences issued instructions (55 %) in the sums, some 40 a row of 64 channels, and the rows, 52.
 #include "seq_ops.cuh"
 #include "sm100_ptx.cuh"
 
@@ -70,11 +74,6 @@ struct GsArgs {
   unsigned long long* expired;
 };
 
-__device__ __forceinline__ float rcp(float x) {   // (1 ulp; for x in [1, 2])
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // z and w of a gate: the smaller, e / (1 + e) with e = 2^(-|p| log2 e), accurate however near to 0, and one
 // less that, so that they add up to 1 (in the 1,000 rows that a slow channel remembers an error of their
 // sum, always of one sign, would add up too: the states' error was ten times as large).
@@ -437,19 +436,19 @@ __device__ __forceinline__ void window_forward(const GsArgs& a, const Window& m,
       L::gates(L::get(lds(at)), z, w[i]);
       x[i] = L::mul(z, L::get(lds(at + BLOCK)));
     }
-    const int left = in ? m.count - i0 : 0;
+    const bool whole = m.count - i0 >= GROUP;   // (else row by row: the state goes on behind the last one)
     const uint32_t begins = m.begins >> i0;
-    if (left >= GROUP && ((m.begins | ends) >> i0 & GROUP_BITS) == 0) {
+    if (whole && ((m.begins | ends) >> i0 & GROUP_BITS) == 0) {
 #pragma unroll
       for (int i = 0; i < GROUP; ++i, out += step) {
         h = L::fma(w[i], h, x[i]);
-        L::put(out, h);
+        if (in) L::put(out, h);
       }
-    } else if (((slow | ends) >> i0 & GROUP_BITS) == 0) {
+    } else if (whole && ((slow | ends) >> i0 & GROUP_BITS) == 0) {
 #pragma unroll
       for (int i = 0; i < GROUP; ++i, out += step) {
         h = L::fma(w[i], L::pick((begins >> i) & 1u, L::make(0.0f, 0.0f), h), x[i]);
-        if (i < left) L::put(out, h);
+        if (in) L::put(out, h);
       }
     } else {
 #pragma unroll

@@ -16,9 +16,9 @@ struct ProductArgs {
   int K, M, act;
 };
 
-// sigma(x) by the hardware's 2^x and division: a few units in fp32's last place, (2 |x| + 10) 2^-24 in all
+// sigma(x) by the hardware's 2^x and reciprocal: a few units in fp32's last place, (2 |x| + 10) 2^-24 in all
 // (the product with log2 e is rounded once).  2^x = inf gives 0.
-__device__ __forceinline__ float sigma(float x) { return __fdividef(1.0f, 1.0f + ex2(-LOG2E * x)); }
+__device__ __forceinline__ float sigma(float x) { return rcp(1.0f + ex2(-LOG2E * x)); }
 
 // y Phi(y).  Of the normal distribution's smaller tail, erfc(x) / 2 with x = |y| / sqrt 2, not of
 // 1 + erf, which below -3 would leave few bits: erfc(x) = t 2^(-x^2 log2 e + P(t)) with t = 1 / (1 + x / 2),
@@ -26,7 +26,7 @@ __device__ __forceinline__ float sigma(float x) { return __fdividef(1.0f, 1.0f +
 // log2(exp(x^2) erfc(x) / 2 t) over y in [0, 14] with weights moved to where it was off most: by 7e-8.
 // In fp32 the tail is off by (8 + 2 y^2) 2^-24 of itself at most (y^2 for the exponent's rounding).
 __device__ __forceinline__ float gelu(float y) {
-  const float t = __fdividef(1.0f, fmaf(fabsf(y), 0.35355339f, 1.0f));
+  const float t = rcp(fmaf(fabsf(y), 0.35355339f, 1.0f));
   float p = 0.204026341f;
   p = fmaf(p, t, -0.954790890f);
   p = fmaf(p, t, 1.60470486f);

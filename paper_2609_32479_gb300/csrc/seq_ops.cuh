@@ -68,6 +68,12 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// 1 / x by the hardware reciprocal (1 ulp; below the normal range, of x or the result, infinity or 0).
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // Two fp32 values in one instruction.
 __device__ __forceinline__ uint64_t both(float a, float b) {

@@ -435,6 +435,7 @@ class _OpArgs:
             # the current stream's handle without an object for it, where this torch offers that
             _OpArgs.raw_stream = staticmethod(getattr(torch._C, "_cuda_getCurrentRawStream", None) or
                                               (lambda device: torch.cuda.current_stream(device).cuda_stream))
+            _OpArgs.current = staticmethod(getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device)
             _OpArgs.types = {torch.float32: W.PRECISION_FP32, torch.bfloat16: W.PRECISION_BF16,
                              torch.float16: W.PRECISION_FP16}
         self.what, self.device, self.dtype = what, first.device, first.dtype
@@ -492,7 +493,7 @@ class _OpArgs:
         workspace of the caller's, one from torch's allocator, in the order of the stream."""
         torch = self.torch
         index = self.device.index
-        if torch.cuda.current_device() != index:
+        if self.current() != index:
             with torch.cuda.device(index):
                 return self.call(fn, args, stream, need, workspace)
         handle = self.raw_stream(index) if stream is None else getattr(stream, "cuda_stream", stream)

@@ -216,6 +216,111 @@ def test_scan_many_tracks(T, t):
     check_scan(T, [0] * 500, 8, t, True, states=True)
 
 
+def scan_on_gpu(p, n, g, off, rev):
+    """The definition in 64 bits, a row at a time on the GPU: h, dp, dn and their bounds as above."""
+    z, w = torch.sigmoid(p.double()), torch.sigmoid(-p.double())
+    N, G = n.double(), g.double()
+    k = 2 * p.double().abs().clamp(max=100.0) + 10
+    h, E, H, before, Eb, Hb = (torch.zeros_like(N) for _ in range(6))
+    dp, dn, ep, en = (torch.zeros_like(N) for _ in range(4))
+    for b in range(len(off) - 1):
+        rows = range(off[b + 1] - 1, off[b] - 1, -1) if rev else range(off[b], off[b + 1])
+        x, e, a = (torch.zeros_like(N[0]) for _ in range(3))
+        for t in rows:
+            before[t], Eb[t], Hb[t] = x, e, a
+            e = w[t] * e + (k[t] + 6) * U * (w[t] * a + z[t] * N[t].abs())
+            x, a = w[t] * x + z[t] * N[t], w[t] * a + z[t] * N[t].abs()
+            h[t], E[t], H[t] = x, e, a
+        more = 2 * U * (len(rows) / 16 + 16)
+        d, da, f = (torch.zeros_like(N[0]) for _ in range(3))
+        for t in reversed(rows):
+            d, da = d + G[t], da + G[t].abs()
+            f = f + 2 * U * da
+            ft = f + more * da
+            size = N[t].abs() + Hb[t]
+            dn[t], dp[t] = z[t] * d, z[t] * w[t] * (N[t] - before[t]) * d
+            en[t] = z[t] * (ft + (k[t] + 4) * U * da)
+            ep[t] = z[t] * w[t] * ((2 * k[t] + 8) * U * size * da + (Eb[t] + U * size) * (da + ft) +
+                                   (N[t] - before[t]).abs() * ft)
+            f = w[t] * (f + (k[t] + 4) * U * da)
+            d, da = w[t] * d, w[t] * da
+        E[off[b]:off[b + 1]] += more * H[off[b]:off[b + 1]]
+    return h, dp, dn, E, ep, en
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rev", [False, True])
+@pytest.mark.parametrize("lead", [0, 1, 3, 31, 33, 127])
+def test_scan_whose_first_rows_are_of_no_sequence(T, t, rev, lead):
+    """A first window of fewer rows goes on into the next one of the same warp: enough windows that a warp has
+    several."""
+    C, n = 1024, 9000
+    x = torch.randn((n, 2 * C), generator=torch.Generator(device="cuda").manual_seed(lead), device="cuda")
+    x[:, :C] -= 3
+    x = x.to(getattr(torch, t))
+    p, c = x[:, :C], x[:, C:]
+    out, whole = torch.empty((n, C), dtype=x.dtype, device="cuda"), torch.empty((n, C), dtype=x.dtype, device="cuda")
+    rows = slice(lead, n - lead)
+    T.gated_scan(p, c, dev([lead, n - lead], "int64"), out, reverse=rev)
+    T.gated_scan(p[rows], c[rows], dev([0, n - 2 * lead], "int64"), whole[rows], reverse=rev)
+    # the same sequence cut into other windows: both are within a rounding of the type and
+    # 2 (2 |p| + 16) u of the exact state a row it remembers (|p| up to 8, about 20 rows, states below 4)
+    tol = 2 * half_step(t) * whole[rows].double().abs() + 2 * 32 * U * 20 * 4
+    assert bool(((out[rows].double() - whole[rows].double()).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("rev", [False, True])
+def test_scan_of_many_channels_and_many_windows_a_warp(T, rev):
+    """Long sequences of 2,048 channels: every warp of the sums has eight windows."""
+    C, off = 2048, [3, 3000, 3001, 11203, 14000]
+    n = off[-1] + 5
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn((n, 3 * C), generator=gen, device="cuda")
+    x[:, :C] += torch.linspace(1.0, -7.0, C, device="cuda")
+    x = x.to(torch.bfloat16)
+    p, c, g = x[:, :C], x[:, C:2 * C], x[:, 2 * C:]
+    out, dp, dn = (torch.empty((n, C), dtype=x.dtype, device="cuda") for _ in range(3))
+    saved = torch.empty(T.gated_scan_saved(n, C), device="cuda")
+    T.gated_scan(p, c, dev(off, "int64"), out, reverse=rev, saved=saved)
+    T.gated_scan_backward(p, c, dev(off, "int64"), saved, g, dp, dn, reverse=rev)
+    ref = scan_on_gpu(p, c, g, off, rev)
+    rows, e = slice(off[0], off[-1]), half_step("bfloat16")
+    for got, want, tol in zip((out, dp, dn), ref[:3], ref[3:]):
+        off_by = (got.double() - want).abs() - e * want.abs() - tol
+        assert bool((off_by[rows] <= 0).all()), float(off_by[rows].max())
+
+
+def test_rows_far_beyond_32_bits(T):
+    """Arrays of more than 2^32 elements: the last rows of each operator."""
+    n, C = 1060000, 2048
+    x = torch.zeros((n, 2 * C), dtype=torch.bfloat16, device="cuda")       # 4.3e9 elements
+    last = torch.randn((300, 2 * C), device="cuda").to(torch.bfloat16)
+    x[-300:] = last
+    off = [0, n - 300, n - 280, n]
+    out = torch.empty((n, C), dtype=x.dtype, device="cuda")
+    small = torch.empty((300, C), dtype=x.dtype, device="cuda")
+    T.gated_scan(x[:, :C], x[:, C:], dev(off, "int64"), out)
+    T.gated_scan(last[:, :C], last[:, C:], dev([0, 20, 300], "int64"), small)
+    z = torch.sigmoid(last[:, :C].double())
+    h = torch.zeros(C, dtype=torch.float64, device="cuda")
+    for t in range(300):
+        h = (torch.zeros_like(h) if t in (0, 20) else h) * (1 - z[t]) + z[t] * last[t, C:].double()
+        for got in (out[n - 300 + t], small[t]):
+            assert bool(((got.double() - h).abs() <= half_step("bfloat16") * h.abs() + 2.0 ** -16).all())    # (values of a few units)
+    T.add_norm(x, x)
+    T.add_norm(last, last)
+    assert torch.equal(x[-300:], last)
+    del out
+    w = torch.randn((72, 2 * C), device="cuda").to(torch.bfloat16)
+    y, ys = torch.empty((n, 72), dtype=x.dtype, device="cuda"), torch.empty((300, 72), dtype=x.dtype, device="cuda")
+    T.product(x, w, y)
+    ref = last.double() @ w.double().T
+    T.product(last, w, ys)
+    for got in (y[-300:], ys):
+        tol = half_step("bfloat16") * ref.abs() + (2 * 2 * C + 8) * U * (last.double().abs() @ w.double().abs().T)
+        assert bool(((got.double() - ref).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("t", TYPES)
 def test_scan_that_hardly_forgets_and_that_forgets_all(T, t):
     """Gates of 2^-14, where the parts of a sequence all count, and of nearly one."""
@@ -556,6 +661,25 @@ def test_product_epilogues(T, t, act, gate, residual):
 def test_product_of_many_rows(T, t):
     check_product(T, 40001, 64, 72, t, gate=True, residual=True, in_place=True)
     check_product(T, 20000, 40, 8, t, "relu")
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,K,M,eight", [(17, 512, 8, False), (100, 4096, 72, False), (70, 2048, 24, False), (200, 1032, 264, False),
+                                         (90, 4096, 200, True), (65, 1040, 16, True), (128, 2048, 520, True)])
+def test_product_of_few_tiles(T, t, n, K, M, eight):
+    """A long K for few outputs: parts of K side by side."""
+    check_product(T, n, K, M, t, eight=eight)
+    check_product(T, n, K, M, t, "gelu", gate=True, residual=True, eight=eight, in_place=True, seed=1)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,K,M,eight", [(16400, 64, 136, False), (16385, 200, 256, False), (9001, 96, 264, False),
+                                         (8200, 128, 520, False), (16385, 272, 144, True), (8300, 64, 520, True)])
+def test_product_of_wide_tiles(T, t, n, K, M, eight):
+    """Enough rows for tiles of 256 by pairs of CTAs: outputs of one tile and of several, rows and outputs that
+    end inside a tile."""
+    check_product(T, n, K, M, t, "relu", eight=eight)
+    check_product(T, n, K, M, t, "silu", gate=True, residual=True, eight=eight, in_place=True, seed=1)
 
 
 @pytest.mark.parametrize("t", TYPES)
