@@ -504,7 +504,7 @@ int trackfit_cross_attention(int32_t dtype, const void* q, int64_t q_stride, con
  *               before it), or NULL; may be state_in.
  *   saved       trackfit_gated_scan_saved() bytes, 16-byte aligned, for
  *               trackfit_gated_scan_backward, or NULL.
- *   workspace   trackfit_gated_scan_workspace() bytes, 16-byte aligned (sequences of more than 32
+ *   workspace   trackfit_gated_scan_workspace() bytes, 16-byte aligned (sequences of more than 64
  *               rows on average are cut and their parts joined through it; NULL when that is 0).
  * z and 1 - z are both off by (2 |p| + 10) 2^-24 of themselves at most, however near to 0.
  * Rows of no sequence may be read here, but nothing comes of them. */

@@ -6,7 +6,7 @@
 // loads under way while one is used.  A thread adds up RM x RN sums, two neighbouring ones in an
 // instruction, in fp32 and in the order of the channels.  Where tiles are few, a cluster of CTAs has a
 // tile, each a part of the channels; each adds up some of the tile's sums out of all parts, in their
-// order.  4000 x 2048 x 4096: 1293 us, 52 TFLOP/s of about 74 that the multipliers could.
+// order.  4000 x 2048 x 4096: 1265 us, 53 TFLOP/s of about 75 that the multipliers could.
 #include "product_units.cuh"
 
 namespace {

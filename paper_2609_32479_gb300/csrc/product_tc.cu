@@ -14,6 +14,12 @@
 //               thread has a row of the piece, puts it into the piece's slot and a warp stores its
 //               32 rows by TMA.  (Stores and loads a row a thread would touch 32 lines each.)
 //
+// Measured: 8011 x 4096 x 4096 in bf16 166 us, 1,618 TFLOP/s (the library's product alone 171), with gelu in
+// fp16 177 to 195 as the card's power lets it, in 8 bits 95 to 102, 2,700 TFLOP/s; bound by the operands' way
+// into the SM (256 rows of 128 bytes a step) and the power.  1,310,003 x 256 x 128, gated onto a residual: 244 us,
+// the bytes at the rate of a copy.  With K small and an activation the epilogue's eight warps bound it:
+// 100,000 x 256 x 896 with silu 119 us of 34.
+//
 // Every wait is limited; one that expires sets the CTA's flag, on which all others give up too,
 // and is counted for trackfit_operator_errors().
 #include "product_units.cuh"

@@ -68,7 +68,7 @@ def test_scan_sizes(lib):
     assert 4 * T.gated_scan_saved(1000, 24) == saved(1000, 24) >= 8 * 24 * 4
     for bad in ((5, 100, 1, 64), (1, -1, 1, 64), (1, 100, -1, 64), (1, 100, 1, 60)):
         assert ws(*bad) == 0
-    assert ws(1, 640, 20, 64) == 0 and ws(1, 641, 20, 64) > 0
+    assert ws(1, 1280, 20, 64) == 0 and ws(1, 1281, 20, 64) > 0
     for t in range(3):
         n = ws(t, 100000, 3, 64)
         assert ws(t, 0, 3, 64) == 0 and ws(t, 200000, 3, 64) >= n
